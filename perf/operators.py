@@ -1,0 +1,578 @@
+"""Cases for the operators of the 8-bit paged K/V cache: attention over the cache, the quantising write of new K/V,
+and the page operations (reserve, fork, free, compact).
+
+A cache holds, for every layer, page and KV head, 128 tokens of 128 one-byte codes for K and for V and one scale each;
+`page_table` [max_seqs, max_pages], `seq_lens` [max_seqs] and `page_refs` [n_pages] are shared by the layers.  A new
+token of a sequence is one of the last positions that its length covers.  `run` computes one pass in plain torch, or
+(with `own`) through the framework's calls, which change the cache's tensors in place.
+"""
+import math
+import random
+
+import torch
+
+own = False
+
+PAGE, DIM = 128, 128
+LARGEST = {"e4m3": 448.0, "int8": 127.0}       # largest code: the scale 2^e is the smallest that brings a block within it
+LEAD = {"e4m3": (1.75, 8), "int8": (1.984375, 6)}  # the same number as mantissa * 2^exponent
+LOWEST = -126                                   # smallest exponent of a scale
+
+
+# ------------------------------------------------------------------------------------------------ cases
+def listed():
+    def attn(name, fmt, hq, hkv, batch, lo, hi, new_lo, new_hi, shape):
+        return dict(name=name, op="attention", fmt=fmt, hq=hq, hkv=hkv, batch=batch, len_lo=lo, len_hi=hi,
+                    new_lo=new_lo, new_hi=new_hi, shape=shape)
+
+    def append(name, fmt, hkv, batch, lo, hi, new_lo, new_hi, shape):
+        return dict(name=name, op="append", fmt=fmt, hkv=hkv, batch=batch, len_lo=lo, len_hi=hi, new_lo=new_lo,
+                    new_hi=new_hi, shape=shape)
+
+    def pages(name, op, hkv, layers, batch, lo, hi, shape, beams=1):
+        return dict(name=name, op=op, fmt="e4m3", hkv=hkv, layers=layers, batch=batch, len_lo=lo, len_hi=hi,
+                    beams=beams, shape=shape)
+
+    return [
+        # one user, one short answer: what counts is latency
+        attn("attention one short", "e4m3", 4, 1, 1, 300, 300, 1, 1, 1),
+        # a server's step: many users at different lengths, one token each
+        attn("attention decode ragged", "e4m3", 32, 8, 32, 1, 8192, 1, 1, 2),
+        # a few long documents
+        attn("attention decode 128k", "int8", 32, 8, 4, 65536, 131072, 1, 1, 3),
+        # one very long document with groups of seven query heads
+        attn("attention decode 256k", "e4m3", 28, 4, 1, 262144, 262144, 1, 1, 4),
+        # a drafted continuation of five tokens is verified for every user
+        attn("attention verify", "e4m3", 32, 8, 16, 500, 16384, 5, 5, 5),
+        # a piece of a prompt over what is cached of it
+        attn("attention chunk", "e4m3", 32, 8, 1, 32768, 32768, 2048, 2048, 6),
+        # follow-up questions of all lengths over cached conversations
+        attn("attention follow-ups", "int8", 28, 4, 8, 700, 20000, 1, 700, 7),
+        # the step that belongs to the second case
+        append("append step", "e4m3", 8, 32, 1, 8192, 1, 1, 8),
+        # prompts enter the cache; their ends do not meet page borders
+        append("append prompts", "int8", 8, 3, 9000, 32768, 9000, 32768, 9),
+        # every step of a beam search: the old beams go, new ones leave the same prompts
+        pages("pages beams", "fork", 8, 8, 16, 200, 8000, 10, beams=4),
+        # half of the users have left: what stays moves to the front of the pool
+        pages("pages compact", "compact", 8, 2, 32, 1000, 16384, 11),
+        # users come and go, no page is moved
+        pages("pages turnover", "turnover", 8, 1, 64, 1, 16384, 12),
+    ]
+
+
+def _log(rng, lo, hi):
+    return min(hi, max(lo, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi + 0.49)))))))
+
+
+def draw(rng):
+    shape = rng.randrange(1 << 30)
+    fmt = rng.choice(("e4m3", "int8"))
+    op = rng.choice(("attention",) * 5 + ("append",) * 2 + ("fork", "compact", "turnover"))
+    if op == "attention":
+        hq, hkv = rng.choice(((4, 1), (32, 8), (28, 4), (8, 8), (16, 1), (6, 2)))
+        if rng.random() < 0.6:   # answering: one or a few new tokens
+            new_hi = rng.choice((1, 1, 1, 2, 4, 7))
+            batch = _log(rng, 1, 64)
+            hi = _log(rng, max(2, new_hi), max(64, min(262144, (1 << 22) // (batch * hkv))))
+            lo = rng.randint(new_hi, hi)
+            new_lo = rng.randint(1, new_hi)
+        else:                    # pieces of prompts
+            batch = _log(rng, 1, 8)
+            new_hi = _log(rng, 8, 2048 // batch)
+            hi = _log(rng, max(new_hi, 16), max(new_hi + 64, 32768 // batch))
+            lo = rng.randint(new_hi, hi)
+            new_lo = rng.randint(1, new_hi)
+        return dict(op=op, fmt=fmt, hq=hq, hkv=hkv, batch=batch, len_lo=lo, len_hi=hi, new_lo=new_lo, new_hi=new_hi,
+                    shape=shape)
+    if op == "append":
+        hkv = rng.choice((1, 2, 4, 8))
+        batch = _log(rng, 1, 64)
+        new_hi = _log(rng, 1, max(1, 65536 // batch))
+        hi = new_hi + _log(rng, 1, 4096)
+        return dict(op=op, fmt=fmt, hkv=hkv, batch=batch, len_lo=new_hi, len_hi=hi, new_lo=rng.randint(1, new_hi),
+                    new_hi=new_hi, shape=shape)
+    hkv, batch = rng.choice((1, 2, 4, 8)), _log(rng, 2, 32)
+    hi = _log(rng, 64, min(16384, 400000 // batch))
+    return dict(op=op, fmt=fmt, hkv=hkv, layers=rng.choice((1, 2) if op != "fork" else (1, 4, 8)), batch=batch,
+                len_lo=rng.randint(1, hi), len_hi=hi, beams=rng.randint(1, 4) if op == "fork" else 1, shape=shape)
+
+
+def _spread(rng, lo, hi, n):
+    """n lengths spread over [lo, hi] by their logarithm, the longest among them."""
+    return [hi] + [_log(rng, lo, hi) for _ in range(n - 1)]
+
+
+def _pages(n):
+    return -(-n // PAGE)
+
+
+def _shape(case):
+    """Lengths, new tokens and the pool's size of a case: the same for every seed."""
+    rng = random.Random(case["shape"])
+    lens = _spread(rng, case["len_lo"], case["len_hi"], case["batch"])
+    rng.shuffle(lens)
+    if case["op"] in ("attention", "append"):
+        new = _spread(rng, case["new_lo"], case["new_hi"], case["batch"])
+        rng.shuffle(new)
+        new = [min(a, b) for a, b in zip(new, lens)]
+    else:
+        new = [0] * case["batch"]
+    used = sum(_pages(x) for x in lens)
+    return lens, new, used
+
+
+def work(case):
+    lens, new, used = _shape(case)
+    h = case["hkv"]
+    if case["op"] == "attention":
+        n, hq = sum(new), case["hq"]
+        # row t of a sequence sees len - new + t + 1 keys
+        pairs = sum(m * (x - m) + m * (m + 1) // 2 for x, m in zip(lens, new))
+        scales = sum(_pages(x) for x in lens) * h * 8
+        return dict(bytes=sum(lens) * h * DIM * 2 + scales + n * hq * (DIM * 4 + 4), flops=4 * DIM * hq * pairs)
+    if case["op"] == "append":
+        return dict(bytes=sum(new) * h * DIM * (2 + 1) * 2, flops=0)
+    per_page = case["layers"] * h * (PAGE * DIM + 4) * 2
+    if case["op"] == "fork":
+        rows = sum(x % PAGE for x in lens) * case["beams"]
+        tables = 2 * 4 * case["beams"] * sum(_pages(x) for x in lens)
+        return dict(bytes=2 * rows * case["layers"] * h * DIM * 2 + tables, flops=0)
+    if case["op"] == "compact":
+        kept, _ = _compact_layout(case)
+        left = len(kept)
+        moved = sum(p >= left for p in kept)
+        return dict(bytes=2 * moved * per_page + 4 * (_pool(case) + left), flops=0)
+    gone, room = _turnover(case)
+    return dict(bytes=4 * (2 * sum(_pages(lens[i]) for i in gone) + 2 * sum(room) + 2 * _pool(case)), flops=0)
+
+
+def _pool(case):
+    _, new, used = _shape(case)
+    if case["op"] == "fork":
+        return used + 2 * case["batch"] * case["beams"] + 8
+    return used + used // 4 + 8
+
+
+def _compact_layout(case):
+    """The pages still in use, and which sequences hold them: every second one has left."""
+    lens, _, used = _shape(case)
+    order = list(range(_pool(case)))
+    random.Random(case["shape"] + 1).shuffle(order)
+    stay = [i for i in range(case["batch"]) if i % 2 == 0]
+    at, own_pages = 0, {}
+    for i, x in enumerate(lens):
+        own_pages[i] = order[at:at + _pages(x)]
+        at += _pages(x)
+    return [p for i in stay for p in own_pages[i]], {i: own_pages[i] for i in stay}
+
+
+def _turnover(case):
+    """Which sequences leave, and the pages that each newcomer needs (they are as long as those that left)."""
+    lens, _, _ = _shape(case)
+    gone = [i for i in range(case["batch"]) if i % 2 == 1]
+    return gone, [_pages(lens[i]) for i in gone]
+
+
+# ------------------------------------------------------------------------------------------------ inputs
+def _exponent(amax, fmt):
+    """Smallest e >= LOWEST with amax <= LARGEST 2^e, for finite amax >= 0 (exact)."""
+    lead, power = LEAD[fmt]
+    m, k = torch.frexp(amax)
+    e = torch.where(2 * m <= lead, k - 1 - power, k - power)
+    return torch.where(amax > 0, e, torch.full_like(e, LOWEST)).clamp(min=LOWEST).to(torch.int32)
+
+
+def _pow2(e):
+    """2^e in float32 for integers -126 <= e <= 127 (the bits of the float)."""
+    return ((e.to(torch.int32) + 127) << 23).view(torch.float32)
+
+
+def _codes(x, fmt):
+    """Values in units of their block's scale to bytes: nearest, ties to even; infinities to the largest code."""
+    if fmt == "e4m3":
+        return x.clamp(-448.0, 448.0).to(torch.float8_e4m3fn).view(torch.uint8)
+    return torch.nan_to_num(x.clamp(-127.0, 127.0).round(), nan=0.0).to(torch.int8).view(torch.uint8)
+
+
+def _values(codes, fmt):
+    return codes.view(torch.float8_e4m3fn if fmt == "e4m3" else torch.int8).float()
+
+
+def _pool_of(case, n_pages, layers, gen, dev):
+    """Codes and scales of a pool as earlier writes would have left them: Gaussian K with some strong channels, V."""
+    out = []
+    for kind in range(2):
+        x = torch.randn(layers, n_pages, case["hkv"], PAGE, DIM, generator=gen, device=dev, dtype=torch.float16)
+        if kind == 0:
+            x[..., ::16] *= 3.0
+        x *= torch.rand(layers, n_pages, case["hkv"], 1, 1, generator=gen, device=dev).mul_(1.5).add_(0.5).half()
+        amax = x.abs().amax((-1, -2)).float()
+        scale = _pow2(_exponent(amax, case["fmt"]))
+        x *= (1.0 / scale).half()[..., None, None]
+        out += [_codes(x, case["fmt"]), scale]
+    return out
+
+
+def prepare(case, seed):
+    dev = torch.device("cuda")
+    gen = torch.Generator(device=dev).manual_seed(int(seed) * 7919 + 13)
+    lens, new, used = _shape(case)
+    layers = case.get("layers", 1)
+    n_pages, batch, beams = _pool(case), case["batch"], case.get("beams", 1)
+    kc, ks, vc, vs = _pool_of(case, n_pages, layers, gen, dev)
+    max_seqs = batch * (1 + beams) if case["op"] == "fork" else batch
+    max_pages = max(_pages(x) for x in lens)
+
+    order = list(range(n_pages))
+    random.Random(int(seed) if case["op"] != "compact" else case["shape"] + 1).shuffle(order)
+    meta = torch.zeros(max_seqs * max_pages + max_seqs + n_pages, dtype=torch.int32)
+    table, seq_lens, refs = _split(meta, max_seqs, max_pages)
+    table.fill_(-1)
+    at = 0
+    for i, x in enumerate(lens):
+        if case["op"] == "compact" and i % 2 == 1:   # has left already
+            at += _pages(x)
+            continue
+        table[i, :_pages(x)] = torch.tensor(order[at:at + _pages(x)], dtype=torch.int32)
+        refs[order[at:at + _pages(x)]] = 1
+        seq_lens[i] = x
+        at += _pages(x)
+    first = meta.to(dev)
+    meta = first.clone()
+    table, seq_lens, refs = _split(meta, max_seqs, max_pages)
+    s = dict(case=case, k_codes=kc, v_codes=vc, k_scale=ks, v_scale=vs, page_table=table, seq_lens=seq_lens,
+             page_refs=refs, meta=meta, first=first, max_new=max(new), max_len=max(lens))
+    ids = list(range(batch))
+    random.Random(int(seed) + 5).shuffle(ids)   # the batch's order is not the cache's
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device=dev)  # noqa: E731
+    s["seq_ids"] = i32(ids)
+    cu = [0]
+    for i in ids:
+        cu.append(cu[-1] + new[i])
+    uniform = len(set(new)) == 1
+    s["cu_tokens"] = None if uniform else i32(cu)
+    s["cu"] = i32(cu)
+    if case["op"] == "attention":
+        s["q"] = torch.randn(cu[-1], case["hq"], DIM, generator=gen, device=dev).bfloat16()
+    elif case["op"] == "append":
+        s["k"], s["v"] = (torch.randn(cu[-1], case["hkv"], DIM, generator=gen, device=dev).bfloat16() for _ in range(2))
+        s["k"][:, :, ::16] *= 3.0
+    elif case["op"] == "fork":
+        s["src"] = i32([i for i in ids for _ in range(beams)])
+        s["dst"] = i32([batch + k for k in range(batch * beams)])
+    elif case["op"] == "turnover":
+        gone, _ = _turnover(case)
+        s["gone"] = i32(gone)
+        s["room"] = i32([lens[i] for i in gone])
+    if own:   # the handle that a user's program keeps beside these tensors
+        import paper_2609_01925_b200 as crisp
+        s["cache"] = crisp.CrispCache(kc, vc, ks, vs, table, seq_lens, refs, fmt=case["fmt"],
+                                      n_q_heads=case.get("hq", case["hkv"]), max_tokens=max(1, cu[-1]))
+    return s
+
+
+def _split(meta, max_seqs, max_pages):
+    n = max_seqs * max_pages
+    return meta[:n].view(max_seqs, max_pages), meta[n:n + max_seqs], meta[n + max_seqs:]
+
+
+# ------------------------------------------------------------------------------------------------ one pass
+def run(s):
+    op = s["case"]["op"]
+    if op in ("compact", "turnover"):
+        s["meta"].copy_(s["first"])   # the tables as they were before the pass; what was moved is still in its old place
+    return (_own if own else _plain)[op](s)
+
+
+def _pool_state(s):
+    # the codes as the numbers they are, in units of their block's scale
+    t = torch.float8_e4m3fn if s["case"]["fmt"] == "e4m3" else torch.int8
+    return [s["k_codes"].view(t), s["v_codes"].view(t), s["k_scale"], s["v_scale"]]
+
+
+def _tables(s):
+    return [s["page_table"], s["seq_lens"], s["page_refs"]]
+
+
+def _own_attention(s):
+    lse = torch.empty(s["q"].shape[1], s["q"].shape[0], dtype=torch.float32, device=s["q"].device)
+    o = s["cache"].attention(s["q"], s["seq_ids"], cu_tokens=s["cu_tokens"], max_new=s["max_new"], lse=lse)
+    return [o, lse]
+
+
+def _own_append(s):
+    s["cache"].append(s["k"], s["v"], s["seq_ids"], cu_tokens=s["cu_tokens"])
+    return _pool_state(s)
+
+
+def _own_fork(s):
+    s["cache"].free(s["dst"])
+    s["cache"].fork(s["src"], s["dst"])
+    return _pool_state(s) + _tables(s)
+
+
+def _own_compact(s):
+    n = s["cache"].compact()
+    return _pool_state(s) + _tables(s) + [n]
+
+
+def _own_turnover(s):
+    s["cache"].free(s["gone"])
+    s["cache"].reserve(s["gone"], s["room"])
+    return _tables(s)
+
+
+def _places(s):
+    """For every new token: its item, position, page and place in the page."""
+    cu, ids = s["cu"].long(), s["seq_ids"].long()
+    t = torch.arange(s["q"].shape[0] if "q" in s else s["k"].shape[0], device=cu.device)
+    item = torch.searchsorted(cu, t, right=True) - 1
+    pos = s["seq_lens"].long()[ids[item]] - (cu[item + 1] - t)
+    page = s["page_table"].long()[ids[item], pos // PAGE]
+    return item, pos, page, pos % PAGE
+
+
+def _plain_attention(s):
+    fmt, ids = s["case"]["fmt"], s["seq_ids"].long()
+    q = s["q"].float()
+    n, hq, _ = q.shape
+    h = s["case"]["hkv"]
+    b, g, m = ids.numel(), hq // h, s["max_new"]
+    lens = s["seq_lens"].long()[ids]
+    pages = s["page_table"].long()[ids, :_pages(s["max_len"])].clamp(min=0)        # [b, p]
+    keys = pages.shape[1] * PAGE
+    j = torch.arange(keys, device=q.device)
+    item, pos, _, _ = _places(s)
+    new = s["cu"].long().diff()
+    row = torch.arange(n, device=q.device) - s["cu"].long()[item]                  # place among the item's new tokens
+    qp = torch.zeros(b, m, hq, DIM, device=q.device)
+    qp[item, row] = q
+    seen = lens[:, None] - new[:, None] + torch.arange(m, device=q.device)         # last key that row may see
+    hidden = j[None, None, :] > seen[:, :, None]                                   # [b, m, keys]
+    hidden |= (j[None, :] >= lens[:, None])[:, None, :]
+
+    def states(codes, scale):
+        x = _values(codes[0][pages], fmt) * scale[0][pages][..., None, None]       # [b, p, h, 128, 128]
+        x = x.transpose(1, 2).reshape(b, h, keys, DIM)
+        return torch.where((j[None, :] < lens[:, None])[:, None, :, None], x, torch.zeros((), device=q.device))
+
+    k = states(s["k_codes"], s["k_scale"])
+    qp = qp.view(b, m, h, g, DIM).permute(0, 2, 1, 3, 4).reshape(b, h, m * g, DIM)
+    x = (qp @ k.transpose(-1, -2)).view(b, h, m, g, keys)
+    del k
+    x *= 1.0 / math.sqrt(DIM)
+    x.masked_fill_(hidden[:, None, :, None, :], -math.inf)
+    top = x.amax(-1, keepdim=True)
+    top = torch.where(top == -math.inf, torch.zeros_like(top), top)
+    x.sub_(top).exp_()
+    total = x.sum(-1, keepdim=True)
+    o = x.view(b, h, m * g, keys) @ states(s["v_codes"], s["v_scale"])
+    o = o.view(b, h, m, g, DIM) / torch.where(total > 0, total, torch.ones_like(total))
+    lse = top + total.log()
+    o = o.permute(0, 2, 1, 3, 4).reshape(b, m, hq, DIM)[item, row]
+    lse = lse[..., 0].permute(0, 2, 1, 3).reshape(b, m, hq)[item, row]
+    return [o.bfloat16(), lse.t().contiguous()]
+
+
+def _plain_append(s):
+    fmt = s["case"]["fmt"]
+    item, pos, page, place = _places(s)
+    first = s["cu"].long()[:-1]                     # the first new token of each item, where it has one
+    first = first[s["cu"].long().diff() > 0]
+    begun = page[first]                             # pages that may hold earlier tokens, and how many
+    held = place[first]
+    touched = torch.zeros(s["page_refs"].numel(), dtype=torch.bool, device=page.device)
+    touched[page] = True
+    keeps = torch.zeros_like(touched)
+    keeps[begun] = held > 0
+    for_rows = torch.arange(PAGE, device=page.device)[None, None, :, None] < held[:, None, None, None]
+
+    def write(x, codes, scale):
+        x = x.float()
+        finite = torch.where(torch.isfinite(x), x.abs(), torch.zeros((), device=x.device)).amax(-1)   # [n, h]
+        amax = torch.zeros_like(scale[0]).index_reduce_(0, page, finite, "amax")
+        e = _exponent(amax, fmt)
+        old = torch.frexp(scale[0])[1] - 1
+        e = torch.where(keeps[:, None], torch.maximum(e, old), e)
+        shrunk = _pow2((old - e).clamp(-126, 0))[begun][..., None, None]
+        before = codes[0][begun]
+        again = _codes(_values(before, fmt) * shrunk, fmt)
+        codes[0][begun] = torch.where(for_rows, again, before)
+        codes[0].index_put_((page[:, None], torch.arange(x.shape[1], device=x.device)[None], place[:, None]),
+                            _codes(x * _pow2(-e)[page][..., None], fmt))
+        scale[0] = torch.where(touched[:, None], _pow2(e), scale[0])
+
+    write(s["k"], s["k_codes"], s["k_scale"])
+    write(s["v"], s["v_codes"], s["v_scale"])
+    return _pool_state(s)
+
+
+def _plain_free(s, ids):
+    ids = ids.long()
+    held = torch.arange(s["page_table"].shape[1], device=ids.device)[None] < _pages_of(s["seq_lens"][ids])[:, None]
+    rows = s["page_table"][ids]
+    s["page_refs"].index_add_(0, rows[held].long(), torch.full_like(rows[held], -1))
+    s["page_table"][ids] = torch.where(held, torch.full_like(rows, -1), rows)
+    s["seq_lens"][ids] = 0
+
+
+def _pages_of(lens):
+    return (lens.long() + PAGE - 1) // PAGE
+
+
+def _plain_fork(s):
+    _plain_free(s, s["dst"])
+    src, dst = s["src"].long(), s["dst"].long()
+    lens = s["seq_lens"][src]
+    rows = s["page_table"][src]
+    col = torch.arange(rows.shape[1], device=rows.device)[None]
+    full, part = (lens.long() // PAGE)[:, None], (lens.long() % PAGE)[:, None]
+    shared = col < full
+    tail = (col == full) & (part > 0)
+    fresh = torch.nonzero(s["page_refs"] == 0)[:, 0]
+    taken = fresh[:lens.numel()][torch.cumsum((part[:, 0] > 0).long(), 0) - 1]      # lowest free pages, in order
+    s["page_refs"].index_add_(0, rows[shared].long(), torch.ones_like(rows[shared]))
+    part_of = part[:, 0] > 0
+    s["page_refs"][taken[part_of]] = 1
+    old = s["page_table"][dst]
+    s["page_table"][dst] = torch.where(shared, rows, torch.where(tail, taken[:, None].int(), old))
+    s["seq_lens"][dst] = lens
+    a, b = rows[tail].long(), taken[part_of]
+    copied = torch.arange(PAGE, device=rows.device)[None, None, None, :, None] < part[part_of][None, :, :, None, None]
+    for_k, for_v = (torch.where(copied, c[:, a], c[:, b]) for c in (s["k_codes"], s["v_codes"]))
+    s["k_codes"][:, b], s["v_codes"][:, b] = for_k, for_v
+    s["k_scale"][:, b], s["v_scale"][:, b] = s["k_scale"][:, a], s["v_scale"][:, a]
+    return _pool_state(s) + _tables(s)
+
+
+def _plain_compact(s):
+    refs = s["page_refs"]
+    used = refs > 0
+    n = used.sum()
+    at = torch.arange(refs.numel(), device=refs.device)
+    a, b = torch.nonzero(used & (at >= n))[:, 0], torch.nonzero(~used & (at < n))[:, 0]
+    now = at.clone()
+    now[a] = b
+    for name in ("k_codes", "v_codes", "k_scale", "v_scale"):
+        s[name][:, b] = s[name][:, a]
+    refs[b] = refs[a]
+    refs[a] = 0
+    table = s["page_table"]
+    held = torch.arange(table.shape[1], device=table.device)[None] < _pages_of(s["seq_lens"])[:, None]
+    table.copy_(torch.where(held, now[table.clamp(min=0).long()].int(), table))
+    return _pool_state(s) + _tables(s) + [n.int().view(1)]
+
+
+def _plain_turnover(s):
+    _plain_free(s, s["gone"])
+    ids, room = s["gone"].long(), s["room"]
+    need = _pages_of(room)
+    fresh = torch.nonzero(s["page_refs"] == 0)[:, 0]
+    start = torch.cumsum(need, 0) - need
+    col = torch.arange(s["page_table"].shape[1], device=ids.device)[None]
+    takes = col < need[:, None]
+    taken = fresh[(start[:, None] + col).clamp(max=fresh.numel() - 1)]
+    s["page_table"][ids] = torch.where(takes, taken.int(), s["page_table"][ids])
+    s["page_refs"][taken[takes]] = 1
+    s["seq_lens"][ids] = room
+    return _tables(s)
+
+
+_plain = dict(attention=_plain_attention, append=_plain_append, fork=_plain_fork, compact=_plain_compact,
+              turnover=_plain_turnover)
+_own = dict(attention=_own_attention, append=_own_append, fork=_own_fork, compact=_own_compact,
+            turnover=_own_turnover)
+
+
+# ------------------------------------------------------------------------------------------------ in 64 bits
+def _exact_values():
+    """The value of each e4m3 byte, from the definition of the format."""
+    out = []
+    for c in range(256):
+        e, m = (c >> 3) & 15, c & 7
+        v = (1 + m / 8) * 2.0 ** (e - 7) if e else m / 8 * 2.0 ** -6
+        out.append((math.nan if c & 127 == 127 else v) * (-1 if c & 128 else 1))
+    return torch.tensor(out, dtype=torch.float64)
+
+
+def _exact_attention(case, s):
+    lens = s["seq_lens"].tolist()
+    cu = s["cu"].tolist()
+    hq, h = case["hq"], case["hkv"]
+    g = hq // h
+    if case["fmt"] == "e4m3":
+        of = _exact_values().to("cuda")
+    else:
+        of = torch.cat([torch.arange(128), torch.arange(-128, 0)]).double().to("cuda")
+    n = s["q"].shape[0]
+    o = torch.zeros(n, hq, DIM, dtype=torch.float64, device="cuda")
+    lse = torch.full((hq, n), -math.inf, dtype=torch.float64, device="cuda")
+    for item, seq in enumerate(s["seq_ids"].tolist()):
+        total, a, b = lens[seq], cu[item], cu[item + 1]
+        where = s["page_table"][seq, :_pages(total)].long()
+        for head in range(h):
+            k = (of[s["k_codes"][0, where, head].long()] * s["k_scale"][0, where, head, None, None].double())
+            v = (of[s["v_codes"][0, where, head].long()] * s["v_scale"][0, where, head, None, None].double())
+            k, v = (x.reshape(-1, DIM)[:total] for x in (k, v))
+            for at in range(a, b, 512):
+                end = min(b, at + 512)
+                q = s["q"][at:end, head * g:(head + 1) * g].double()
+                x = torch.einsum("tgd,jd->tgj", q, k) / math.sqrt(DIM)
+                last = total - b + torch.arange(at, end, device="cuda")
+                x[(torch.arange(total, device="cuda")[None] > last[:, None])[:, None].expand_as(x)] = -math.inf
+                l = torch.logsumexp(x, -1)
+                o[at:end, head * g:(head + 1) * g] = torch.einsum("tgj,jd->tgd", torch.exp(x - l[..., None]), v)
+                lse[head * g:(head + 1) * g, at:end] = l.t()
+    return [o, lse]
+
+
+def _nearest(x, fmt):
+    """Bytes of the nearest codes of float64 values in units of the scale, ties to the even code."""
+    if fmt == "int8":
+        return torch.round(x.clamp(-127, 127)).to(torch.int8).view(torch.uint8)
+    grid = _exact_values()[:127].to(x.device)
+    a = x.abs().clamp(max=448.0)
+    hi = torch.searchsorted(grid, a).clamp(max=126)
+    lo = (hi - 1).clamp(min=0)
+    up, down = grid[hi] - a, a - grid[lo]
+    pick = torch.where((down < up) | ((down == up) & (lo % 2 == 0)), lo, hi)
+    return (pick + 128 * torch.signbit(x)).to(torch.uint8)
+
+
+def _exact_append(case, s):
+    fmt = case["fmt"]
+    top = int(LARGEST[fmt])
+    of = _exact_values() if fmt == "e4m3" else torch.cat([torch.arange(128), torch.arange(-128, 0)]).double()
+    of = of.to("cuda")
+    lens, cu = s["seq_lens"].tolist(), s["cu"].tolist()
+    table = s["page_table"].tolist()
+    for item, seq in enumerate(s["seq_ids"].tolist()):
+        t, pos = cu[item], lens[seq] - (cu[item + 1] - cu[item])
+        while pos < lens[seq]:
+            page, held = table[seq][pos // PAGE], pos % PAGE
+            n = min(PAGE - held, lens[seq] - pos)
+            for x, codes, scale in ((s["k"], s["k_codes"], s["k_scale"]), (s["v"], s["v_codes"], s["v_scale"])):
+                y = x[t:t + n].double().transpose(0, 1)                            # [h, n, 128]
+                amax = y.abs().amax((1, 2))
+                e = torch.ceil(torch.log2(torch.clamp(amax, min=1e-300) / top))
+                e = torch.where(amax > top * torch.exp2(e), e + 1, e)
+                e = torch.where(amax <= top * torch.exp2(e - 1), e - 1, e).clamp(min=LOWEST)
+                if held:
+                    old = torch.log2(scale[0, page].double()).round()
+                    e = torch.maximum(e, old)
+                    now = of[codes[0, page, :, :held].long()] * torch.exp2(old - e)[:, None, None]
+                    codes[0, page, :, :held] = _nearest(now, fmt)
+                codes[0, page, :, held:held + n] = _nearest(y / torch.exp2(e)[:, None, None], fmt)
+                scale[0, page] = torch.exp2(e).float()
+            t, pos = t + n, pos + n
+    return _pool_state(s)
+
+
+def exact(case, seed):
+    if case["op"] not in ("attention", "append"):
+        return None   # only bytes are moved and whole numbers counted: there is nothing to round
+    s = prepare(case, seed)
+    if case["op"] == "append":
+        return _exact_append(case, s)
+    return _exact_attention(case, s)
