@@ -267,8 +267,7 @@ def prepare(case, seed):
         s["room"] = i32([lens[i] for i in gone])
     if own:   # the handle that a user's program keeps beside these tensors
         import paper_2609_01925_b200 as crisp
-        s["cache"] = crisp.CrispCache(kc, vc, ks, vs, table, seq_lens, refs, fmt=case["fmt"],
-                                      n_q_heads=case.get("hq", case["hkv"]), max_tokens=max(1, cu[-1]))
+        s["cache"] = crisp.CrispCache(kc, vc, ks, vs, table, seq_lens, refs, fmt=case["fmt"])
     return s
 
 
