@@ -9,6 +9,8 @@
  *                        (Algorithm 4), and the expansion into per-query-block key-block lists
  *   crisp_sparse_prefill exact softmax attention over the listed blocks, causal (Eq. 1)
  *   crisp_dense_prefill  the same kernel over every causal block (the dense baseline)
+ * and, for what follows the prompt, a paged K/V cache held in 8 bits (crisp_cache_...; not part of the paper):
+ * its pages, the quantising write of new K/V and causal attention over it.
  *
  * Conventions shared by every entry point
  *   - Tensors are contiguous, row major, bf16: Q and O are [seq_len, n_q_heads, 128]; K and V are
@@ -43,7 +45,9 @@ typedef enum crisp_status {
   CRISP_ERR_CAPACITY = -4,       /* col_idx capacity too small for the selected blocks               */
   CRISP_ERR_CUDA = -5,           /* a CUDA runtime / driver call failed (see crisp_last_cuda_error)  */
   CRISP_ERR_DEVICE_TIMEOUT = -6, /* a bounded device-side wait gave up                               */
-  CRISP_ERR_BAD_LIST = -7        /* row_ptr / col_idx given to crisp_sparse_prefill break the list rules */
+  CRISP_ERR_BAD_LIST = -7,       /* row_ptr / col_idx given to crisp_sparse_prefill break the list rules */
+  CRISP_ERR_NO_PAGES = -8,       /* not enough free pages in the cache, or no room in a sequence's row   */
+  CRISP_ERR_BAD_CACHE = -9       /* the cache's tables or the lists of sequences break their rules       */
 } crisp_status;
 
 /* Pattern labels written by crisp_route (Algorithm 2). */
@@ -265,6 +269,111 @@ int crisp_forward_host(const crisp_params* p, const void* q_host, const void* k_
                        int32_t* pattern_host, int64_t* nnz_host, void* cuda_stream);
 
 /*
+ * A paged K/V cache in 8 bits (the paper stops at the prompt; the layout and the calls are this library's).
+ * A page holds one block of 128 tokens of one sequence, for every layer and KV head: 128 x 128 one-byte codes for K
+ * and for V, and one scale for each of them.  An element is code * scale.  Scales are powers of two, 2^e with
+ * -126 <= e <= 127: the smallest that brings the block's largest finite magnitude within the format's largest code
+ * (448 for e4m3, 127 for int8), so that converting, and rescaling when a later token raises e, multiply exactly and
+ * round once, to the nearest code, ties to even.  Infinities become the largest code; NaN stays NaN in e4m3 and
+ * becomes 0 in int8.
+ * page_table, seq_lens and page_refs describe the sequences for all layers: sequence s holds seq_lens[s] tokens in
+ * the pages page_table[s][0 .. ceil(seq_lens[s] / 128) - 1], and page_refs[p] counts the sequences that hold page p
+ * (0 = free).  The caller owns all arrays; an empty cache is page_refs = 0 and seq_lens = 0 (codes, scales and
+ * page_table may hold anything).  The calls below change them on the stream.  A page that several sequences hold is
+ * never written: such pages are full, and a branch gets its own copy of a page that is not.
+ *
+ * Lists of sequences (DEVICE int32): seq_ids[i] is the sequence of item i; a negative entry is padding and is
+ * skipped; NULL means item i is sequence i.  At most CRISP_CACHE_MAX_BATCH items.  Nothing on the device is trusted:
+ * what breaks a rule is not read or written, and sets the status word of the workspace to CRISP_ERR_BAD_CACHE or
+ * CRISP_ERR_NO_PAGES.  Unlike the calls above, cache calls do not clear that word: the first error stays until
+ * crisp_poll_device_status, so a run of calls needs one poll.  The caller therefore zeroes a workspace once before
+ * its first use (all of crisp_cache_attention's - it counts in it, and the counts are zero again after the call - and
+ * the first 256 bytes of the other), and again after CRISP_ERR_DEVICE_TIMEOUT.  Calls that use one workspace must not
+ * overlap in time, and neither must calls that change one cache.
+ */
+#define CRISP_CACHE_E4M3 0
+#define CRISP_CACHE_INT8 1
+#define CRISP_CACHE_MAX_BATCH 1024
+typedef struct crisp_cache {
+  int32_t struct_size;   /* = sizeof(crisp_cache); ABI guard                                                 */
+  int32_t format;        /* CRISP_CACHE_E4M3 or CRISP_CACHE_INT8                                             */
+  int32_t n_layers;
+  int32_t n_kv_heads;
+  int32_t n_pages;       /* n_layers * n_pages * n_kv_heads <= 2^24 - 1                                      */
+  int32_t max_seqs;
+  int32_t max_pages;     /* pages of the longest sequence (columns of page_table), <= 2^24 - 1               */
+  int32_t head_dim;      /* 128 only                                                                         */
+  void* k_codes;         /* [n_layers][n_pages][n_kv_heads][128 tokens][128], 16-byte aligned                */
+  void* v_codes;
+  float* k_scale;        /* [n_layers][n_pages][n_kv_heads]                                                  */
+  float* v_scale;
+  int32_t* page_table;   /* [max_seqs][max_pages]                                                            */
+  int32_t* seq_lens;     /* [max_seqs]                                                                       */
+  int32_t* page_refs;    /* [n_pages]                                                                        */
+} crisp_cache;
+
+/* Workspace sizes: pages_ws for reserve, append, fork, free and compact, attention_ws for crisp_cache_attention. */
+int crisp_cache_workspace_bytes(const crisp_cache* c, size_t* pages_ws, size_t* attention_ws);
+
+/*
+ * Makes room for n_new[i] (NULL: 1) more tokens of every listed sequence and adds them to its length: new pages are
+ * the lowest free ones, in the order of the list.  All or nothing: with too few free pages, a row of page_table that
+ * is too short (CRISP_ERR_NO_PAGES), or a sequence listed twice (CRISP_ERR_BAD_CACHE), nothing changes.  The new
+ * tokens' contents are undefined until crisp_cache_append has written them, for each layer.
+ */
+int crisp_cache_reserve(const crisp_cache* c, const int32_t* seq_ids, const int32_t* n_new, int32_t batch, void* ws,
+                        size_t ws_bytes, void* cuda_stream);
+
+/*
+ * Writes new tokens into the cache.  k, v [n_tokens][n_kv_heads][128] bf16 hold the items' tokens one after the
+ * other: item i owns tokens cu_tokens[i] .. cu_tokens[i+1] - 1 (DEVICE, batch + 1 int32, non-decreasing, from 0 to at
+ * most n_tokens; NULL: n_tokens / batch each, which must divide), and they are the last positions that the
+ * sequence's length covers (crisp_cache_reserve has counted them in).  Earlier tokens of a page whose scale grows
+ * are rescaled.  A sequence may be listed only once (CRISP_ERR_BAD_CACHE; its new tokens are then undefined), and the
+ * pages written must be held by it alone.
+ */
+int crisp_cache_append(const crisp_cache* c, int32_t layer, const int32_t* seq_ids, const int32_t* cu_tokens,
+                       int32_t batch, int32_t n_tokens, const void* k, const void* v, void* ws, size_t ws_bytes,
+                       void* cuda_stream);
+
+/*
+ * Causal attention of the items' newest tokens over everything their sequences hold (the cached form of Eq. 1).
+ * q, o [n_tokens][n_q_heads][128] bf16, packed as in crisp_cache_append; query t of an item with n new tokens of a
+ * sequence of length L stands at position L - n + t and sees the keys j <= L - n + t:
+ *   o = sum_j softmax_j(q . k_j * scale) v_j,  scale = softmax_scale or 1 / sqrt(128) when that is 0.
+ * A query that sees nothing (n > L) gets o = 0 and lse = -inf.  lse: optional, [n_q_heads][n_tokens] f32, natural log.
+ * max_new bounds every item's number of tokens (HOST; an item above it is refused on the device); it picks the
+ * kernel: one or a few tokens read the cache once at HBM speed, longer pieces run on the tensor cores.  Tokens of
+ * skipped or refused items and tokens behind the last item are left as they are.  A sequence may be listed more than
+ * once.  n_q_heads / n_kv_heads <= 16.  A NaN among a sequence's cached V may reach every row of its items.
+ * Row results depend on the batch only through the order of fp32 sums; the same call gives the same bits.
+ */
+int crisp_cache_attention(const crisp_cache* c, int32_t layer, const int32_t* seq_ids, const int32_t* cu_tokens,
+                          int32_t batch, int32_t n_tokens, int32_t max_new, int32_t n_q_heads, float softmax_scale,
+                          const void* q, void* o, float* lse, void* ws, size_t ws_bytes, void* cuda_stream);
+
+/*
+ * Branches: sequence dst[i], which must be empty, becomes the first n_tokens[i] (NULL: all) tokens of sequence
+ * src[i].  share != 0: full pages are shared (their reference count grows) and only a partial last page is copied;
+ * share == 0: every page is copied.  One src may be branched many times; every dst must be listed once.  Entries with
+ * a negative src or dst are skipped.  All or nothing, judged on the state before the call.  Copies cover all layers.
+ */
+int crisp_cache_fork(const crisp_cache* c, const int32_t* src, const int32_t* dst, const int32_t* n_tokens,
+                     int32_t count, int32_t share, void* ws, size_t ws_bytes, void* cuda_stream);
+
+/* Empties the listed sequences: their pages lose a reference (free at zero), their rows of page_table become -1.
+ * Freeing an empty sequence, or one twice, does nothing.  seq_ids must not be NULL. */
+int crisp_cache_free(const crisp_cache* c, const int32_t* seq_ids, int32_t count, void* ws, size_t ws_bytes,
+                     void* cuda_stream);
+
+/*
+ * Moves the pages in use to the front of the pool: with U pages in use, those at or above U move, in ascending
+ * order, to the free pages below U, with contents (all layers), reference counts and every row of page_table.
+ * *n_used (DEVICE int32) receives U: pages U .. n_pages - 1 are then free.
+ */
+int crisp_cache_compact(const crisp_cache* c, int32_t* n_used, void* ws, size_t ws_bytes, void* cuda_stream);
+
+/*
  * Diagnostic (the paper has no counterpart): per-kernel device times of the stage calls, for benchmarks.
  * crisp_profile_enable(1) discards earlier records and switches recording on: from then on every kernel the
  * library launches is bracketed by two CUDA events on the caller's stream (the events are created on first use
@@ -291,8 +400,8 @@ int crisp_selftest_bounded_wait(void* ws, size_t ws_bytes, int64_t limit_ns, voi
 
 /*
  * Synchronises `cuda_stream`, reads the status word at the start of `ws`, clears it and returns it
- * (CRISP_OK, CRISP_ERR_CAPACITY, CRISP_ERR_DEVICE_TIMEOUT or CRISP_ERR_BAD_LIST), or CRISP_ERR_CUDA if the
- * stream failed.
+ * (CRISP_OK, CRISP_ERR_CAPACITY, CRISP_ERR_DEVICE_TIMEOUT, CRISP_ERR_BAD_LIST, CRISP_ERR_NO_PAGES or
+ * CRISP_ERR_BAD_CACHE), or CRISP_ERR_CUDA if the stream failed.
  */
 int crisp_poll_device_status(void* ws, void* cuda_stream);
 

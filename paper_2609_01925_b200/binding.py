@@ -23,14 +23,19 @@ ERR_CAPACITY = -4
 ERR_CUDA = -5
 ERR_DEVICE_TIMEOUT = -6
 ERR_BAD_LIST = -7
+ERR_NO_PAGES = -8
+ERR_BAD_CACHE = -9
 PATTERN_PE, PATTERN_VS = 0, 1
+CACHE_E4M3, CACHE_INT8 = 0, 1
+CACHE_MAX_BATCH = 1024
 
 EXPORTS = (
     "crisp_version", "crisp_status_string", "crisp_last_cuda_error", "crisp_workspace_bytes",
     "crisp_route", "crisp_route_static", "crisp_select", "crisp_sparse_prefill", "crisp_dense_prefill",
     "crisp_poll_device_status", "crisp_forward", "crisp_route_jsd", "crisp_varlen_layout",
     "crisp_forward_varlen", "crisp_selftest_bounded_wait", "crisp_profile_enable", "crisp_profile_read",
-    "crisp_forward_host", "crisp_forward_host_stage_bytes",
+    "crisp_forward_host", "crisp_forward_host_stage_bytes", "crisp_cache_workspace_bytes", "crisp_cache_reserve",
+    "crisp_cache_append", "crisp_cache_attention", "crisp_cache_fork", "crisp_cache_free", "crisp_cache_compact",
 )
 
 
@@ -43,6 +48,17 @@ class CrispParams(ctypes.Structure):
         ("k_min_blocks", ctypes.c_int32), ("selector", ctypes.c_int32),
         ("force_pattern", ctypes.c_int32), ("tau", ctypes.c_float), ("alpha", ctypes.c_float),
         ("gamma", ctypes.c_float), ("softmax_scale", ctypes.c_float),
+    ]
+
+
+class CrispCacheDesc(ctypes.Structure):
+    """Mirror of `crisp_cache` (include/crisp.h)."""
+    _fields_ = [
+        ("struct_size", ctypes.c_int32), ("format", ctypes.c_int32), ("n_layers", ctypes.c_int32),
+        ("n_kv_heads", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("max_seqs", ctypes.c_int32),
+        ("max_pages", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("k_codes", ctypes.c_void_p),
+        ("v_codes", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+        ("page_table", ctypes.c_void_p), ("seq_lens", ctypes.c_void_p), ("page_refs", ctypes.c_void_p),
     ]
 
 
@@ -117,6 +133,21 @@ def load() -> ctypes.CDLL:
                                        ctypes.POINTER(ctypes.c_int32)]
     lib.crisp_selftest_bounded_wait.restype = ctypes.c_int
     lib.crisp_selftest_bounded_wait.argtypes = [vp, sz, i64, vp]
+    C, i32 = ctypes.POINTER(CrispCacheDesc), ctypes.c_int32
+    lib.crisp_cache_workspace_bytes.restype = ctypes.c_int
+    lib.crisp_cache_workspace_bytes.argtypes = [C, ctypes.POINTER(sz), ctypes.POINTER(sz)]
+    lib.crisp_cache_reserve.restype = ctypes.c_int
+    lib.crisp_cache_reserve.argtypes = [C, vp, vp, i32, vp, sz, vp]
+    lib.crisp_cache_append.restype = ctypes.c_int
+    lib.crisp_cache_append.argtypes = [C, i32, vp, vp, i32, i32, vp, vp, vp, sz, vp]
+    lib.crisp_cache_attention.restype = ctypes.c_int
+    lib.crisp_cache_attention.argtypes = [C, i32, vp, vp, i32, i32, i32, i32, ctypes.c_float, vp, vp, vp, vp, sz, vp]
+    lib.crisp_cache_fork.restype = ctypes.c_int
+    lib.crisp_cache_fork.argtypes = [C, vp, vp, vp, i32, i32, vp, sz, vp]
+    lib.crisp_cache_free.restype = ctypes.c_int
+    lib.crisp_cache_free.argtypes = [C, vp, i32, vp, sz, vp]
+    lib.crisp_cache_compact.restype = ctypes.c_int
+    lib.crisp_cache_compact.argtypes = [C, vp, vp, sz, vp]
     lib.crisp_poll_device_status.restype = ctypes.c_int
     lib.crisp_poll_device_status.argtypes = [vp, vp]
     _lib = lib
@@ -272,6 +303,43 @@ def crisp_profile_read(max_records: int = 4096):
 
 def crisp_selftest_bounded_wait(ws, limit_ns, stream=None) -> int:
     return load().crisp_selftest_bounded_wait(_ptr(ws), _nbytes(ws), int(limit_ns), _stream(stream))
+
+
+def crisp_cache_workspace_bytes(c: CrispCacheDesc) -> Tuple[int, int]:
+    a, b = ctypes.c_size_t(), ctypes.c_size_t()
+    rc = load().crisp_cache_workspace_bytes(ctypes.byref(c), ctypes.byref(a), ctypes.byref(b))
+    if rc != OK:
+        raise CrispError(rc, "crisp_cache_workspace_bytes")
+    return a.value, b.value
+
+
+def crisp_cache_reserve(c, seq_ids, n_new, batch, ws, stream=None) -> int:
+    return load().crisp_cache_reserve(c, _ptr(seq_ids), _ptr(n_new), batch, _ptr(ws), _nbytes(ws), _stream(stream))
+
+
+def crisp_cache_append(c, layer, seq_ids, cu_tokens, batch, n_tokens, k, v, ws, stream=None) -> int:
+    return load().crisp_cache_append(c, layer, _ptr(seq_ids), _ptr(cu_tokens), batch, n_tokens, _ptr(k), _ptr(v),
+                                     _ptr(ws), _nbytes(ws), _stream(stream))
+
+
+def crisp_cache_attention(c, layer, seq_ids, cu_tokens, batch, n_tokens, max_new, n_q_heads, softmax_scale, q, o, lse,
+                          ws, stream=None) -> int:
+    return load().crisp_cache_attention(c, layer, _ptr(seq_ids), _ptr(cu_tokens), batch, n_tokens, max_new, n_q_heads,
+                                        softmax_scale, _ptr(q), _ptr(o), _ptr(lse), _ptr(ws), _nbytes(ws),
+                                        _stream(stream))
+
+
+def crisp_cache_fork(c, src, dst, n_tokens, count, share, ws, stream=None) -> int:
+    return load().crisp_cache_fork(c, _ptr(src), _ptr(dst), _ptr(n_tokens), count, 1 if share else 0, _ptr(ws),
+                                   _nbytes(ws), _stream(stream))
+
+
+def crisp_cache_free(c, seq_ids, count, ws, stream=None) -> int:
+    return load().crisp_cache_free(c, _ptr(seq_ids), count, _ptr(ws), _nbytes(ws), _stream(stream))
+
+
+def crisp_cache_compact(c, n_used, ws, stream=None) -> int:
+    return load().crisp_cache_compact(c, _ptr(n_used), _ptr(ws), _nbytes(ws), _stream(stream))
 
 
 def crisp_poll_device_status(ws, stream=None) -> int:

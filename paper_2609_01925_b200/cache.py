@@ -1,0 +1,189 @@
+"""The K/V cache of the answering phase: 8-bit pages, their bookkeeping and attention over them.
+
+CrispCache holds the tensors of one cache (include/crisp.h, `crisp_cache`) and its two workspaces and passes pointers
+to libcrisp.so.  Nothing is computed in Python and nothing waits for the device, except poll().
+"""
+from __future__ import annotations
+
+import ctypes
+from typing import Optional
+
+import torch
+
+from . import binding as B
+
+PAGE = 128
+_FORMATS = {"e4m3": B.CACHE_E4M3, "int8": B.CACHE_INT8}
+
+
+class CrispCache:
+    """A paged 8-bit K/V cache over tensors that the caller (or `allocate`) provides.
+
+    k_codes, v_codes  uint8 [layers, pages, kv_heads, 128, 128]: one byte per element, `fmt` "e4m3" or "int8"
+    k_scale, v_scale  float32 [layers, pages, kv_heads]: powers of two
+    page_table        int32 [max_seqs, max_pages];  seq_lens int32 [max_seqs];  page_refs int32 [pages]
+
+    Lists of sequences are int32 tensors on the cache's device (negative entries are padding).  All calls enqueue on
+    `stream` (default: the current stream of the cache's device) and may be captured into a CUDA graph; mistakes that
+    only the device can see (no free page, a sequence listed twice, ...) are raised by poll().
+    """
+
+    def __init__(self, k_codes, v_codes, k_scale, v_scale, page_table, seq_lens, page_refs, *, fmt: str = "e4m3"):
+        if fmt not in _FORMATS:
+            raise ValueError(f"fmt must be one of {sorted(_FORMATS)}, not {fmt!r}")
+        if k_codes.dim() != 5 or k_codes.shape[3:] != (PAGE, 128):
+            raise ValueError("k_codes must be [layers, pages, kv_heads, 128, 128]")
+        self.fmt, self.device = fmt, k_codes.device
+        if self.device.type != "cuda":
+            raise RuntimeError("CrispCache needs CUDA tensors (no CPU fallback)")
+        layers, pages, heads = k_codes.shape[:3]
+        max_seqs, max_pages = page_table.shape
+        for name, t, shape, dtype in (
+                ("k_codes", k_codes, k_codes.shape, torch.uint8), ("v_codes", v_codes, k_codes.shape, torch.uint8),
+                ("k_scale", k_scale, (layers, pages, heads), torch.float32),
+                ("v_scale", v_scale, (layers, pages, heads), torch.float32),
+                ("page_table", page_table, (max_seqs, max_pages), torch.int32),
+                ("seq_lens", seq_lens, (max_seqs,), torch.int32), ("page_refs", page_refs, (pages,), torch.int32)):
+            self._check(name, t, dtype)
+            if tuple(t.shape) != tuple(shape):
+                raise ValueError(f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}")
+        self.k_codes, self.v_codes, self.k_scale, self.v_scale = k_codes, v_codes, k_scale, v_scale
+        self.page_table, self.seq_lens, self.page_refs = page_table, seq_lens, page_refs
+        self.n_layers, self.n_pages, self.n_kv_heads = layers, pages, heads
+        self.desc = B.CrispCacheDesc(ctypes.sizeof(B.CrispCacheDesc), _FORMATS[fmt], layers, heads, pages, max_seqs,
+                                     max_pages, 128, *(t.data_ptr() for t in (
+                                         k_codes, v_codes, k_scale, v_scale, page_table, seq_lens, page_refs)))
+        pages_ws, attention_ws = B.crisp_cache_workspace_bytes(self.desc)
+        self.pages_ws = torch.zeros(pages_ws, dtype=torch.uint8, device=self.device)
+        self.attention_ws = torch.zeros(attention_ws, dtype=torch.uint8, device=self.device)
+        self._c = ctypes.byref(self.desc)
+
+    @classmethod
+    def allocate(cls, n_pages: int, n_kv_heads: int, max_seqs: int, max_pages: int, *, n_layers: int = 1,
+                 fmt: str = "e4m3", device="cuda") -> "CrispCache":
+        """An empty cache with tensors of its own."""
+        if not torch.cuda.is_available():
+            raise RuntimeError("CrispCache needs a CUDA device (no CPU fallback)")
+        shape = (n_layers, n_pages, n_kv_heads)
+        codes = [torch.empty(*shape, PAGE, 128, dtype=torch.uint8, device=device) for _ in range(2)]
+        scale = [torch.empty(shape, dtype=torch.float32, device=device) for _ in range(2)]
+        table = torch.full((max_seqs, max_pages), -1, dtype=torch.int32, device=device)
+        lens, refs = (torch.zeros(n, dtype=torch.int32, device=device) for n in (max_seqs, n_pages))
+        return cls(*codes, *scale, table, lens, refs, fmt=fmt)
+
+    # ---- argument checks (host side: types, shapes and places; the device checks the contents)
+    def _check(self, name, t, dtype):
+        if t.dtype != dtype or t.device != self.device or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous {dtype} tensor on {self.device}")
+
+    def _list(self, name, t, n=None):
+        if t is None:
+            return
+        self._check(name, t, torch.int32)
+        if t.dim() != 1 or (n is not None and t.shape[0] != n):
+            raise ValueError(f"{name} must be one-dimensional" + ("" if n is None else f" with {n} entries"))
+
+    def _tokens(self, name, t, heads):
+        self._check(name, t, torch.bfloat16)
+        if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != 128:
+            raise ValueError(f"{name} must be [tokens, {heads}, 128]")
+
+    def _call(self, fn, stream, *args):
+        """fn(desc, *args, stream) with the cache's device current."""
+        if stream is None:
+            stream = torch.cuda.current_stream(self.device)
+        if torch.cuda.current_device() == self.device.index:
+            rc = fn(self._c, *args, stream)
+        else:
+            with torch.cuda.device(self.device):
+                rc = fn(self._c, *args, stream)
+        if rc != B.OK:
+            raise B.CrispError(rc, fn.__name__)
+
+    # ---- pages
+    def reserve(self, seq_ids, n_new: Optional[torch.Tensor] = None, stream=None) -> None:
+        """Adds n_new[i] (None: one) tokens to sequence seq_ids[i] and gives it the pages for them."""
+        self._list("seq_ids", seq_ids)
+        self._list("n_new", n_new, seq_ids.shape[0])
+        self._call(B.crisp_cache_reserve, stream, seq_ids, n_new, seq_ids.shape[0], self.pages_ws)
+
+    def fork(self, src, dst, n_tokens: Optional[torch.Tensor] = None, share: bool = True, stream=None) -> None:
+        """Makes the empty sequence dst[i] the first n_tokens[i] (None: all) tokens of src[i]."""
+        self._list("src", src)
+        self._list("dst", dst, src.shape[0])
+        self._list("n_tokens", n_tokens, src.shape[0])
+        self._call(B.crisp_cache_fork, stream, src, dst, n_tokens, src.shape[0], share, self.pages_ws)
+
+    def free(self, seq_ids, stream=None) -> None:
+        """Empties the listed sequences."""
+        self._list("seq_ids", seq_ids)
+        self._call(B.crisp_cache_free, stream, seq_ids, seq_ids.shape[0], self.pages_ws)
+
+    def compact(self, n_used: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        """Moves the pages in use to the front of the pool; returns how many there are (int32 [1], on the device)."""
+        if n_used is None:
+            n_used = self._new((1,), torch.int32, stream)
+        self._list("n_used", n_used, 1)
+        self._call(B.crisp_cache_compact, stream, n_used, self.pages_ws)
+        return n_used
+
+    # ---- contents
+    def append(self, k, v, seq_ids, cu_tokens: Optional[torch.Tensor] = None, layer: int = 0, stream=None) -> None:
+        """Writes the last tokens of the listed sequences, packed in k and v [tokens, kv_heads, 128] bf16: item i owns
+        tokens cu_tokens[i] .. cu_tokens[i + 1] - 1 (None: the same number for every item)."""
+        self._tokens("k", k, self.n_kv_heads)
+        self._tokens("v", v, self.n_kv_heads)
+        if v.shape[0] != k.shape[0]:
+            raise ValueError("k and v must hold the same tokens")
+        self._list("seq_ids", seq_ids)
+        self._list("cu_tokens", cu_tokens, seq_ids.shape[0] + 1)
+        self._call(B.crisp_cache_append, stream, layer, seq_ids, cu_tokens, seq_ids.shape[0], k.shape[0], k, v,
+                   self.pages_ws)
+
+    def attention(self, q, seq_ids, cu_tokens: Optional[torch.Tensor] = None, max_new: Optional[int] = None,
+                  layer: int = 0, softmax_scale: float = 0.0, o: Optional[torch.Tensor] = None,
+                  lse: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        """Causal attention of the newest tokens, q [tokens, q_heads, 128] bf16 packed as in append, over everything
+        their sequences hold.  max_new: a bound on the items' numbers of tokens (None: what the shapes allow).
+        lse: optional float32 [q_heads, tokens].  Returns o like q."""
+        if q.dim() != 3:
+            raise ValueError("q must be [tokens, q_heads, 128]")
+        n, hq = q.shape[0], q.shape[1]
+        self._tokens("q", q, hq)
+        self._list("seq_ids", seq_ids)
+        batch = seq_ids.shape[0]
+        self._list("cu_tokens", cu_tokens, batch + 1)
+        if max_new is None:
+            max_new = n if cu_tokens is not None or batch == 0 else n // batch
+        if o is None:
+            o = self._new(q.shape, torch.bfloat16, stream)
+        else:
+            self._tokens("o", o, hq)
+            if o.shape[0] != n:
+                raise ValueError("o must have the shape of q")
+        if lse is not None:
+            self._check("lse", lse, torch.float32)
+            if tuple(lse.shape) != (hq, n):
+                raise ValueError(f"lse must be [{hq}, {n}]")
+        self._call(B.crisp_cache_attention, stream, layer, seq_ids, cu_tokens, batch, n, max_new, hq, softmax_scale, q,
+                   o, lse, self.attention_ws)
+        return o
+
+    def _new(self, shape, dtype, stream):
+        """An output, allocated on the stream that will write it."""
+        if stream is None or not isinstance(stream, torch.cuda.Stream):
+            return torch.empty(shape, dtype=dtype, device=self.device)
+        with torch.cuda.stream(stream):
+            return torch.empty(shape, dtype=dtype, device=self.device)
+
+    def poll(self, stream=None) -> None:
+        """Waits for the stream and raises the first error that the device has recorded since the last poll."""
+        if stream is None:
+            stream = torch.cuda.current_stream(self.device)
+        with torch.cuda.device(self.device):
+            status = [(name, B.crisp_poll_device_status(ws, stream))
+                      for ws, name in ((self.pages_ws, "pages"), (self.attention_ws, "attention"))]
+        if status[1][1] == B.ERR_DEVICE_TIMEOUT:
+            self.attention_ws.zero_()   # the call that gave up may have left its counters behind
+        for name, rc in status:
+            B.check(rc, f"cache status ({name})")

@@ -6,6 +6,7 @@
 #include <mutex>
 #include <vector>
 
+#include "cache.cuh"
 #include "common.cuh"
 
 namespace crisp {
@@ -102,6 +103,28 @@ int make_tmap_bf16_nhd(CUtensorMap* out, const void* base, int n, int heads, int
   return CRISP_OK;
 }
 
+int make_tmap_codes(CUtensorMap* out, const void* base, size_t rows) {
+  EncodeTiledFn enc = encode_fn();
+  if (!enc) {
+    set_cu_error("cuTensorMapEncodeTiled is not available (no CUDA driver?)");
+    return CRISP_ERR_CUDA;
+  }
+  const cuuint64_t dims[2] = {static_cast<cuuint64_t>(kHeadDim), static_cast<cuuint64_t>(rows)};
+  const cuuint64_t strides[1] = {static_cast<cuuint64_t>(kHeadDim)};
+  const cuuint32_t box[2] = {static_cast<cuuint32_t>(kHeadDim), static_cast<cuuint32_t>(kPage)};
+  const cuuint32_t estr[2] = {1, 1};
+  CUresult r = enc(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr,
+                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) {
+    char msg[96];
+    std::snprintf(msg, sizeof(msg), "cuTensorMapEncodeTiled failed with CUresult %d", static_cast<int>(r));
+    set_cu_error(msg);
+    return CRISP_ERR_CUDA;
+  }
+  return CRISP_OK;
+}
+
 // dense_only: the call runs dense attention alone, which is defined for every length >= 1 and reads none of
 // the routing parameters' relation to the length.
 int validate(const crisp_params* p, Dims* d, bool dense_only) {
@@ -151,6 +174,62 @@ int validate(const crisp_params* p, Dims* d, bool dense_only) {
 
 static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
+// ---- the 8-bit cache: host-side checks (what lives on the device is checked by the kernels)
+int check_cache(const crisp_cache* c, CacheView* v) {
+  if (!c || c->struct_size != static_cast<int32_t>(sizeof(crisp_cache))) return CRISP_ERR_INVALID_ARG;
+  if (c->n_layers <= 0 || c->n_kv_heads <= 0 || c->n_pages <= 0 || c->max_seqs <= 0 || c->max_pages <= 0)
+    return CRISP_ERR_INVALID_ARG;
+  if (c->format != CRISP_CACHE_E4M3 && c->format != CRISP_CACHE_INT8) return CRISP_ERR_INVALID_ARG;
+  if (c->head_dim != kHeadDim) return CRISP_ERR_UNSUPPORTED;
+  // token rows of the code arrays are TMA coordinates and token positions are int32: both stay below 2^31
+  constexpr int64_t kMost = (1 << 24) - 1;
+  if (c->max_pages > kMost || c->n_kv_heads > 65535) return CRISP_ERR_UNSUPPORTED;
+  if (static_cast<__int128>(c->n_layers) * c->n_pages * c->n_kv_heads > kMost) return CRISP_ERR_UNSUPPORTED;
+  if (!c->k_codes || !c->v_codes || !c->k_scale || !c->v_scale || !c->page_table || !c->seq_lens || !c->page_refs)
+    return CRISP_ERR_INVALID_ARG;
+  if (!aligned16(c->k_codes) || !aligned16(c->v_codes)) return CRISP_ERR_INVALID_ARG;
+  v->k_codes = static_cast<uint8_t*>(c->k_codes);
+  v->v_codes = static_cast<uint8_t*>(c->v_codes);
+  v->k_scale = c->k_scale;
+  v->v_scale = c->v_scale;
+  v->page_table = c->page_table;
+  v->seq_lens = c->seq_lens;
+  v->page_refs = c->page_refs;
+  v->format = c->format;
+  v->layers = c->n_layers;
+  v->heads = c->n_kv_heads;
+  v->pages = c->n_pages;
+  v->max_seqs = c->max_seqs;
+  v->max_pages = c->max_pages;
+  return CRISP_OK;
+}
+
+static int check_count(int32_t count) {
+  if (count < 0) return CRISP_ERR_INVALID_ARG;
+  return count > kMaxCacheBatch ? CRISP_ERR_UNSUPPORTED : CRISP_OK;
+}
+
+int check_batch(const int32_t* seq_ids, const int32_t* cu, int32_t batch, int32_t n_tokens,
+                int32_t max_new, CacheBatch* b) {
+  const int rc = check_count(batch);
+  if (rc != CRISP_OK) return rc;
+  if (n_tokens < 0 || max_new < 0) return CRISP_ERR_INVALID_ARG;
+  if (batch > 0 && !cu && n_tokens % batch != 0) return CRISP_ERR_INVALID_ARG;
+  b->seq_ids = seq_ids;
+  b->cu = cu;
+  b->batch = batch;
+  b->n_tokens = n_tokens;
+  b->per = batch > 0 && !cu ? n_tokens / batch : 0;
+  b->max_new = max_new < n_tokens ? max_new : n_tokens;
+  if (!cu && b->per > b->max_new) return CRISP_ERR_INVALID_ARG;
+  return CRISP_OK;
+}
+
+static int check_pages_ws(const CacheView& v, const void* ws, size_t ws_bytes) {
+  if (!ws) return CRISP_ERR_INVALID_ARG;
+  return !aligned16(ws) || ws_bytes < cache_pages_ws_bytes(v) ? CRISP_ERR_WORKSPACE : CRISP_OK;
+}
+
 }  // namespace crisp
 
 using namespace crisp;
@@ -169,6 +248,8 @@ const char* crisp_status_string(int status) {
     case CRISP_ERR_CUDA: return "CUDA error";
     case CRISP_ERR_DEVICE_TIMEOUT: return "device-side wait timed out";
     case CRISP_ERR_BAD_LIST: return "index lists break the list rules";
+    case CRISP_ERR_NO_PAGES: return "not enough free cache pages";
+    case CRISP_ERR_BAD_CACHE: return "cache tables or sequence lists break their rules";
     default: return "unknown status";
   }
 }
@@ -669,6 +750,91 @@ int crisp_forward_host(const crisp_params* p, const void* q_host, const void* k_
   }
   if (nnz_host) *nnz_host = nnz;
   return CRISP_OK;
+}
+
+int crisp_cache_workspace_bytes(const crisp_cache* c, size_t* pages_ws, size_t* attention_ws) {
+  CacheView v;
+  const int rc = check_cache(c, &v);
+  if (rc != CRISP_OK) return rc;
+  if (pages_ws) *pages_ws = cache_pages_ws_bytes(v);
+  if (attention_ws) *attention_ws = cache_attention_ws_bytes();
+  return CRISP_OK;
+}
+
+int crisp_cache_reserve(const crisp_cache* c, const int32_t* seq_ids, const int32_t* n_new, int32_t batch, void* ws,
+                        size_t ws_bytes, void* cuda_stream) {
+  CacheView v;
+  int rc = check_cache(c, &v);
+  if (rc == CRISP_OK) rc = check_count(batch);
+  if (rc == CRISP_OK) rc = check_pages_ws(v, ws, ws_bytes);
+  if (rc != CRISP_OK || batch == 0) return rc;
+  return launch_cache_reserve(v, seq_ids, n_new, batch, ws, static_cast<cudaStream_t>(cuda_stream));
+}
+
+int crisp_cache_append(const crisp_cache* c, int32_t layer, const int32_t* seq_ids, const int32_t* cu_tokens,
+                       int32_t batch, int32_t n_tokens, const void* k, const void* v_in, void* ws, size_t ws_bytes,
+                       void* cuda_stream) {
+  CacheView v;
+  CacheBatch b;
+  int rc = check_cache(c, &v);
+  if (rc == CRISP_OK) rc = check_batch(seq_ids, cu_tokens, batch, n_tokens, n_tokens, &b);
+  if (rc == CRISP_OK && (layer < 0 || layer >= v.layers)) rc = CRISP_ERR_INVALID_ARG;
+  if (rc != CRISP_OK || batch == 0 || n_tokens == 0) return rc;
+  if (!k || !v_in || !aligned16(k) || !aligned16(v_in)) return CRISP_ERR_INVALID_ARG;
+  rc = check_pages_ws(v, ws, ws_bytes);
+  if (rc != CRISP_OK) return rc;
+  return launch_cache_append(v, layer, b, k, v_in, ws, static_cast<cudaStream_t>(cuda_stream));
+}
+
+int crisp_cache_attention(const crisp_cache* c, int32_t layer, const int32_t* seq_ids, const int32_t* cu_tokens,
+                          int32_t batch, int32_t n_tokens, int32_t max_new, int32_t n_q_heads, float softmax_scale,
+                          const void* q, void* o, float* lse, void* ws, size_t ws_bytes, void* cuda_stream) {
+  CacheView v;
+  CacheBatch b;
+  int rc = check_cache(c, &v);
+  if (rc == CRISP_OK) rc = check_batch(seq_ids, cu_tokens, batch, n_tokens, max_new, &b);
+  if (rc != CRISP_OK) return rc;
+  if (layer < 0 || layer >= v.layers) return CRISP_ERR_INVALID_ARG;
+  if (batch == 0 || n_tokens == 0) return CRISP_OK;
+  if (!q || !o || !aligned16(q) || !aligned16(o)) return CRISP_ERR_INVALID_ARG;
+  if (n_q_heads <= 0 || n_q_heads % v.heads != 0) return CRISP_ERR_INVALID_ARG;
+  if (!(softmax_scale >= 0.f) || !std::isfinite(softmax_scale)) return CRISP_ERR_INVALID_ARG;
+  if (n_q_heads / v.heads > kMaxGroup) return CRISP_ERR_UNSUPPORTED;
+  if (!ws) return CRISP_ERR_INVALID_ARG;
+  if (!aligned16(ws) || ws_bytes < cache_attention_ws_bytes()) return CRISP_ERR_WORKSPACE;
+  const float scale = softmax_scale > 0.f ? softmax_scale : 1.0f / std::sqrt(static_cast<float>(kHeadDim));
+  return launch_cache_attention(v, layer, b, n_q_heads, scale, q, o, lse, ws, static_cast<cudaStream_t>(cuda_stream));
+}
+
+int crisp_cache_fork(const crisp_cache* c, const int32_t* src, const int32_t* dst, const int32_t* n_tokens,
+                     int32_t count, int32_t share, void* ws, size_t ws_bytes, void* cuda_stream) {
+  CacheView v;
+  int rc = check_cache(c, &v);
+  if (rc == CRISP_OK) rc = check_count(count);
+  if (rc == CRISP_OK && count > 0 && (!src || !dst)) rc = CRISP_ERR_INVALID_ARG;
+  if (rc == CRISP_OK) rc = check_pages_ws(v, ws, ws_bytes);
+  if (rc != CRISP_OK || count == 0) return rc;
+  return launch_cache_fork(v, src, dst, n_tokens, count, share != 0, ws, static_cast<cudaStream_t>(cuda_stream));
+}
+
+int crisp_cache_free(const crisp_cache* c, const int32_t* seq_ids, int32_t count, void* ws, size_t ws_bytes,
+                     void* cuda_stream) {
+  CacheView v;
+  int rc = check_cache(c, &v);
+  if (rc == CRISP_OK) rc = check_count(count);
+  if (rc == CRISP_OK && count > 0 && !seq_ids) rc = CRISP_ERR_INVALID_ARG;
+  if (rc == CRISP_OK) rc = check_pages_ws(v, ws, ws_bytes);
+  if (rc != CRISP_OK || count == 0) return rc;
+  return launch_cache_free(v, seq_ids, count, ws, static_cast<cudaStream_t>(cuda_stream));
+}
+
+int crisp_cache_compact(const crisp_cache* c, int32_t* n_used, void* ws, size_t ws_bytes, void* cuda_stream) {
+  CacheView v;
+  int rc = check_cache(c, &v);
+  if (rc == CRISP_OK && !n_used) rc = CRISP_ERR_INVALID_ARG;
+  if (rc == CRISP_OK) rc = check_pages_ws(v, ws, ws_bytes);
+  if (rc != CRISP_OK) return rc;
+  return launch_cache_compact(v, n_used, ws, static_cast<cudaStream_t>(cuda_stream));
 }
 
 int crisp_poll_device_status(void* ws, void* cuda_stream) {

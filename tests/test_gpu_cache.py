@@ -1,0 +1,442 @@
+"""The paged 8-bit cache on the GPU against a plain cache in float64 (cache_reference.py): the quantising write and the
+page operations are exact and compared for equality; attention within bounds derived from its roundings."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2609_01925_b200 as crisp
+from paper_2609_01925_b200 import binding as B
+from tests import cache_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda"
+
+
+def i32(x):
+    return torch.tensor([int(v) for v in x], dtype=torch.int32, device=DEV)
+
+
+def tokens(n, heads, seed, spread=0.0):
+    """bf16 [n, heads, 128]; with `spread` the tokens' magnitudes differ by powers of two up to 2^spread."""
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(n, heads, 128, generator=g)
+    if spread:
+        x = x * torch.exp2(torch.rand(n, heads, 1, generator=g) * spread - spread / 2)
+    return x.bfloat16()
+
+
+class Both:
+    """A cache on the GPU and its reference, driven by the same calls."""
+
+    def __init__(self, fmt, heads, pages, max_seqs, max_pages, layers=1, garbage=True):
+        self.gpu = crisp.CrispCache.allocate(pages, heads, max_seqs, max_pages, n_layers=layers, fmt=fmt)
+        if garbage:   # what no token has been written to holds NaN codes and NaN scales
+            for t in (self.gpu.k_codes, self.gpu.v_codes):
+                t.fill_(0xff)
+            for t in (self.gpu.k_scale, self.gpu.v_scale):
+                t.fill_(float("nan"))
+        self.ref = ref.RefCache(layers, pages, heads, max_seqs, max_pages, fmt)
+
+    def grow(self, ids, n_new, seed, spread=0.0, layers=None):
+        """reserve, and append of random tokens to every layer (or the given ones)."""
+        heads = self.ref.heads
+        cu = np.concatenate([[0], np.cumsum(n_new)]).tolist()
+        self.gpu.reserve(i32(ids), i32(n_new))
+        self.ref.reserve(ids, n_new)
+        for layer in range(self.ref.layers) if layers is None else layers:
+            k, v = (tokens(cu[-1], heads, seed + 100003 * (2 * layer + j), spread) for j in range(2))
+            self.gpu.append(k.to(DEV), v.to(DEV), i32(ids), i32(cu), layer=layer)
+            self.ref.append(k.double().numpy(), v.double().numpy(), ids, cu, layer)
+
+    def check_tables(self):
+        self.gpu.poll()
+        assert np.array_equal(self.gpu.seq_lens.cpu().numpy(), self.ref.lens)
+        assert np.array_equal(self.gpu.page_refs.cpu().numpy(), self.ref.refs)
+        assert np.array_equal(self.gpu.page_table.cpu().numpy(), self.ref.table)
+
+    def check_contents(self):
+        """Every stored token's codes and every used block's scale are those of the reference."""
+        for name, codes, scale in (("k", self.gpu.k_codes, self.gpu.k_scale), ("v", self.gpu.v_codes, self.gpu.v_scale)):
+            codes, scale = codes.cpu().numpy(), scale.cpu().numpy()
+            for s in range(self.ref.max_seqs):
+                n = self.ref.lens[s]
+                for j in range(ref.pages_of(n)):
+                    p, rows = self.ref.table[s, j], min(128, n - 128 * j)
+                    got = ref.values(codes[:, p, :, :rows], self.ref.fmt)
+                    want = ref.values(self.ref.codes[name][:, p, :, :rows], self.ref.fmt)
+                    np.testing.assert_array_equal(got, want)
+                    np.testing.assert_array_equal(scale[:, p], 2.0 ** self.ref.exps[name][:, p])
+
+    def check_attention(self, hq, ids, n_new, seed, layer=0, q=None, cu=None, **kw):
+        if cu is None:
+            cu = np.concatenate([[0], np.cumsum(n_new)]).tolist()
+        if q is None:
+            q = tokens(cu[-1], hq, seed)
+        lse = torch.full((hq, q.shape[0]), 7.0, device=DEV)
+        o = torch.full(q.shape, 7.0, dtype=torch.bfloat16, device=DEV)
+        out = self.gpu.attention(q.to(DEV), i32(ids), i32(cu), max_new=max(n_new), layer=layer, o=o, lse=lse, **kw)
+        assert out is o
+        self.gpu.poll()
+        want = self.ref.attention(q.double().numpy(), ids, cu, layer)
+        check_rows(o, lse, want, max(n_new) * hq // self.ref.heads)
+        return o, lse
+
+
+def check_rows(o, lse, reference, rows, untouched=7.0):
+    want, want_lse, slack, dots = reference
+    o, lse = o.double().cpu().numpy(), lse.double().cpu().numpy()
+    none = np.isnan(want)
+    assert (o[none] == untouched).all() and (lse[np.isnan(want_lse)] == untouched).all()
+    # weights are rounded to fp16 (2^-11) by the kernel for few rows, to bf16 (2^-8) by the one for many
+    tol = ref.tolerance(want, slack, 2.0 ** -11 if rows <= 32 else 2.0 ** -8, 64)
+    bad = ~none & ~(np.abs(o - want) <= tol)
+    assert not bad.any(), (int(bad.sum()), np.argwhere(bad)[:4], np.nanmax(np.abs(o - want) / tol))
+    fin = np.isfinite(want_lse)
+    assert np.array_equal(lse == -np.inf, want_lse == -np.inf)
+    assert (np.abs(lse[fin] - want_lse[fin]) <= ref.lse_tolerance(want_lse[fin], dots[fin], 64)).all()
+
+
+# ------------------------------------------------------------------------------------------------ append
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("spread", [0.0, 12.0, 60.0])
+def test_append_in_pieces_equals_the_definition(fmt, spread):
+    """Pieces of one token, across page borders, of whole pages, from sequences in any order; scales that grow."""
+    both = Both(fmt, heads=3, pages=24, max_seqs=5, max_pages=6)
+    seed = 0
+    for ids, n_new in (([2, 0, 4], [1, 127, 130]), ([0, 2], [1, 1]), ([4, 2, 0], [126, 255, 2]), ([1], [300]),
+                       ([0, 1, 2, 4], [1, 1, 1, 1]), ([3, 1], [0, 1]), ([-1, 3, -1], [0, 5, 0])):
+        both.grow(ids, n_new, seed, spread)
+        seed += 2
+        both.check_tables()
+        both.check_contents()
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+def test_append_of_extreme_values(fmt):
+    """Zeros, infinities, NaN, the largest and the smallest bf16 numbers, exact ties and scale borders."""
+    both = Both(fmt, heads=2, pages=8, max_seqs=2, max_pages=4)
+    k, v = tokens(200, 2, 1), tokens(200, 2, 2)
+    top = torch.finfo(torch.bfloat16).max
+    k[0, 0, :4] = torch.tensor([float("inf"), -float("inf"), float("nan"), -0.0])
+    k[1, 1] = 0
+    k[5, 0, 7] = 448 * 2.0 ** 3             # exactly the border of e = 3 (e4m3)
+    v[:128, 0] = 0                          # a block of zeros
+    v[128:, 0] *= 2.0 ** -130               # subnormal values
+    v[3, 1, 5] = top
+    k[130:, 1] = torch.linspace(-508, 508, 70)[:, None].bfloat16().expand(70, 128)   # ties on the int8 grid
+    both.gpu.reserve(i32([1]), i32([200]))
+    both.ref.reserve([1], [200])
+    both.gpu.append(k.to(DEV), v.to(DEV), i32([1]))
+    both.ref.append(k.double().numpy(), v.double().numpy(), [1], [0, 200])
+    both.check_tables()
+    both.check_contents()
+
+
+def test_append_writes_only_its_layer_and_its_rows():
+    both = Both("e4m3", heads=2, pages=6, max_seqs=3, max_pages=2, layers=3)
+    both.grow([1, 0], [100, 20], 5, layers=[1])
+    got = both.gpu.k_codes.cpu().numpy()
+    assert (got[[0, 2]] == 0xff).all()
+    assert (got[1, both.ref.table[1, 0], :, 100:] == 0xff).all() and (got[1, both.ref.table[0, 0], :, 20:] == 0xff).all()
+    assert (got[1, 2:] == 0xff).all()
+
+
+# ------------------------------------------------------------------------------------------------ attention
+SHAPES = [(4, 1), (8, 2), (7, 1), (2, 2), (16, 1), (6, 2)]
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("hq,hkv", SHAPES)
+def test_one_token_at_many_lengths(fmt, hq, hkv):
+    lens = [1, 2, 31, 32, 33, 127, 128, 129, 300, 1000]
+    both = Both(fmt, hkv, pages=40, max_seqs=len(lens), max_pages=8)
+    both.grow(list(range(len(lens))), lens, 11, spread=2.0)
+    ids = [3, 9, 0, 1, 7, 2, 8, 4, 5, 6]
+    both.check_attention(hq, ids, [1] * len(ids), 12)
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("hq,hkv", SHAPES)
+@pytest.mark.parametrize("new", [[2, 1, 3, 2], [5, 1, 0, 4], [9, 30, 16, 1]])
+def test_several_new_tokens(fmt, hq, hkv, new):
+    lens = [2, 130, 300, 517]
+    both = Both(fmt, hkv, pages=16, max_seqs=4, max_pages=6)
+    both.grow([0, 1, 2, 3], [max(n, m) for n, m in zip(lens, new)], 21)
+    both.check_attention(hq, [0, 1, 2, 3], new, 22)
+
+
+@pytest.mark.parametrize("new", [1, 3])
+def test_rows_that_see_nothing_and_padding(new):
+    """Empty sequences, more queries than keys, padding entries, tokens behind the last item: zeros or untouched."""
+    both = Both("e4m3", 2, pages=8, max_seqs=5, max_pages=3)
+    both.grow([1, 3], [2, 200], 31)
+    ids = [0, 1, -1, 3, 4]
+    cu = [0, new, new + 3, new + 4, new + 5, new + 6]
+    q = tokens(cu[-1] + 2, 8, 32)
+    o, lse = both.check_attention(8, ids, [3], 0, q=q, cu=cu)
+    assert (o[:new] == 0).all() and (lse[:, :new] == -float("inf")).all()
+    assert (o[new] == 0).all()           # the first of three queries over two keys
+    assert (o[-2:] == 7).all() and (o[new + 3] == 7).all()
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+def test_long_sequences_are_cut_and_joined(fmt):
+    """A single long sequence is spread over all CTAs (two levels of joining), beside short ones."""
+    both = Both(fmt, 1, pages=420, max_seqs=3, max_pages=400)
+    both.grow([1, 0, 2], [50000, 5, 777], 41)
+    both.check_attention(4, [1], [1], 42)
+    both.check_attention(4, [0, 1, 2], [1, 1, 1], 43)
+    both.check_attention(4, [1, 2], [5, 2], 44)
+
+
+def test_very_different_scales_between_pages():
+    """Pages whose scales differ by 2^100 in V and by 2^20 in K."""
+    both = Both("e4m3", 1, pages=8, max_seqs=1, max_pages=6)
+    for i, (ek, ev) in enumerate([(0, 0), (-10, 60), (10, -40), (0, -126)]):
+        k, v = tokens(128, 1, 50 + 2 * i) * 2.0 ** ek, tokens(128, 1, 51 + 2 * i) * 2.0 ** ev
+        both.gpu.reserve(i32([0]), i32([128]))
+        both.ref.reserve([0], [128])
+        both.gpu.append(k.to(DEV), v.to(DEV), i32([0]))
+        both.ref.append(k.double().numpy(), v.double().numpy(), [0], [0, 128])
+    q = tokens(2, 4, 60)
+    q[0] *= 2.0 ** -120
+    both.check_attention(4, [0], [2], 0, q=q)
+
+
+def test_layers_and_scale_and_repeats():
+    both = Both("int8", 2, pages=12, max_seqs=3, max_pages=4, layers=2)
+    both.grow([0, 2], [300, 10], 71)
+    both.check_attention(4, [2, 0, 0, 2], [1, 1, 1, 1], 72, layer=1)   # a sequence may be read twice
+    q = tokens(2, 4, 73)
+    o = both.gpu.attention(q.to(DEV), i32([0, 2]), layer=1, softmax_scale=0.5)
+    want, _, slack, _ = ref.attention(lambda s: (both.ref.states("k", s, 1), both.ref.states("v", s, 1)),
+                                   q.double().numpy(), [0, 2], [0, 1, 2], 0.5)
+    assert (np.abs(o.double().cpu().numpy() - want) <= ref.tolerance(want, slack, 2.0 ** -11, 64)).all()
+
+
+def test_same_call_same_bits_and_uniform_form():
+    both = Both("e4m3", 2, pages=200, max_seqs=4, max_pages=100)
+    both.grow([0, 1, 2], [9000, 300, 4000], 81)
+    q = tokens(6, 8, 82).to(DEV)
+    a = both.gpu.attention(q, i32([2, 0, 1]), i32([0, 2, 4, 6]))
+    b = both.gpu.attention(q, i32([2, 0, 1]))
+    c = both.gpu.attention(q, i32([2, 0, 1]))
+    assert torch.equal(b, c) and torch.equal(a, b)
+
+
+# ------------------------------------------------------------------------------------------------ pages
+def test_pages_random_walk():
+    """Reserve, append, fork (shared and copied, whole and cut), free and compact in random order: tables equal, and
+    contents of all that is stored equal."""
+    rng = np.random.RandomState(3)
+    both = Both("e4m3", heads=1, pages=60, max_seqs=8, max_pages=7, layers=2)
+    for step in range(120):
+        live = [s for s in range(8) if both.ref.lens[s] > 0]
+        empty = [s for s in range(8) if both.ref.lens[s] == 0]
+        op = rng.randint(5)
+        try:
+            if op <= 1:
+                ids = rng.permutation(8)[:rng.randint(1, 5)].tolist()
+                n = [int(rng.choice([1, 1, 7, 128, 200])) for _ in ids]
+                if any(both.ref.lens[s] + m > 7 * 128 for s, m in zip(ids, n)):
+                    continue
+                both.ref._take(sum(ref.pages_of(both.ref.lens[s] + m) - ref.pages_of(both.ref.lens[s]) for s, m in zip(ids, n)))
+                both.grow(ids, n, 1000 + 2 * step, spread=4.0)
+            elif op == 2 and live and empty:
+                dst = empty[:rng.randint(1, len(empty) + 1)]
+                src = [int(rng.choice(live)) for _ in dst]
+                n = [int(rng.randint(0, both.ref.lens[s] + 1)) for s in src] if rng.randint(2) else None
+                share = bool(rng.randint(3))
+                both.ref.fork(src, dst, n, share)
+                both.gpu.fork(i32(src), i32(dst), None if n is None else i32(n), share)
+            elif op == 3:
+                ids = rng.permutation(8)[:rng.randint(1, 4)].tolist()
+                ids = ids + ids[:1] + [-1]        # twice, and padding
+                both.ref.free(ids)
+                both.gpu.free(i32(ids))
+            else:
+                assert int(both.gpu.compact().item()) == both.ref.compact()
+        except ref.Refused:
+            continue
+        both.check_tables()
+    both.check_contents()
+
+
+def test_calls_that_do_not_fit_change_nothing():
+    both = Both("e4m3", heads=1, pages=4, max_seqs=4, max_pages=3)
+    both.grow([0, 1], [130, 100], 91)
+    before = [t.clone() for t in (both.gpu.page_table, both.gpu.seq_lens, both.gpu.page_refs, both.gpu.k_codes)]
+
+    def refused(code, call, *args, **kw):
+        call(*args, **kw)
+        with pytest.raises(crisp.CrispError) as e:
+            both.gpu.poll()
+        assert e.value.status == code
+        both.gpu.poll()
+        for a, b in zip(before, (both.gpu.page_table, both.gpu.seq_lens, both.gpu.page_refs, both.gpu.k_codes)):
+            assert torch.equal(a, b)
+
+    refused(B.ERR_NO_PAGES, both.gpu.reserve, i32([2, 1]), i32([128, 29]))          # two pages, one free
+    refused(B.ERR_NO_PAGES, both.gpu.reserve, i32([0]), i32([300]))                 # longer than a row
+    refused(B.ERR_BAD_CACHE, both.gpu.reserve, i32([2, 2]), i32([1, 1]))            # twice
+    refused(B.ERR_BAD_CACHE, both.gpu.reserve, i32([4]))                            # no such sequence
+    refused(B.ERR_BAD_CACHE, both.gpu.reserve, i32([0]), i32([-1]))
+    refused(B.ERR_NO_PAGES, both.gpu.fork, i32([0, 1]), i32([2, 3]))                # two copies, one free
+    refused(B.ERR_BAD_CACHE, both.gpu.fork, i32([0]), i32([1]))                     # not empty
+    refused(B.ERR_BAD_CACHE, both.gpu.fork, i32([0, 1]), i32([2, 2]))               # twice
+    refused(B.ERR_BAD_CACHE, both.gpu.fork, i32([0]), i32([2]), i32([131]))         # longer than its source
+    refused(B.ERR_BAD_CACHE, both.gpu.free, i32([9]))
+
+
+def test_append_refuses_what_it_must_not_write():
+    both = Both("e4m3", heads=1, pages=8, max_seqs=4, max_pages=3)
+    both.grow([0], [256], 95)
+    both.gpu.fork(i32([0]), i32([1]))
+    before = both.gpu.k_codes.clone()
+    k = tokens(10, 1, 96).to(DEV)
+    for ids, cu in (([0], [0, 10]),        # its last page is shared
+                    ([2], [0, 10]),        # more new tokens than it has
+                    ([7], [0, 10])):       # no such sequence
+        both.gpu.append(k, k, i32(ids), i32(cu))
+        with pytest.raises(crisp.CrispError) as e:
+            both.gpu.poll()
+        assert e.value.status == B.ERR_BAD_CACHE
+    both.gpu.append(k, k, i32([0]), i32([0, 11]))   # offsets beyond the tokens
+    with pytest.raises(crisp.CrispError):
+        both.gpu.poll()
+    both.gpu.append(k, k, i32([0]), i32([5, 3]))    # offsets that fall
+    with pytest.raises(crisp.CrispError):
+        both.gpu.poll()
+    assert torch.equal(before, both.gpu.k_codes)
+
+
+def test_attention_skips_what_breaks_its_rules():
+    """Items with a bad description are reported and their rows left alone; the others are computed."""
+    both = Both("e4m3", heads=1, pages=8, max_seqs=3, max_pages=3)
+    both.grow([0, 1], [200, 90], 97)
+    q = tokens(6, 4, 98).to(DEV)
+    want = both.gpu.attention(q[:1], i32([0]))
+    o = torch.full_like(q, 7.0)
+    both.gpu.attention(q, i32([0, 5, 1]), i32([0, 1, 2, 6]), max_new=2, o=o)   # no sequence 5; four tokens are over 2
+    with pytest.raises(crisp.CrispError) as e:
+        both.gpu.poll()
+    assert e.value.status == B.ERR_BAD_CACHE
+    assert torch.equal(o[0], want[0]) and (o[1:] == 7).all()
+    both.gpu.page_table[0, 1] = 8               # no such page: reported, nothing read beyond the pool
+    both.gpu.attention(q[:1], i32([0]))
+    with pytest.raises(crisp.CrispError):
+        both.gpu.poll()
+
+
+# ------------------------------------------------------------------------------------------------ as they are used
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+def test_prompt_answer_branch_and_compact(fmt):
+    """The way of a request: a prompt through Algorithm 1, its K/V into the cache, answer tokens, a branch, the first
+    user leaves, the pool is compacted, and the branch answers on.  Attention is checked at every step."""
+    from workloads import synth
+    w = synth.tiny(n=700)
+    q, k, v = synth.make_qkv(w, device=DEV)
+    hq, hkv = w.n_q_heads, w.n_kv_heads
+    p = crisp.make_params(w.seq_len, hq, hkv, sink_tokens=w.sink_tokens, local_tokens=w.local_tokens)
+    layer = crisp.CrispLayer(p)
+    layer.forward(q, k, v)
+    layer.poll()
+    both = Both(fmt, hkv, pages=20, max_seqs=4, max_pages=10)
+
+    def write(ids, cu, k, v):
+        n = [b - a for a, b in zip(cu, cu[1:])]
+        both.gpu.reserve(i32(ids), i32(n))
+        both.gpu.append(k.to(DEV), v.to(DEV), i32(ids), i32(cu))
+        both.ref.reserve(ids, n)
+        both.ref.append(k.double().cpu().numpy(), v.double().cpu().numpy(), ids, cu)
+
+    write([0], [0, 700], k, v)
+    for step in range(3):
+        write([0], [0, 1], tokens(1, hkv, 200 + step), tokens(1, hkv, 210 + step))
+        both.check_attention(hq, [0], [1], 220 + step)
+    both.gpu.fork(i32([0, 0]), i32([1, 3]), i32([650, 703]))
+    both.ref.fork([0, 0], [1, 3], [650, 703])
+    write([3, 1, 0], [0, 1, 3, 4], tokens(4, hkv, 230), tokens(4, hkv, 231))
+    both.check_attention(hq, [3, 1, 0], [1, 2, 1], 232)
+    both.gpu.free(i32([0]))
+    both.ref.free([0])
+    assert int(both.gpu.compact().item()) == both.ref.compact()
+    write([1, 3], [0, 1, 2], tokens(2, hkv, 240), tokens(2, hkv, 241))
+    both.check_attention(hq, [1, 3], [1, 1], 242)
+    both.check_tables()
+    both.check_contents()
+
+
+def test_step_in_a_graph_and_on_another_stream():
+    """reserve, append and attention of a decode step replay from one CUDA graph as the sequences grow; the same step on
+    a side stream gives the same bits."""
+    both, other = (Both("e4m3", 2, pages=24, max_seqs=3, max_pages=8) for _ in range(2))
+    for b in (both, other):
+        b.grow([0, 1, 2], [126, 300, 5], 301)
+    ids = i32([2, 0, 1])
+    steps = [[tokens(3, h, 310 + 3 * s + j).to(DEV) for j, h in enumerate((8, 2, 2))] for s in range(5)]
+    q, k, v = (x.clone() for x in steps[0])
+    o = torch.empty_like(q)
+    lse = torch.empty(8, 3, device=DEV)
+
+    def step(c):
+        c.reserve(ids)
+        c.append(k, v, ids)
+        c.attention(q, ids, o=o, lse=lse)
+
+    torch.cuda.synchronize()
+    state = [t.clone() for t in (both.gpu.page_table, both.gpu.seq_lens, both.gpu.page_refs)]
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        step(both.gpu)     # set-up outside the capture
+    torch.cuda.synchronize()
+    for t, s in zip((both.gpu.page_table, both.gpu.seq_lens, both.gpu.page_refs), state):
+        t.copy_(s)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(both.gpu)
+    for s in range(5):
+        for dst, src in zip((q, k, v), steps[s]):
+            dst.copy_(src)
+        graph.replay()
+        torch.cuda.synchronize()
+        got, got_lse = o.clone(), lse.clone()
+        stream = torch.cuda.Stream()
+        stream.wait_stream(torch.cuda.current_stream())
+        other.gpu.reserve(ids, stream=stream)
+        other.gpu.append(steps[s][1], steps[s][2], ids, stream=stream)
+        want_lse = torch.empty_like(lse)
+        want = other.gpu.attention(steps[s][0], ids, lse=want_lse, stream=stream)
+        stream.synchronize()
+        assert torch.equal(got, want) and torch.equal(got_lse, want_lse)
+    both.gpu.poll()
+    other.gpu.poll()
+    assert both.gpu.seq_lens.tolist() == [131, 305, 10]
+
+
+def test_arguments_are_checked():
+    c = crisp.CrispCache.allocate(4, 2, 2, 2)
+    q = tokens(2, 4, 1).to(DEV)
+    ids = i32([0, 1])
+    for bad in (lambda: c.attention(q.float(), ids), lambda: c.attention(q.transpose(0, 1), ids),
+                lambda: c.attention(q, ids.long()), lambda: c.attention(q, ids, i32([0, 2])),
+                lambda: c.attention(q.cpu(), ids), lambda: c.attention(q, ids, lse=torch.empty(2, 4, device=DEV)),
+                lambda: c.attention(q, ids, o=q[:1]), lambda: c.append(q, q, ids), lambda: c.reserve(ids, i32([1])),
+                lambda: c.append(q[:, :2].contiguous(), q[:1, :2].contiguous(), ids),
+                lambda: c.fork(ids, i32([0])), lambda: c.free(ids[::2].expand(2)),
+                lambda: crisp.CrispCache(c.k_codes, c.v_codes, c.k_scale, c.v_scale, c.page_table, c.seq_lens,
+                                         c.page_refs, fmt="fp4"),
+                lambda: crisp.CrispCache(c.k_codes, c.v_codes[:, :3], c.k_scale, c.v_scale, c.page_table, c.seq_lens,
+                                         c.page_refs)):
+        with pytest.raises(ValueError):
+            bad()
+    for bad in (lambda: c.attention(q, ids, layer=1), lambda: c.attention(q, ids, softmax_scale=-1.0),
+                lambda: c.attention(q, ids, max_new=0), lambda: c.attention(tokens(3, 4, 1).to(DEV), ids),
+                lambda: c.attention(tokens(2, 3, 1).to(DEV), ids), lambda: c.attention(tokens(2, 34, 1).to(DEV), ids)):
+        with pytest.raises(crisp.CrispError):
+            bad()
+    c.attention(q[:0], ids[:0])            # nothing to do
+    c.reserve(ids[:0])
+    c.free(ids[:0])
+    c.poll()
