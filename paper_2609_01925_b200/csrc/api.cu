@@ -103,7 +103,7 @@ int make_tmap_bf16_nhd(CUtensorMap* out, const void* base, int n, int heads, int
   return CRISP_OK;
 }
 
-int make_tmap_codes(CUtensorMap* out, const void* base, size_t rows) {
+int make_tmap_codes(CUtensorMap* out, const void* base, size_t rows, int box_rows) {
   EncodeTiledFn enc = encode_fn();
   if (!enc) {
     set_cu_error("cuTensorMapEncodeTiled is not available (no CUDA driver?)");
@@ -111,7 +111,7 @@ int make_tmap_codes(CUtensorMap* out, const void* base, size_t rows) {
   }
   const cuuint64_t dims[2] = {static_cast<cuuint64_t>(kHeadDim), static_cast<cuuint64_t>(rows)};
   const cuuint64_t strides[1] = {static_cast<cuuint64_t>(kHeadDim)};
-  const cuuint32_t box[2] = {static_cast<cuuint32_t>(kHeadDim), static_cast<cuuint32_t>(kPage)};
+  const cuuint32_t box[2] = {static_cast<cuuint32_t>(kHeadDim), static_cast<cuuint32_t>(box_rows)};
   const cuuint32_t estr[2] = {1, 1};
   CUresult r = enc(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr,
                    CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
@@ -224,6 +224,8 @@ int check_batch(const int32_t* seq_ids, const int32_t* cu, int32_t batch, int32_
   if (!cu && b->per > b->max_new) return CRISP_ERR_INVALID_ARG;
   return CRISP_OK;
 }
+
+static size_t attention_ws_bytes() { return cache_prefill_ws(nullptr, cache_decode_ws(nullptr, kWsHeader)); }
 
 static int check_pages_ws(const CacheView& v, const void* ws, size_t ws_bytes) {
   if (!ws) return CRISP_ERR_INVALID_ARG;
@@ -757,7 +759,7 @@ int crisp_cache_workspace_bytes(const crisp_cache* c, size_t* pages_ws, size_t* 
   const int rc = check_cache(c, &v);
   if (rc != CRISP_OK) return rc;
   if (pages_ws) *pages_ws = cache_pages_ws_bytes(v);
-  if (attention_ws) *attention_ws = cache_attention_ws_bytes();
+  if (attention_ws) *attention_ws = attention_ws_bytes();
   return CRISP_OK;
 }
 
@@ -801,9 +803,24 @@ int crisp_cache_attention(const crisp_cache* c, int32_t layer, const int32_t* se
   if (!(softmax_scale >= 0.f) || !std::isfinite(softmax_scale)) return CRISP_ERR_INVALID_ARG;
   if (n_q_heads / v.heads > kMaxGroup) return CRISP_ERR_UNSUPPORTED;
   if (!ws) return CRISP_ERR_INVALID_ARG;
-  if (!aligned16(ws) || ws_bytes < cache_attention_ws_bytes()) return CRISP_ERR_WORKSPACE;
+  if (!aligned16(ws) || ws_bytes < attention_ws_bytes()) return CRISP_ERR_WORKSPACE;
   const float scale = softmax_scale > 0.f ? softmax_scale : 1.0f / std::sqrt(static_cast<float>(kHeadDim));
-  return launch_cache_attention(v, layer, b, n_q_heads, scale, q, o, lse, ws, static_cast<cudaStream_t>(cuda_stream));
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  int dev = 0, n_sm = 0;
+  CRISP_CUDA_TRY(cudaGetDevice(&dev), "cache_attention: device");
+  CRISP_CUDA_TRY(cudaDeviceGetAttribute(&n_sm, cudaDevAttrMultiProcessorCount, dev), "cache_attention: SM count");
+  const size_t decode_off = kWsHeader, prefill_off = cache_decode_ws(nullptr, decode_off);
+  // Up to 16 rows per KV head (new tokens x query heads of its group) are two fragments of the kernel that reads the
+  // cache at HBM speed; more rows would make it read the cache again.
+  const bool few = static_cast<long long>(b.max_new) * (n_q_heads / v.heads) <= kDecodeRows;
+  CUtensorMap tk, tv;
+  const size_t code_rows = static_cast<size_t>(v.layers) * v.pages * v.heads * kPage;
+  rc = make_tmap_codes(&tk, v.k_codes, code_rows, few ? kPage : kPage / 2);
+  if (rc == CRISP_OK) rc = make_tmap_codes(&tv, v.v_codes, code_rows, few ? kPage : kPage / 2);
+  if (rc != CRISP_OK) return rc;
+  if (few)
+    return launch_cache_decode(v, layer, b, n_q_heads, scale, q, o, lse, ws, decode_off, tk, tv, n_sm, st);
+  return launch_cache_prefill(v, layer, b, n_q_heads, scale, q, o, lse, ws, prefill_off, tk, tv, n_sm, st);
 }
 
 int crisp_cache_fork(const crisp_cache* c, const int32_t* src, const int32_t* dst, const int32_t* n_tokens,

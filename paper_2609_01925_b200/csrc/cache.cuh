@@ -6,6 +6,8 @@ namespace crisp {
 
 constexpr int kPage = kBlock;              // tokens of a page = the block of the sparse path
 constexpr int kPageTileBytes = kPage * kHeadDim;  // codes of one page and KV head, K or V: 16 KB
+constexpr int kMaxSets = 3;                // sets of eight rows of the kernel for few rows
+constexpr int kDecodeRows = 8 * kMaxSets;  // most rows per KV head that it takes
 constexpr int kMaxCacheBatch = CRISP_CACHE_MAX_BATCH;
 
 // A crisp_cache passed to kernels by value.
@@ -30,8 +32,8 @@ int check_cache(const crisp_cache* c, CacheView* v);
 int check_batch(const int32_t* seq_ids, const int32_t* cu, int32_t batch, int32_t n_tokens,
                 int32_t max_new, CacheBatch* b);
 
-// Tensor map of the code tiles, [rows][128] bytes, with a {128, 128} box and 128-byte swizzle.
-int make_tmap_codes(CUtensorMap* out, const void* base, size_t rows);
+// Tensor map of the code tiles, [rows][128] bytes, with a {128, box_rows} box and 128-byte swizzle.
+int make_tmap_codes(CUtensorMap* out, const void* base, size_t rows, int box_rows);
 
 int launch_cache_reserve(const CacheView& v, const int32_t* seq_ids, const int32_t* n_new, int batch, void* ws,
                          cudaStream_t stream);
@@ -41,10 +43,17 @@ int launch_cache_fork(const CacheView& v, const int32_t* src, const int32_t* dst
                       int share, void* ws, cudaStream_t stream);
 int launch_cache_free(const CacheView& v, const int32_t* seq_ids, int count, void* ws, cudaStream_t stream);
 int launch_cache_compact(const CacheView& v, int32_t* n_used, void* ws, cudaStream_t stream);
-int launch_cache_attention(const CacheView& v, int layer, const CacheBatch& b, int n_q_heads, float scale, const void* q,
-                           void* o, float* lse, void* ws, cudaStream_t stream);
+// Attention: the kernel for few rows per KV head (cache_attention.cu) and the one for many (cache_prefill.cu).  The
+// workspace is the header, then each kernel's part; *_ws returns the offset behind it.
+int launch_cache_decode(const CacheView& v, int layer, const CacheBatch& b, int n_q_heads, float scale, const void* q,
+                        void* o, float* lse, void* ws, size_t ws_off, const CUtensorMap& tk, const CUtensorMap& tv, int n_sm,
+                        cudaStream_t stream);
+int launch_cache_prefill(const CacheView& v, int layer, const CacheBatch& b, int n_q_heads, float scale, const void* q,
+                         void* o, float* lse, void* ws, size_t ws_off, const CUtensorMap& tk, const CUtensorMap& tv, int n_sm,
+                         cudaStream_t stream);
+size_t cache_decode_ws(void* ws, size_t off);
+size_t cache_prefill_ws(void* ws, size_t off);
 size_t cache_pages_ws_bytes(const CacheView& v);
-size_t cache_attention_ws_bytes();
 
 #ifdef __CUDACC__
 __host__ __device__ __forceinline__ int pages_of(int tokens) { return (tokens + kPage - 1) / kPage; }
