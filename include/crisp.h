@@ -286,10 +286,9 @@ int crisp_forward_host(const crisp_params* p, const void* q_host, const void* k_
  * skipped; NULL means item i is sequence i.  At most CRISP_CACHE_MAX_BATCH items.  Nothing on the device is trusted:
  * what breaks a rule is not read or written, and sets the status word of the workspace to CRISP_ERR_BAD_CACHE or
  * CRISP_ERR_NO_PAGES.  Unlike the calls above, cache calls do not clear that word: the first error stays until
- * crisp_poll_device_status, so a run of calls needs one poll.  The caller therefore zeroes a workspace once before
- * its first use (all of crisp_cache_attention's - it counts in it, and the counts are zero again after the call - and
- * the first 256 bytes of the other), and again after CRISP_ERR_DEVICE_TIMEOUT.  Calls that use one workspace must not
- * overlap in time, and neither must calls that change one cache.
+ * crisp_poll_device_status, so a run of calls needs one poll.  The caller therefore zeroes the first 256 bytes of a
+ * workspace once before its first use.  Calls that use one workspace must not overlap in time, and neither must calls
+ * that change one cache.
  */
 #define CRISP_CACHE_E4M3 0
 #define CRISP_CACHE_INT8 1

@@ -9,7 +9,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcrisp.so")
 SOURCES = ["api.cu", "route.cu", "select.cu", "prefill.cu", "cache_pages.cu", "cache_attention.cu", "cache_prefill.cu",
-           "selftest.cu"]
+           "cache_join.cu", "selftest.cu"]
 HEADERS = ["common.cuh", "cache.cuh", "cache_split.cuh", "cache_codes.cuh", "softmax_rows.cuh",
            "sm100_ptx.cuh", os.path.join("..", "..", "include", "crisp.h")]
 

@@ -54,8 +54,10 @@ class CrispCache:
                                      max_pages, 128, *(t.data_ptr() for t in (
                                          k_codes, v_codes, k_scale, v_scale, page_table, seq_lens, page_refs)))
         pages_ws, attention_ws = B.crisp_cache_workspace_bytes(self.desc)
-        self.pages_ws = torch.zeros(pages_ws, dtype=torch.uint8, device=self.device)
-        self.attention_ws = torch.zeros(attention_ws, dtype=torch.uint8, device=self.device)
+        self.pages_ws, self.attention_ws = (torch.empty(n, dtype=torch.uint8, device=self.device)
+                                            for n in (pages_ws, attention_ws))
+        for ws in (self.pages_ws, self.attention_ws):
+            ws[:256].zero_()   # status words: the calls only set them
         self._c = ctypes.byref(self.desc)
 
     @classmethod
@@ -183,7 +185,5 @@ class CrispCache:
         with torch.cuda.device(self.device):
             status = [(name, B.crisp_poll_device_status(ws, stream))
                       for ws, name in ((self.pages_ws, "pages"), (self.attention_ws, "attention"))]
-        if status[1][1] == B.ERR_DEVICE_TIMEOUT:
-            self.attention_ws.zero_()   # the call that gave up may have left its counters behind
         for name, rc in status:
             B.check(rc, f"cache status ({name})")

@@ -5,8 +5,7 @@
 //  * One unit of work is one page of one KV head (16 KB of K codes, 16 KB of V codes, by TMA into a ring of slots).
 //    The units of all items and heads form one sequence that is cut into equal runs, one per CTA, whatever the
 //    lengths are; a run that begins or ends inside a group leaves a partial result (maximum, sum, O) in the workspace,
-//    and the CTA that completes a set of partials joins them: first within sets of 16 CTAs, then the sets' results, so
-//    a single long sequence is not joined by one CTA alone.  The order of every sum is fixed by the sizes.
+//    and a second small kernel joins them (cache_split.cuh).  The order of every sum is fixed by the sizes.
 //  * Codes are not converted in bulk: a warp takes its fragments from shared memory, converts them in registers and
 //    multiplies with m16n8k16 (fp16 in, fp32 out).  Products are computed transposed, S^T = K Q^T and O^T = V^T P^T, so
 //    that the padded dimension, N = 8, is the few query rows.  (tcgen05 has no shape for so few rows without
@@ -38,20 +37,6 @@ __host__ __device__ constexpr int ctas_per_sm(int sets) { return sets == 1 ? 3 :
 __host__ __device__ constexpr int slots_of(int sets) { return sets == 1 ? 3 : 8; }  // ring slots of one K or V tile
 __host__ __device__ constexpr int threads_of(int sets) { return sets * kSetWarps * 32 + 32; }
 
-Partials carve_decode(void* ws, size_t* off) {
-  uint8_t* base = static_cast<uint8_t*>(ws);
-  Partials w;
-  w.n_slots = 2 * kMaxCtas;
-  w.rows = kMaxRows;
-  w.counters = reinterpret_cast<int*>(base + *off);
-  *off += sizeof(int) * 2 * w.n_slots;
-  w.ml = reinterpret_cast<float2*>(base + *off);
-  *off += sizeof(float2) * w.n_slots * kMaxRows;
-  w.o = reinterpret_cast<float*>(base + *off);
-  *off += sizeof(float) * w.n_slots * kMaxRows * kHeadDim;
-  return w;
-}
-
 struct AttnArgs {
   CacheView c;
   CacheBatch b;
@@ -73,7 +58,6 @@ struct DecodeSmem {
   uint64_t full[slots_of(kSets)], empty[slots_of(kSets)], q_full[2], q_empty[2];
   long long scratch[33];
   int abort_flag;
-  int last;
   int start[kMaxCacheBatch + 1];   // units of one head before item i
 };
 
@@ -180,13 +164,14 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
   }
   if (tid == 0) s.start[batch] = static_cast<int>(min(carry, 0x7fffffffLL));
   __syncthreads();
-  if (carry * heads >= 0x7fffffffLL) {  // units are counted in 32 bits
-    if (tid == 0) cache_fail(a.status, CRISP_ERR_BAD_CACHE);
+  const bool too_many = carry * heads >= 0x7fffffffLL;  // units are counted in 32 bits
+  if (too_many && tid == 0) cache_fail(a.status, CRISP_ERR_BAD_CACHE);
+  const Cut cut(too_many ? 0 : static_cast<int>(carry) * heads, gridDim.x);
+  const int cta = blockIdx.x;
+  if (cta >= cut.ctas) {
+    if (tid == 0) a.w.desc[cta].rows = 0;  // nothing to join
     return;
   }
-  const Cut cut(static_cast<int>(carry) * heads, gridDim.x);
-  const int cta = blockIdx.x;
-  if (cta >= cut.ctas) return;
   const int u0 = cut.first(cta), u1 = cut.first(cta + 1);
   volatile int* abort_flag = &s.abort_flag;
   Walk<kRowTile> w;
@@ -271,6 +256,7 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
       }
     };
     bool ok = true;  // after a wait that gave up, the loops and barriers run on without waiting
+    JoinDesc todo = {0, 0, 0, 0, 0, 0};
     for (w.seek(s.start, a, u0);; w.next(s.start, a)) {
       if (w.clip(u0, u1)) {
         const Segment& g = w.g;
@@ -485,12 +471,12 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
             if (lane == 0) a.w.ml[at] = make_float2(top, sum);
           }
         }
-        if (!whole)
-          finish_partial<kWarps>(cut, g, cta, a.w, a.out, it.t0, g.tile * kRowTile, min(kRowTile, w.rows - g.tile * kRowTile),
-                                 &s.last);
+        const JoinDesc d = join_desc(cut, g, cta, it.t0, g.tile * kRowTile, min(kRowTile, w.rows - g.tile * kRowTile));
+        if (d.rows > 0) todo = d;
       }
       if (w.g_end >= u1) break;
     }
+    if (tid == 0) a.w.desc[cta] = todo;
   }
   __syncthreads();
   if (tid == 0 && s.abort_flag) {
@@ -514,7 +500,7 @@ int launch_decode(const CUtensorMap& tk, const CUtensorMap& tv, const AttnArgs& 
   CRISP_KERNEL("cache_decode", stream, launch_pdl(cache_decode_kernel<kFormat, kSets>, dim3(grid), dim3(threads_of(kSets)),
                                                   smem, stream, tk, tv, a));
   CRISP_CUDA_TRY(cudaGetLastError(), "cache_attention: launch");
-  return CRISP_OK;
+  return launch_cache_join(a.w, a.out, 8 * kSets, grid, stream);
 }
 
 template <int kFormat>
@@ -528,7 +514,7 @@ int launch_format(const CUtensorMap& tk, const CUtensorMap& tv, const AttnArgs& 
 }  // namespace
 
 size_t cache_decode_ws(void* ws, size_t off) {
-  carve_decode(ws, &off);
+  carve_partials(ws, &off, kMaxCtas, kMaxRows);
   return off;
 }
 
@@ -544,7 +530,7 @@ int launch_cache_decode(const CacheView& v, int layer, const CacheBatch& b, int 
   a.q = static_cast<const __nv_bfloat16*>(q);
   a.out = Output{static_cast<__nv_bfloat16*>(o), lse, n_q_heads, a.group, b.n_tokens};
   a.status = static_cast<int*>(ws);
-  a.w = carve_decode(ws, &ws_off);
+  a.w = carve_partials(ws, &ws_off, kMaxCtas, kMaxRows);
   return v.format == CRISP_CACHE_E4M3 ? launch_format<CRISP_CACHE_E4M3>(tk, tv, a, n_sm, stream)
                                       : launch_format<CRISP_CACHE_INT8>(tk, tv, a, n_sm, stream);
 }

@@ -63,7 +63,6 @@ struct TileSmem {
   int start[kMaxCacheBatch + 1];  // units of one head before item i
   uint32_t tmem_base;
   int abort_flag;
-  int last;
 };
 
 // Pages that tile `tile` of an item (n new tokens, length len) can see; at least one, so that its rows are written.
@@ -176,13 +175,14 @@ cache_prefill_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
   }
   if (tid == 0) s.start[batch] = static_cast<int>(min(carry, 0x7fffffffLL));
   __syncthreads();
-  if (carry * heads >= 0x7fffffffLL) {  // units are counted in 32 bits
-    if (tid == 0) cache_fail(a.status, CRISP_ERR_BAD_CACHE);
+  const bool too_many = carry * heads >= 0x7fffffffLL;  // units are counted in 32 bits
+  if (too_many && tid == 0) cache_fail(a.status, CRISP_ERR_BAD_CACHE);
+  const Cut cut(too_many ? 0 : static_cast<int>(carry) * heads, gridDim.x);
+  const int cta = blockIdx.x;
+  if (cta >= cut.ctas) {
+    if (tid == 0) a.w.desc[cta].rows = 0;  // nothing to join
     return;
   }
-  const Cut cut(static_cast<int>(carry) * heads, gridDim.x);
-  const int cta = blockIdx.x;
-  if (cta >= cut.ctas) return;
   const int u0 = cut.first(cta), u1 = cut.first(cta + 1);
 
   if (warp == 8) {
@@ -204,7 +204,8 @@ cache_prefill_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
     const uint32_t o_addr = tm + lane_addr + 256 + t * 128;
     uint32_t step_count = 0;  // steps of this tile so far: phase of s_full / p_ready / o_done
     uint32_t page_count = 0;  // pages so far
-    bool ok = true;           // after a wait that gave up, the loops and barriers run on without waiting
+    bool ok = true;           // after a wait that gave up, the loops run on without waiting
+    JoinDesc todo = {0, 0, 0, 0, 0, 0};
     auto rescale_o = [&](float f) {
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
@@ -376,11 +377,11 @@ cache_prefill_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
       } else {
         page_count += static_cast<uint32_t>(g.p1 - g.p0);
       }
-      if (!whole) {
-        finish_partial<8>(cut, g, cta, a.w, a.out, it.t0, row0, rows, &s.last);
-      }
+      const JoinDesc d = join_desc(cut, g, cta, it.t0, row0, rows);
+      if (d.rows > 0) todo = d;
       u += g.p1 - g.p0;
     }
+    if (tid == 0) a.w.desc[cta] = todo;
   } else if (warp < 12) {
     reg_dealloc<kRegsMisc>();
     if (warp == 8) {
@@ -612,20 +613,6 @@ cache_prefill_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
   if (warp == 8) tmem_dealloc(tm, 512);
 }
 
-Partials carve_tiles(void* ws, size_t* off) {
-  uint8_t* base = static_cast<uint8_t*>(ws);
-  Partials w;
-  w.n_slots = 2 * kMaxTileCtas;
-  w.rows = kTileRows;
-  w.counters = reinterpret_cast<int*>(base + *off);
-  *off += align_up(sizeof(int) * 2 * w.n_slots, 256);
-  w.ml = reinterpret_cast<float2*>(base + *off);
-  *off += sizeof(float2) * w.n_slots * kTileRows;
-  w.o = reinterpret_cast<float*>(base + *off);
-  *off += sizeof(float) * static_cast<size_t>(w.n_slots) * kTileRows * kHeadDim;
-  return w;
-}
-
 template <int kFormat>
 int launch_tiles(const CUtensorMap& tk, const CUtensorMap& tv, const TileArgs& a, int n_sm, cudaStream_t stream) {
   const size_t smem = sizeof(TileSmem) + 1024;
@@ -636,13 +623,13 @@ int launch_tiles(const CUtensorMap& tk, const CUtensorMap& tv, const TileArgs& a
   CRISP_KERNEL("cache_prefill", stream, launch_pdl(cache_prefill_kernel<kFormat>, dim3(grid), dim3(kPrefillThreads), smem,
                                                    stream, tk, tv, a));
   CRISP_CUDA_TRY(cudaGetLastError(), "cache_attention: launch");
-  return CRISP_OK;
+  return launch_cache_join(a.w, a.out, kTileRows, grid, stream);
 }
 
 }  // namespace
 
 size_t cache_prefill_ws(void* ws, size_t off) {
-  carve_tiles(ws, &off);
+  carve_partials(ws, &off, kMaxTileCtas, kTileRows);
   return off;
 }
 
@@ -659,7 +646,7 @@ int launch_cache_prefill(const CacheView& v, int layer, const CacheBatch& b, int
   a.q = static_cast<const __nv_bfloat16*>(q);
   a.out = Output{static_cast<__nv_bfloat16*>(o), lse, n_q_heads, a.group, b.n_tokens};
   a.status = static_cast<int*>(ws);
-  a.w = carve_tiles(ws, &ws_off);
+  a.w = carve_partials(ws, &ws_off, kMaxTileCtas, kTileRows);
   return v.format == CRISP_CACHE_E4M3 ? launch_tiles<CRISP_CACHE_E4M3>(tk, tv, a, n_sm, stream)
                                       : launch_tiles<CRISP_CACHE_INT8>(tk, tv, a, n_sm, stream);
 }
