@@ -58,7 +58,8 @@ class CrispCache:
                                             for n in (pages_ws, attention_ws))
         for ws in (self.pages_ws, self.attention_ws):
             ws[:256].zero_()   # status words: the calls only set them
-        self._c = ctypes.byref(self.desc)
+        self._pages_ws, self._attention_ws = ((ws.data_ptr(), ws.numel()) for ws in (self.pages_ws, self.attention_ws))
+        self._c, self._lib = ctypes.byref(self.desc), B.load()
 
     @classmethod
     def allocate(cls, n_pages: int, n_kv_heads: int, max_seqs: int, max_pages: int, *, n_layers: int = 1,
@@ -75,100 +76,97 @@ class CrispCache:
 
     # ---- argument checks (host side: types, shapes and places; the device checks the contents)
     def _check(self, name, t, dtype):
-        if t.dtype != dtype or t.device != self.device or not t.is_contiguous():
+        if t.dtype is not dtype or t.device != self.device or not t.is_contiguous():
             raise ValueError(f"{name} must be a contiguous {dtype} tensor on {self.device}")
 
     def _list(self, name, t, n=None):
+        """Pointer of an int32 list (None: null)."""
         if t is None:
-            return
+            return None
         self._check(name, t, torch.int32)
         if t.dim() != 1 or (n is not None and t.shape[0] != n):
             raise ValueError(f"{name} must be one-dimensional" + ("" if n is None else f" with {n} entries"))
+        return t.data_ptr()
 
-    def _tokens(self, name, t, heads):
+    def _tokens(self, name, t, tokens, heads):
+        """Pointer of a [tokens, heads, 128] bf16 tensor."""
         self._check(name, t, torch.bfloat16)
-        if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != 128:
-            raise ValueError(f"{name} must be [tokens, {heads}, 128]")
+        if t.shape != (tokens, heads, 128):
+            raise ValueError(f"{name} must be [{tokens}, {heads}, 128]")
+        return t.data_ptr()
 
-    def _call(self, fn, stream, *args):
-        """fn(desc, *args, stream) with the cache's device current."""
+    def _call(self, name, stream, *args):
+        """The C call of that name on (cache, *args, stream), with the cache's device current.  (The answering loop calls
+        this once or more per layer and token, so the way to the library is kept short.)"""
+        index = self.device.index
         if stream is None:
-            stream = torch.cuda.current_stream(self.device)
-        if torch.cuda.current_device() == self.device.index:
-            rc = fn(self._c, *args, stream)
+            stream = torch._C._cuda_getCurrentRawStream(index)
+        elif not isinstance(stream, int):
+            stream = stream.cuda_stream
+        if torch.cuda.current_device() == index:
+            rc = getattr(self._lib, name)(self._c, *args, stream)
         else:
-            with torch.cuda.device(self.device):
-                rc = fn(self._c, *args, stream)
+            with torch.cuda.device(index):
+                rc = getattr(self._lib, name)(self._c, *args, stream)
         if rc != B.OK:
-            raise B.CrispError(rc, fn.__name__)
+            raise B.CrispError(rc, name)
 
     # ---- pages
     def reserve(self, seq_ids, n_new: Optional[torch.Tensor] = None, stream=None) -> None:
         """Adds n_new[i] (None: one) tokens to sequence seq_ids[i] and gives it the pages for them."""
-        self._list("seq_ids", seq_ids)
-        self._list("n_new", n_new, seq_ids.shape[0])
-        self._call(B.crisp_cache_reserve, stream, seq_ids, n_new, seq_ids.shape[0], self.pages_ws)
+        ids, n = self._list("seq_ids", seq_ids), seq_ids.shape[0]
+        self._call("crisp_cache_reserve", stream, ids, self._list("n_new", n_new, n), n, *self._pages_ws)
 
     def fork(self, src, dst, n_tokens: Optional[torch.Tensor] = None, share: bool = True, stream=None) -> None:
         """Makes the empty sequence dst[i] the first n_tokens[i] (None: all) tokens of src[i]."""
-        self._list("src", src)
-        self._list("dst", dst, src.shape[0])
-        self._list("n_tokens", n_tokens, src.shape[0])
-        self._call(B.crisp_cache_fork, stream, src, dst, n_tokens, src.shape[0], share, self.pages_ws)
+        n = src.shape[0]
+        self._call("crisp_cache_fork", stream, self._list("src", src), self._list("dst", dst, n),
+                   self._list("n_tokens", n_tokens, n), n, 1 if share else 0, *self._pages_ws)
 
     def free(self, seq_ids, stream=None) -> None:
         """Empties the listed sequences."""
-        self._list("seq_ids", seq_ids)
-        self._call(B.crisp_cache_free, stream, seq_ids, seq_ids.shape[0], self.pages_ws)
+        self._call("crisp_cache_free", stream, self._list("seq_ids", seq_ids), seq_ids.shape[0], *self._pages_ws)
 
     def compact(self, n_used: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         """Moves the pages in use to the front of the pool; returns how many there are (int32 [1], on the device)."""
         if n_used is None:
             n_used = self._new((1,), torch.int32, stream)
-        self._list("n_used", n_used, 1)
-        self._call(B.crisp_cache_compact, stream, n_used, self.pages_ws)
+        self._call("crisp_cache_compact", stream, self._list("n_used", n_used, 1), *self._pages_ws)
         return n_used
 
     # ---- contents
     def append(self, k, v, seq_ids, cu_tokens: Optional[torch.Tensor] = None, layer: int = 0, stream=None) -> None:
         """Writes the last tokens of the listed sequences, packed in k and v [tokens, kv_heads, 128] bf16: item i owns
         tokens cu_tokens[i] .. cu_tokens[i + 1] - 1 (None: the same number for every item)."""
-        self._tokens("k", k, self.n_kv_heads)
-        self._tokens("v", v, self.n_kv_heads)
-        if v.shape[0] != k.shape[0]:
-            raise ValueError("k and v must hold the same tokens")
-        self._list("seq_ids", seq_ids)
-        self._list("cu_tokens", cu_tokens, seq_ids.shape[0] + 1)
-        self._call(B.crisp_cache_append, stream, layer, seq_ids, cu_tokens, seq_ids.shape[0], k.shape[0], k, v,
-                   self.pages_ws)
+        n, batch = k.shape[0], seq_ids.shape[0]
+        self._call("crisp_cache_append", stream, layer, self._list("seq_ids", seq_ids),
+                   self._list("cu_tokens", cu_tokens, batch + 1), batch, n, self._tokens("k", k, n, self.n_kv_heads),
+                   self._tokens("v", v, n, self.n_kv_heads), *self._pages_ws)
 
     def attention(self, q, seq_ids, cu_tokens: Optional[torch.Tensor] = None, max_new: Optional[int] = None,
                   layer: int = 0, softmax_scale: float = 0.0, o: Optional[torch.Tensor] = None,
                   lse: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         """Causal attention of the newest tokens, q [tokens, q_heads, 128] bf16 packed as in append, over everything
-        their sequences hold.  max_new: a bound on the items' numbers of tokens (None: what the shapes allow).
+        their sequences hold.  max_new: a bound on the items' numbers of tokens (None: what the shapes allow); it picks
+        the kernel, so a server that answers token by token with cu_tokens should give it.
         lse: optional float32 [q_heads, tokens].  Returns o like q."""
         if q.dim() != 3:
             raise ValueError("q must be [tokens, q_heads, 128]")
-        n, hq = q.shape[0], q.shape[1]
-        self._tokens("q", q, hq)
-        self._list("seq_ids", seq_ids)
+        n, hq, _ = q.shape
         batch = seq_ids.shape[0]
-        self._list("cu_tokens", cu_tokens, batch + 1)
+        pq, ids, cu = self._tokens("q", q, n, hq), self._list("seq_ids", seq_ids), self._list("cu_tokens", cu_tokens, batch + 1)
         if max_new is None:
             max_new = n if cu_tokens is not None or batch == 0 else n // batch
-        if o is None:
-            o = self._new(q.shape, torch.bfloat16, stream)
-        else:
-            self._tokens("o", o, hq)
-            if o.shape[0] != n:
-                raise ValueError("o must have the shape of q")
+        plse = None
         if lse is not None:
             self._check("lse", lse, torch.float32)
-            if tuple(lse.shape) != (hq, n):
+            if lse.shape != (hq, n):
                 raise ValueError(f"lse must be [{hq}, {n}]")
-        self._call(B.crisp_cache_attention, stream, layer, seq_ids, cu_tokens, batch, n, max_new, hq, softmax_scale, q,
-                   o, lse, self.attention_ws)
+            plse = lse.data_ptr()
+        if o is None:
+            o = self._new(q.shape, torch.bfloat16, stream)
+        self._call("crisp_cache_attention", stream, layer, ids, cu, batch, n, max_new, hq, softmax_scale, pq,
+                   self._tokens("o", o, n, hq), plse, *self._attention_ws)
         return o
 
     def _new(self, shape, dtype, stream):

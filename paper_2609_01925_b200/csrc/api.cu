@@ -1,5 +1,6 @@
 // C-ABI entry points: argument validation, workspace sizing, status handling.  Every step of the
 // path runs in the CUDA kernels of route.cu / select.cu / prefill.cu; nothing here computes.
+#include <atomic>
 #include <cmath>
 #include <cstdio>
 #include <cstring>
@@ -173,6 +174,18 @@ int validate(const crisp_params* p, Dims* d, bool dense_only) {
 }
 
 static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+int current_sm_count(int* n_sm) {
+  static std::atomic<int> known[64];
+  int dev = 0;
+  CRISP_CUDA_TRY(cudaGetDevice(&dev), "device");
+  const bool keep = dev >= 0 && dev < 64;
+  *n_sm = keep ? known[dev].load(std::memory_order_relaxed) : 0;
+  if (*n_sm > 0) return CRISP_OK;
+  CRISP_CUDA_TRY(cudaDeviceGetAttribute(n_sm, cudaDevAttrMultiProcessorCount, dev), "SM count");
+  if (keep) known[dev].store(*n_sm, std::memory_order_relaxed);
+  return CRISP_OK;
+}
 
 // ---- the 8-bit cache: host-side checks (what lives on the device is checked by the kernels)
 int check_cache(const crisp_cache* c, CacheView* v) {
@@ -806,9 +819,9 @@ int crisp_cache_attention(const crisp_cache* c, int32_t layer, const int32_t* se
   if (!aligned16(ws) || ws_bytes < attention_ws_bytes()) return CRISP_ERR_WORKSPACE;
   const float scale = softmax_scale > 0.f ? softmax_scale : 1.0f / std::sqrt(static_cast<float>(kHeadDim));
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  int dev = 0, n_sm = 0;
-  CRISP_CUDA_TRY(cudaGetDevice(&dev), "cache_attention: device");
-  CRISP_CUDA_TRY(cudaDeviceGetAttribute(&n_sm, cudaDevAttrMultiProcessorCount, dev), "cache_attention: SM count");
+  int n_sm = 0;
+  rc = current_sm_count(&n_sm);
+  if (rc != CRISP_OK) return rc;
   const size_t decode_off = kWsHeader, prefill_off = cache_decode_ws(nullptr, decode_off);
   // Up to 16 rows per KV head (new tokens x query heads of its group) are two fragments of the kernel that reads the
   // cache at HBM speed; more rows would make it read the cache again.

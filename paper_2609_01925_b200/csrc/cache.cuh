@@ -28,6 +28,9 @@ struct CacheBatch {
   int batch, n_tokens, per, max_new;
 };
 
+// Multiprocessors of the current device (asked once per device).
+int current_sm_count(int* n_sm);
+
 int check_cache(const crisp_cache* c, CacheView* v);
 int check_batch(const int32_t* seq_ids, const int32_t* cu, int32_t batch, int32_t n_tokens,
                 int32_t max_new, CacheBatch* b);

@@ -561,14 +561,6 @@ cache_compact_kernel(const CacheView c, int32_t* n_used, PagesWs w) {
   }
 }
 
-int move_grid(int* grid) {
-  int dev = 0, n_sm = 0;
-  CRISP_CUDA_TRY(cudaGetDevice(&dev), "cache: device");
-  CRISP_CUDA_TRY(cudaDeviceGetAttribute(&n_sm, cudaDevAttrMultiProcessorCount, dev), "cache: SM count");
-  *grid = 8 * n_sm;
-  return CRISP_OK;
-}
-
 }  // namespace
 
 size_t cache_pages_ws_bytes(const CacheView& v) {
@@ -610,9 +602,10 @@ int launch_cache_fork(const CacheView& v, const int32_t* src, const int32_t* dst
                       int share, void* ws, cudaStream_t stream) {
   size_t total;
   const PagesWs w = carve(v, ws, &total);
-  int grid = 0;
-  const int rc = move_grid(&grid);
+  int n_sm = 0;
+  const int rc = current_sm_count(&n_sm);
   if (rc != CRISP_OK) return rc;
+  const int grid = 8 * n_sm;
   CRISP_KERNEL("cache_fork", stream, launch_pdl(cache_fork_kernel, dim3(1), dim3(kPlanThreads), 0, stream, v, src, dst,
                                                 n_tokens, count, share, w));
   CRISP_KERNEL("cache_move", stream, launch_pdl(cache_move_kernel, dim3(grid), dim3(kMoveThreads), 0, stream, v, w, 0));
@@ -630,9 +623,10 @@ int launch_cache_free(const CacheView& v, const int32_t* seq_ids, int count, voi
 int launch_cache_compact(const CacheView& v, int32_t* n_used, void* ws, cudaStream_t stream) {
   size_t total;
   const PagesWs w = carve(v, ws, &total);
-  int grid = 0;
-  const int rc = move_grid(&grid);
+  int n_sm = 0;
+  const int rc = current_sm_count(&n_sm);
   if (rc != CRISP_OK) return rc;
+  const int grid = 8 * n_sm;
   CRISP_KERNEL("cache_compact", stream, launch_pdl(cache_compact_kernel, dim3(1), dim3(kPlanThreads), 0, stream, v, n_used, w));
   CRISP_KERNEL("cache_move", stream, launch_pdl(cache_move_kernel, dim3(grid), dim3(kMoveThreads), 0, stream, v, w, 1));
   CRISP_CUDA_TRY(cudaGetLastError(), "cache_compact: launch");
