@@ -31,6 +31,7 @@ constexpr int kConv = 6;           // ring of converted halves (16 KB)
 constexpr int kInfo = 16;          // words per load or page under way; more than there can be
 constexpr int kIsK = -0x40000000;  // marks a load of K where V's has the number of its tokens that exist
 constexpr int kTileRows = 256;     // rows of a group of work
+constexpr int kGroupUnits = 4;     // what beginning and ending a group costs, in pages
 constexpr int kMaxTileCtas = 160;  // bound on the grid; sizes the workspace
 constexpr int kPrefillThreads = 512;
 constexpr float kNothing = -1e30f;  // running maximum of a row that has seen nothing
@@ -75,54 +76,82 @@ __device__ __forceinline__ int tiles_of(int n, int tile_tokens) { return (n + ti
 // Units of one head of an item, summed by a whole warp (at most 2^31 - 1: the caller refuses that many).
 __device__ __forceinline__ int item_units(int len, int n, int tile_tokens, int lane) {
   long long sum = 0;
-  for (int t = lane; t < tiles_of(n, tile_tokens); t += 32) sum += tile_pages(len, n, t, tile_tokens);
+  for (int t = lane; t < tiles_of(n, tile_tokens); t += 32) sum += tile_pages(len, n, t, tile_tokens) + kGroupUnits;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
   return static_cast<int>(min(sum, 0x7fffffffLL));
 }
 
-// The segment that begins at unit u, found by a whole warp; *it receives its item.
-__device__ __forceinline__ Segment tile_segment(const TileSmem& s, const TileArgs& a, int u, int end, int lane,
-                                                CacheItem* it) {
+// Walks the groups of a CTA's run in order.  A group is kGroupUnits units without work, then its pages.
+struct TileWalk {
   Segment g;
-  int lo = 0, hi = a.b.batch;
-  const int key = u / a.c.heads;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (s.start[mid] <= key) lo = mid; else hi = mid;
+  CacheItem it;
+  int tiles;  // of the item
+  int rows;   // of the group: up to 256
+  int g_end;  // unit behind the group
+
+  __device__ __forceinline__ void load(const TileArgs& a) {
+    it = load_item(a.c, a.b, g.item, a.status);
+    tiles = tiles_of(it.n, a.tile_tokens);
   }
-  g.item = lo;
-  *it = load_item(a.c, a.b, lo, a.status);
-  const int per_head = s.start[lo + 1] - s.start[lo];
-  int rem = u - s.start[lo] * a.c.heads;
-  g.head = rem / per_head;
-  rem -= g.head * per_head;
-  const int tiles = tiles_of(it->n, a.tile_tokens);
-  g.tile = 0;
-  g.pages = 1;
-  for (int t0 = 0; t0 < tiles; t0 += 32) {
-    const int mine = t0 + lane < tiles ? tile_pages(it->len, it->n, t0 + lane, a.tile_tokens) : 0;
-    int incl = mine;
+  __device__ __forceinline__ void place(const TileArgs& a, int first_unit) {
+    g.pages = tile_pages(it.len, it.n, g.tile, a.tile_tokens);
+    rows = min(a.tile_tokens, it.n - g.tile * a.tile_tokens) * a.group;
+    g.g0 = first_unit + kGroupUnits;
+    g_end = g.g0 + g.pages;
+  }
+  // the group that holds unit u; a whole warp searches
+  __device__ __forceinline__ void seek(const int* start, const TileArgs& a, int u, int lane) {
+    int lo = 0, hi = a.b.batch;
+    const int key = u / a.c.heads;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (start[mid] <= key) lo = mid; else hi = mid;
+    }
+    g.item = lo;
+    load(a);
+    const int per_head = start[lo + 1] - start[lo];
+    int rem = u - start[lo] * a.c.heads;
+    g.head = rem / per_head;
+    rem -= g.head * per_head;
+    g.tile = 0;
+    for (int t0 = 0; t0 < tiles; t0 += 32) {
+      int incl = t0 + lane < tiles ? tile_pages(it.len, it.n, t0 + lane, a.tile_tokens) + kGroupUnits : 0;
+      const int mine = incl;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int x = __shfl_up_sync(0xffffffffu, incl, o);
-      if (lane >= o) incl += x;
+      for (int o = 1; o < 32; o <<= 1) {
+        const int x = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += x;
+      }
+      const uint32_t past = __ballot_sync(0xffffffffu, incl > rem);
+      if (past) {
+        const int src = __ffs(past) - 1;
+        g.tile = t0 + src;
+        rem -= __shfl_sync(0xffffffffu, incl - mine, src);
+        break;
+      }
+      rem -= __shfl_sync(0xffffffffu, incl, 31);
     }
-    const uint32_t past = __ballot_sync(0xffffffffu, incl > rem);
-    if (past) {
-      const int src = __ffs(past) - 1;
-      g.tile = t0 + src;
-      g.pages = __shfl_sync(0xffffffffu, mine, src);
-      rem -= __shfl_sync(0xffffffffu, incl, src) - g.pages;
-      break;
-    }
-    rem -= __shfl_sync(0xffffffffu, incl, 31);
+    place(a, u - rem);
   }
-  g.p0 = rem;
-  g.g0 = u - rem;
-  g.p1 = min(g.pages, g.p0 + end - u);
-  return g;
-}
+  __device__ __forceinline__ void next(const int* start, const TileArgs& a) {
+    if (++g.tile == tiles) {
+      g.tile = 0;
+      if (++g.head == a.c.heads) {
+        g.head = 0;
+        do ++g.item; while (start[g.item + 1] == start[g.item]);  // items without work
+        load(a);
+      }
+    }
+    place(a, g_end);
+  }
+  // the part of the group within units [u0, u1); false when none of its pages is
+  __device__ __forceinline__ bool clip(int u0, int u1) {
+    g.p0 = max(u0 - g.g0, 0);
+    g.p1 = min(u1 - g.g0, g.pages);
+    return g.p0 < g.p1;
+  }
+};
 
 __host__ __device__ constexpr uint32_t umma_idesc_f16(int M, int N) {
   return (1u << 4) | (static_cast<uint32_t>(N >> 3) << 17) | (static_cast<uint32_t>(M >> 4) << 24);  // f16 x f16 -> f32
@@ -194,6 +223,7 @@ cache_prefill_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
   tc_fence_after_sync();
   const uint32_t tm = s.tmem_base;
   volatile int* abort_flag = &s.abort_flag;
+  TileWalk w;
 
   if (warp < 8) {
     // =============================================================== softmax / epilogue, one row per thread
@@ -217,11 +247,15 @@ cache_prefill_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
         tmem_st_x32(o_addr + c * 32, ov);
       }
     };
-    for (int u = u0; u < u1;) {
-      CacheItem it;
-      const Segment g = tile_segment(s, a, u, u1, lane, &it);
+    for (w.seek(s.start, a, u0, lane);; w.next(s.start, a)) {
+      if (!w.clip(u0, u1)) {
+        if (w.g_end >= u1) break;
+        continue;
+      }
+      const Segment& g = w.g;
+      const CacheItem& it = w.it;
       const int row0 = g.tile * a.tile_tokens * a.group;               // first row of the pair of tiles
-      const int rows = min(a.tile_tokens, it.n - g.tile * a.tile_tokens) * a.group;
+      const int rows = w.rows;
       const int my_row = t * 128 + r;
       const bool active = t * 128 < rows;                               // the tile has rows
       const bool whole = g.p0 == 0 && g.p1 == g.pages;
@@ -379,7 +413,7 @@ cache_prefill_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
       }
       const JoinDesc d = join_desc(cut, g, cta, it.t0, row0, rows);
       if (d.rows > 0) todo = d;
-      u += g.p1 - g.p0;
+      if (w.g_end >= u1) break;
     }
     if (tid == 0) a.w.desc[cta] = todo;
   } else if (warp < 12) {
@@ -398,9 +432,13 @@ cache_prefill_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
         tma_load_2d(s.raw[slot], map, &s.raw_full[slot], 0, block * kPage + half * kHalf);
         ++load;
       };
-      for (int u = u0; u < u1;) {
-        CacheItem it;
-        const Segment g = tile_segment(s, a, u, u1, lane, &it);
+      for (w.seek(s.start, a, u0, lane);; w.next(s.start, a)) {
+        if (!w.clip(u0, u1)) {
+          if (w.g_end >= u1) break;
+          continue;
+        }
+        const Segment& g = w.g;
+        const CacheItem& it = w.it;
         const int* row = a.c.page_table + static_cast<size_t>(it.seq) * a.c.max_pages;
         int block = 0, block_next = 0;  // of pages p and p + 1
         float vs = 0.f, vs_next = 0.f;
@@ -442,7 +480,7 @@ cache_prefill_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
           block = block_next;
           vs = vs_next;
         }
-        u += g.p1 - g.p0;
+        if (w.g_end >= u1) break;
       }
       if (lane == 0 && !ok) {
         // given up: the copies in flight still write to this CTA's shared memory, so see them in (bounded)
@@ -509,11 +547,13 @@ cache_prefill_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
         umma_commit(&s.conv_empty[slot]);
         next_load();
       };
-      for (int u = u0; u < u1;) {
-        CacheItem it;
-        const Segment g = tile_segment(s, a, u, u1, lane, &it);
-        const int rows = min(a.tile_tokens, it.n - g.tile * a.tile_tokens) * a.group;
-        const int n = g.p1 - g.p0;
+      for (w.seek(s.start, a, u0, lane);; w.next(s.start, a)) {
+        if (!w.clip(u0, u1)) {
+          if (w.g_end >= u1) break;
+          continue;
+        }
+        const int rows = w.rows;
+        const int n = w.g.p1 - w.g.p0;
         if (lane == 0) {
           if (t * 128 >= rows) {
             // a tile without rows: see the loads through
@@ -543,7 +583,7 @@ cache_prefill_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
           }
         }
         __syncwarp();
-        u += n;
+        if (w.g_end >= u1) break;
       }
     }
   } else {
@@ -552,7 +592,11 @@ cache_prefill_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
     reg_dealloc<kRegsConv>();
     const int ct = tid & 63, chunk = ct & 7, row_of = ct >> 3;  // eight threads per token, 16 codes each
     const uint32_t pair = (tid >> 6) & 1;
-    const uint32_t n_loads = 4u * static_cast<uint32_t>(u1 - u0);
+    uint32_t n_loads = 0;  // four per page
+    for (w.seek(s.start, a, u0, lane);; w.next(s.start, a)) {
+      if (w.clip(u0, u1)) n_loads += 4u * static_cast<uint32_t>(w.g.p1 - w.g.p0);
+      if (w.g_end >= u1) break;
+    }
     // A thread's 16 codes become two 16-byte chunks of a 64-dim half; which of the two comes first depends on the half
     // and on the token's parity, so that the threads of a phase touch different banks in the loads (8 bytes) and in the
     // stores (16 bytes).  (A thread's tokens are row_of + 8 j: the swizzle is the same for all of them.)
