@@ -56,7 +56,6 @@ struct TileSmem {
   alignas(1024) uint8_t conv[kConv][2][8192];  // [slot][64-dim half]
   alignas(1024) uint8_t raw[kRaw][kPageTileBytes / 2];
   uint64_t raw_full[kRaw], raw_empty[kRaw], conv_full[kConv], conv_empty[kConv];
-  uint64_t in_exp[4];  // per scheduler: odd phase while tile 1's warp is in the first part of its exponentials
   uint64_t q_full[2], s_full[2][2], p_ready[2][2], o_done[2][2];
   float load_scale[kInfo], page_scale[kInfo];  // V's scale by load, K's by page
   int load_rows[kInfo];
@@ -175,7 +174,6 @@ cache_prefill_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
       mbar_init(&s.conv_full[i], 2);
       mbar_init(&s.conv_empty[i], 2);  // one arrival per issuer, whether or not its tile has rows
     }
-    for (int i = 0; i < 4; ++i) mbar_init(&s.in_exp[i], 1);
     for (int t = 0; t < 2; ++t) {
       mbar_init(&s.q_full[t], 128);
       for (int h = 0; h < 2; ++h) {
@@ -296,30 +294,7 @@ cache_prefill_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
         const int last_key = min(it.len - it.n + g.tile * a.tile_tokens + my_row / a.group, it.len - 1);
         const int all_see = it.len - it.n + g.tile * a.tile_tokens + (my_row - lane) / a.group;
         float m_used = kNothing, l_run = 0.f;
-        // Pacing (see prefill.cu): the warps of the two tiles that share a scheduler take turns in their runs of
-        // exponentials.  A hint, never needed for progress: the wait gives up after 2 us.
-        uint64_t* in_exp = &s.in_exp[warp & 3];
-        auto pace_enter = [&](float& pin) {
-          if (t == 0) {
-            if (!mbar_try_wait(in_exp, 1)) {
-              const unsigned long long t0 = global_timer_ns();
-              while (!mbar_try_wait(in_exp, 1) && global_timer_ns() - t0 < 2000ull) {
-              }
-            }
-            __syncwarp();
-            asm volatile("" : "+f"(pin)::"memory");  // keeps the exponentials behind the wait
-          }
-          if (t == 1) {
-            if (lane == 0) mbar_arrive(in_exp);
-          }
-        };
-        auto pace_release = [&](uint32_t& pin) {
-          if (t == 1) {
-            asm volatile("" : "+r"(pin)::"memory");
-            __syncwarp();
-            if (lane == 0) mbar_arrive(in_exp);
-          }
-        };
+        auto no_pacing = [](uint32_t&) {};
         float scale = 0.f;
         // one step of the online softmax per half page; both halves run the same code (two copies of it, beside the
         // converters', do not fit the instruction caches: a third of all stalls were fetches)
@@ -355,9 +330,8 @@ cache_prefill_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
             m_used = m_new;
           }
           uint32_t pk[2][16];
-          pace_enter(m_used);
-          l_run += masked ? exp_pack<true>(x, lim, 0, scale, m_used, pk, pace_release)
-                          : exp_pack<false>(x, lim, 0, scale, m_used, pk, pace_release);
+          l_run += masked ? exp_pack<true>(x, lim, 0, scale, m_used, pk, no_pacing)
+                          : exp_pack<false>(x, lim, 0, scale, m_used, pk, no_pacing);
           asm volatile("" : "+f"(l_run)::"memory");  // the run of exponentials ends here
           tmem_st_x16(half_addr, pk[0]);       // P over the columns of its own S, which this warp has read
           tmem_st_x16(half_addr + 16, pk[1]);
@@ -565,20 +539,18 @@ cache_prefill_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
           } else {
             ok = ok && mbar_wait(&s.q_full[t], q_count & 1, abort_flag);
             ++q_count;
-            if (ok) mma_qk(0);
-            if (ok) mma_qk(1);
-            // two bursts per step: P_A V_A then the next Q K_A^T, P_B V_B then the next Q K_B^T (see prefill.cu)
-            for (int j = 0; j < n && ok; ++j) {
-              const bool more = j + 1 < n;
-              ok = mbar_wait(&s.p_ready[t][0], p_count & 1, abort_flag);
-              if (!ok) break;
-              mma_pv(0, j == 0);
-              if (more && ok) mma_qk(0);
-              ok = ok && mbar_wait(&s.p_ready[t][1], p_count & 1, abort_flag);
-              if (!ok) break;
-              ++p_count;
-              mma_pv(1, false);
-              if (more && ok) mma_qk(1);
+            // half-step i is P_h V_h and the next page's Q K_h^T, h = i mod 2 (see prefill.cu); the first two are Q K^T
+            // alone.  (One copy of the code: the roles share the instruction caches.)
+#pragma unroll 1
+            for (int i = -2; i < 2 * n && ok; ++i) {
+              const int h = i & 1;
+              if (i >= 0) {
+                ok = mbar_wait(&s.p_ready[t][h], p_count & 1, abort_flag);
+                if (!ok) break;
+                mma_pv(h, i == 0);
+                p_count += h;
+              }
+              if (i + 2 < 2 * n && ok) mma_qk(h);
             }
           }
         }
@@ -615,8 +587,10 @@ cache_prefill_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
       const int exist = *reinterpret_cast<volatile int*>(&s.load_rows[load % kInfo]);
       const uint8_t* src = s.raw[raw];
       uint8_t* dst = s.conv[conv][0];
+      // (short loops on purpose: unrolled eight and four times they made the kernel 27 % slower, because the roles' code no
+      // longer fits the instruction caches)
       if (exist == kIsK) {
-#pragma unroll 4
+#pragma unroll 2
         for (int j = 0; j < 8; ++j) {
           const uint2 a8 = *reinterpret_cast<const uint2*>(src + src_a + j * 1024);
           const uint2 b8 = *reinterpret_cast<const uint2*>(src + src_b + j * 1024);
@@ -629,7 +603,7 @@ cache_prefill_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
           *reinterpret_cast<uint4*>(dst + dst_b + j * 1024) = make_uint4(h[4], h[5], h[6], h[7]);
         }
       } else {
-#pragma unroll 2
+#pragma unroll 1
         for (int j = 0; j < 8; ++j) {
           uint2 a8 = *reinterpret_cast<const uint2*>(src + src_a + j * 1024);
           uint2 b8 = *reinterpret_cast<const uint2*>(src + src_b + j * 1024);
