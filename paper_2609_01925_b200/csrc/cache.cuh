@@ -6,8 +6,7 @@ namespace crisp {
 
 constexpr int kPage = kBlock;              // tokens of a page = the block of the sparse path
 constexpr int kPageTileBytes = kPage * kHeadDim;  // codes of one page and KV head, K or V: 16 KB
-constexpr int kMaxSets = 3;                // sets of eight rows of the kernel for few rows
-constexpr int kDecodeRows = 8 * kMaxSets;  // most rows per KV head that it takes
+constexpr int kDecodeRows = 24;  // most rows per KV head for the kernel for few rows
 constexpr int kMaxCacheBatch = CRISP_CACHE_MAX_BATCH;
 
 // A crisp_cache passed to kernels by value.

@@ -27,17 +27,18 @@ using namespace sm100;
 
 namespace {
 
-constexpr int kSetWarps = 4;         // warps that share a page: 32 tokens each
+constexpr int kWarps = 4;            // consumer warps, which share a page: 32 tokens each
+constexpr int kThreads = kWarps * 32 + 32;
 constexpr int kMaxCtas = 512;        // bound on the grid; sizes the workspace
-constexpr int kMaxRows = 8 * kMaxSets;  // rows of a partial result
+constexpr int kMaxRows = kDecodeRows;  // rows of a partial result
 constexpr int kGroupUnits = 1;       // what beginning and ending a group costs, in pages
 
-// Sets of warps: every set reads all pages of the CTA and computes eight rows.  With one set three CTAs share an SM, and a
-// ring of one K and one V tile each is enough: 96 KB under way per SM (three slots: 2 us more on 82 MB spread over 32
-// sequences; two CTAs with five slots: 4 % less bandwidth on long sequences).
-__host__ __device__ constexpr int ctas_per_sm(int sets) { return sets == 1 ? 3 : 1; }
-__host__ __device__ constexpr int slots_of(int sets) { return sets == 1 ? 2 : 4; }  // ring slots of one K or V tile
-__host__ __device__ constexpr int threads_of(int sets) { return sets * kSetWarps * 32 + 32; }
+// Rows come in tiles of eight; a CTA computes kTiles of them at once, which share the loads and conversions of a page.
+// One tile: three CTAs share an SM, and a ring of one K and one V slot each is enough: 96 KB under way per SM (three slots:
+// 2 us more on 82 MB spread over 32 sequences; two CTAs with five slots: 4 % less bandwidth on long sequences).  Two or
+// three tiles need 168 registers: two CTAs.
+__host__ __device__ constexpr int ctas_per_sm(int tiles) { return tiles == 1 ? 3 : 2; }
+__host__ __device__ constexpr int slots_of(int tiles) { return tiles == 1 ? 2 : 4; }
 
 struct AttnArgs {
   CacheView c;
@@ -50,14 +51,16 @@ struct AttnArgs {
   int* status;
 };
 
-template <int kSets>
+template <int kTiles>
 struct DecodeSmem {
-  alignas(1024) uint8_t ring[slots_of(kSets)][kPageTileBytes];
-  float4 red[kSets][kSetWarps][8][kHeadDim / 4];  // the warps' O of eight rows
-  alignas(16) uint8_t q[2][8 * kSets][kHeadDim * 2];
-  float red_m[kSets][kSetWarps][8], red_l[kSets][kSetWarps][8];
-  float scale[slots_of(kSets)];
-  uint64_t full[slots_of(kSets)], empty[slots_of(kSets)], q_full[2], q_empty[2];
+  alignas(1024) uint8_t ring[slots_of(kTiles)][kPageTileBytes];
+  float4 red[kWarps][8][kHeadDim / 4];      // the warps' O of eight rows
+  alignas(16) uint8_t q[2][8 * kTiles][kHeadDim * 2];
+  uint2 q_frag[kTiles][8][32];              // Q as fp16 fragments: [tile][K step][lane]
+  float2 col_scale[kTiles][4];              // logit scales of rows 2 t, 2 t + 1
+  float red_m[kWarps][8], red_l[kWarps][8];
+  float scale[slots_of(kTiles)];
+  uint64_t full[slots_of(kTiles)], empty[slots_of(kTiles)], q_full[2], q_empty[2];
   long long scratch[33];
   int abort_flag;
   int start[kMaxCacheBatch + 1];   // units of one head before item i
@@ -127,13 +130,13 @@ struct Walk {
   }
 };
 
-template <int kFormat, int kSets>
-__global__ void __launch_bounds__(threads_of(kSets), ctas_per_sm(kSets))
+template <int kFormat, int kTiles>
+__global__ void __launch_bounds__(kThreads, ctas_per_sm(kTiles))
 cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const AttnArgs a) {
-  constexpr int kRowTile = 8 * kSets, kSlots = slots_of(kSets), kWarps = kSets * kSetWarps, kThreads = threads_of(kSets);
+  constexpr int kRowTile = 8 * kTiles, kSlots = slots_of(kTiles);
   pdl_enter();
   extern __shared__ uint8_t smem_raw[];
-  auto& s = *reinterpret_cast<DecodeSmem<kSets>*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  auto& s = *reinterpret_cast<DecodeSmem<kTiles>*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int heads = a.c.heads, batch = a.b.batch;
   if (tid == 0) {
@@ -247,7 +250,6 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
     __syncwarp();
   } else {
     // =============================================================== consumers
-    const int set = warp / kSetWarps, sw = warp % kSetWarps;  // the set's rows 8 set .., the warp's tokens 32 sw ..
     const int gid = lane >> 2, t = lane & 3;
     const int perm = (gid >> 1) | ((gid & 1) << 2);  // token of fragment row gid for K, chunk of fragment row gid for V
     uint32_t slot = 0, phase = 0, segs = 0;
@@ -263,93 +265,97 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
       if (w.clip(u0, u1)) {
         const Segment& g = w.g;
         const CacheItem& it = w.it;
-        const int first_row = g.tile * kRowTile + 8 * set;
-        // ---- Q fragments: row gid, dims 16 t .. and 64 + 16 t ..
-        uint32_t qf[8][2];
-        float col_scale[2];
-        int col_last[2];  // last position that the column's row may see
+        const int first_row = g.tile * kRowTile;
+        // ---- Q fragments, one tile per warp: row gid, dims 16 t .. and 64 + 16 t ..
         {
           const int qb = segs & 1;
           ok = ok && mbar_wait_warp(&s.q_full[qb], (segs >> 1) & 1, abort_flag);
-          uint4 x[4];
-          const uint4* p = reinterpret_cast<const uint4*>(s.q[qb][8 * set + gid]);
-          const bool have = first_row + gid < w.rows;
+          if (warp < kTiles) {
+            uint4 x[4];
+            const uint4* p = reinterpret_cast<const uint4*>(s.q[qb][8 * warp + gid]);
+            const bool have = first_row + 8 * warp + gid < w.rows;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) x[i] = have ? p[(i & 1) + 2 * t + 8 * (i >> 1)] : make_uint4(0, 0, 0, 0);
-          __syncwarp();
+            for (int i = 0; i < 4; ++i) x[i] = have ? p[(i & 1) + 2 * t + 8 * (i >> 1)] : make_uint4(0, 0, 0, 0);
+            uint32_t amax = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const uint32_t wd[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+#pragma unroll
+              for (int k = 0; k < 4; ++k) amax = __vmaxu2(amax, wd[k] & 0x7fff7fffu);
+            }
+            amax = __vmaxu2(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
+            amax = __vmaxu2(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
+            amax = max(amax & 0xffffu, amax >> 16);
+            const int ex = static_cast<int>(amax >> 7);  // 255: the row holds an infinity or NaN and stays one
+            const int e = ex == 255 ? 0 : min(141 - ex, 126);  // the row's largest element lands in [2^14, 2^15)
+            const float f = pow2i(e);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const uint32_t wd[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+#pragma unroll
+              for (int k = 0; k < 4; k += 2)
+                // chunk i / 2, elements 8 (i % 2) + 2 k: K step 4 (i / 2) + 2 (i % 2) + k / 2
+                s.q_frag[warp][4 * (i >> 1) + 2 * (i & 1) + (k >> 1)][lane] = make_uint2(
+                    half2_bits(__uint_as_float(wd[k] << 16) * f, __uint_as_float(wd[k] & 0xffff0000u) * f),
+                    half2_bits(__uint_as_float(wd[k + 1] << 16) * f, __uint_as_float(wd[k + 1] & 0xffff0000u) * f));
+            }
+            if (t == 0) reinterpret_cast<float*>(s.col_scale[warp])[gid] = a.scale_log2 * pow2i(-e);
+          }
+          named_bar_sync(1, kWarps * 32);
           if (lane == 0) mbar_arrive(&s.q_empty[qb]);
           ++segs;
-          uint32_t amax = 0;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const uint32_t wd[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-#pragma unroll
-            for (int k = 0; k < 4; ++k) amax = __vmaxu2(amax, wd[k] & 0x7fff7fffu);
-          }
-          amax = __vmaxu2(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
-          amax = __vmaxu2(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
-          amax = max(amax & 0xffffu, amax >> 16);
-          const int ex = static_cast<int>(amax >> 7);  // 255: the row holds an infinity or NaN and stays one
-          const int e = ex == 255 ? 0 : min(141 - ex, 126);  // the row's largest element lands in [2^14, 2^15)
-          const float f = pow2i(e);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const uint32_t wd[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-              // chunk i / 2, elements 8 (i % 2) + 2 k: K step 4 (i / 2) + 2 (i % 2) + k / 2, pair k % 2
-              qf[4 * (i >> 1) + 2 * (i & 1) + (k >> 1)][k & 1] =
-                  half2_bits(__uint_as_float(wd[k] << 16) * f, __uint_as_float(wd[k] & 0xffff0000u) * f);
-          }
-          const float back = a.scale_log2 * pow2i(-e);
-#pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            col_scale[k] = __shfl_sync(0xffffffffu, back, (2 * t + k) * 4);
-            col_last[k] = it.len - it.n + (first_row + 2 * t + k) / a.group;
-          }
         }
-        const int all_see = it.len - it.n + first_row / a.group;  // every row of the set sees the keys up to here
+        const int all_see = it.len - it.n + first_row / a.group;  // every row sees the keys up to here
 
-        float o[8][4];
-        float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+        float o[kTiles][8][4];
+        float m[kTiles][2], l[kTiles][2];
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
+        for (int nt = 0; nt < kTiles; ++nt) {
+          m[nt][0] = m[nt][1] = -INFINITY;
+          l[nt][0] = l[nt][1] = 0.f;
 #pragma unroll
-          for (int k = 0; k < 4; ++k) o[j][k] = 0.f;
+          for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) o[nt][j][k] = 0.f;
+        }
 
 #pragma unroll 1
         for (int p = g.p0; p < g.p1; ++p) {
-          const int tok0 = sw * 32;              // the warp's tokens in the page
+          const int tok0 = warp * 32;            // the warp's tokens in the page
           const int pos0 = p * kPage + tok0;     // and their first position
           // ---- S^T = K Q^T: two tiles of 16 tokens
-          float x[2][4];
+          float x[kTiles][2][4];
 #pragma unroll
-          for (int mt = 0; mt < 2; ++mt)
+          for (int nt = 0; nt < kTiles; ++nt)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) x[mt][k] = 0.f;
+            for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+              for (int k = 0; k < 4; ++k) x[nt][mt][k] = 0.f;
           ok = ok && mbar_wait_warp(&s.full[slot], phase, abort_flag);
           const float ks = s.scale[slot];
 #pragma unroll
-          for (int mt = 0; mt < 2; ++mt) {
-            const int tok = tok0 + 16 * mt + perm;   // rows gid and gid + 8: tokens tok and tok + 8 (same swizzle)
-            const uint8_t* base = s.ring[slot] + tok * kHeadDim;
-            uint4 kw[2][2];  // [row half][chunk t, t + 4]
+          for (int ch = 0; ch < 2; ++ch) {
+            uint4 kw[2][2];  // [tile of tokens][row half]: rows gid and gid + 8 are tokens perm and perm + 8 (same swizzle)
 #pragma unroll
-            for (int ch = 0; ch < 2; ++ch) {
-              const int off = ((t + 4 * ch) ^ (tok & 7)) << 4;
-              kw[0][ch] = *reinterpret_cast<const uint4*>(base + off);
-              kw[1][ch] = *reinterpret_cast<const uint4*>(base + 8 * kHeadDim + off);
+            for (int mt = 0; mt < 2; ++mt) {
+              const int tok = tok0 + 16 * mt + perm;
+              const uint8_t* base = s.ring[slot] + tok * kHeadDim + (((t + 4 * ch) ^ (tok & 7)) << 4);
+              kw[mt][0] = *reinterpret_cast<const uint4*>(base);
+              kw[mt][1] = *reinterpret_cast<const uint4*>(base + 8 * kHeadDim);
             }
 #pragma unroll
-            for (int ch = 0; ch < 2; ++ch) {
-              const uint32_t up[4] = {kw[0][ch].x, kw[0][ch].y, kw[0][ch].z, kw[0][ch].w};
-              const uint32_t dn[4] = {kw[1][ch].x, kw[1][ch].y, kw[1][ch].z, kw[1][ch].w};
+            for (int k = 0; k < 4; ++k) {
+              uint2 qf[kTiles];
 #pragma unroll
-              for (int k = 0; k < 4; ++k) {
+              for (int nt = 0; nt < kTiles; ++nt) qf[nt] = s.q_frag[nt][4 * ch + k][lane];
+#pragma unroll
+              for (int mt = 0; mt < 2; ++mt) {
+                auto word = [&](const uint4& v) { return k == 0 ? v.x : k == 1 ? v.y : k == 2 ? v.z : v.w; };
                 uint32_t f[4];
-                decode4<kFormat>(up[k], f[0], f[2]);
-                decode4<kFormat>(dn[k], f[1], f[3]);
-                mma_f16(x[mt], f, qf[4 * ch + k][0], qf[4 * ch + k][1]);
+                decode4<kFormat>(word(kw[mt][0]), f[0], f[2]);
+                decode4<kFormat>(word(kw[mt][1]), f[1], f[3]);
+#pragma unroll
+                for (int nt = 0; nt < kTiles; ++nt) mma_f16(x[nt][mt], f, qf[nt].x, qf[nt].y);
               }
             }
           }
@@ -358,45 +364,52 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
           next_slot();
           // ---- online softmax of the columns (the query rows) over the warp's 32 tokens
           const bool masked = pos0 + 31 > all_see;
-          uint32_t pf[2][2];
-          float alpha[2], ref[2] = {-INFINITY, -INFINITY};
+          uint32_t pf[kTiles][2][2];
+          float alpha[kTiles][2];
 #pragma unroll
-          for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              x[mt][k] *= col_scale[k & 1] * ks;
-            }
-          if (masked) {
+          for (int nt = 0; nt < kTiles; ++nt) {
+            const float2 cs = s.col_scale[nt][t];
+            const float sc[2] = {cs.x * ks, cs.y * ks};
+            float ref[2] = {-INFINITY, -INFINITY};
 #pragma unroll
             for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
-              for (int k = 0; k < 4; ++k)
-                if (pos0 + 16 * mt + perm + 8 * (k >> 1) > col_last[k & 1]) x[mt][k] = -INFINITY;
-          }
+              for (int k = 0; k < 4; ++k) x[nt][mt][k] *= sc[k & 1];
+            if (masked) {
+              int last[2];  // last position that the column's row may see
 #pragma unroll
-          for (int mt = 0; mt < 2; ++mt)
+              for (int k = 0; k < 2; ++k) last[k] = it.len - it.n + (first_row + 8 * nt + 2 * t + k) / a.group;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) ref[k & 1] = fmaxf(ref[k & 1], x[mt][k]);
+              for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
-          for (int k = 0; k < 2; ++k) {
-#pragma unroll
-            for (int sh = 4; sh <= 16; sh <<= 1) ref[k] = fmaxf(ref[k], __shfl_xor_sync(0xffffffffu, ref[k], sh));
-            const float m_new = fmaxf(m[k], ref[k]);
-            ref[k] = m_new == -INFINITY ? 0.f : m_new;
-            alpha[k] = ex2(m[k] - ref[k]);  // 0 while nothing has been seen
-            m[k] = m_new;
-            l[k] *= alpha[k];
-          }
-#pragma unroll
-          for (int mt = 0; mt < 2; ++mt) {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              x[mt][k] = ex2(x[mt][k] - ref[k & 1]);
-              l[k & 1] += x[mt][k];
+                for (int k = 0; k < 4; ++k)
+                  if (pos0 + 16 * mt + perm + 8 * (k >> 1) > last[k & 1]) x[nt][mt][k] = -INFINITY;
             }
 #pragma unroll
-            for (int half = 0; half < 2; ++half)
-              pf[mt][half] = transpose8x8(half2_bits(x[mt][2 * half], x[mt][2 * half + 1]));
+            for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+              for (int k = 0; k < 4; ++k) ref[k & 1] = fmaxf(ref[k & 1], x[nt][mt][k]);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+#pragma unroll
+              for (int sh = 4; sh <= 16; sh <<= 1) ref[k] = fmaxf(ref[k], __shfl_xor_sync(0xffffffffu, ref[k], sh));
+              const float m_new = fmaxf(m[nt][k], ref[k]);
+              ref[k] = m_new == -INFINITY ? 0.f : m_new;
+              alpha[nt][k] = ex2(m[nt][k] - ref[k]);  // 0 while nothing has been seen
+              m[nt][k] = m_new;
+              l[nt][k] *= alpha[nt][k];
+            }
+#pragma unroll
+            for (int mt = 0; mt < 2; ++mt) {
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                x[nt][mt][k] = ex2(x[nt][mt][k] - ref[k & 1]);
+                l[nt][k & 1] += x[nt][mt][k];
+              }
+#pragma unroll
+              for (int half = 0; half < 2; ++half)
+                pf[nt][mt][half] = transpose8x8(half2_bits(x[nt][mt][2 * half], x[nt][mt][2 * half + 1]));
+            }
           }
           // ---- O^T += V^T P^T: eight tiles of 16 dims, two steps of 16 tokens
           ok = ok && mbar_wait_warp(&s.full[slot], phase, abort_flag);
@@ -416,7 +429,7 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
           next_slot();
 #pragma unroll
           for (int j = 0; j < 8; ++j) {  // fragment rows gid, gid + 8: dims 16 perm + 2 j, + 1
-            float acc[4] = {0.f, 0.f, 0.f, 0.f};
+            uint32_t f[2][4];
 #pragma unroll
             for (int mt = 0; mt < 2; ++mt) {
               auto word = [&](int k) {
@@ -424,64 +437,71 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
                 return (j >> 1) == 0 ? v.x : (j >> 1) == 1 ? v.y : (j >> 1) == 2 ? v.z : v.w;
               };
               const uint32_t sel = (j & 1) ? 0x7362u : 0x5140u;
-              uint32_t f[4];
-              decode4<kFormat>(__byte_perm(word(0), word(1), sel), f[0], f[1]);
-              decode4<kFormat>(__byte_perm(word(2), word(3), sel), f[2], f[3]);
-              mma_f16(acc, f, pf[mt][0], pf[mt][1]);
+              decode4<kFormat>(__byte_perm(word(0), word(1), sel), f[mt][0], f[mt][1]);
+              decode4<kFormat>(__byte_perm(word(2), word(3), sel), f[mt][2], f[mt][3]);
             }
 #pragma unroll
-            for (int k = 0; k < 4; ++k) o[j][k] = fmaf(acc[k], vs, o[j][k] * alpha[k & 1]);
+            for (int nt = 0; nt < kTiles; ++nt) {
+              float acc[4] = {0.f, 0.f, 0.f, 0.f};
+              mma_f16(acc, f[0], pf[nt][0][0], pf[nt][0][1]);
+              mma_f16(acc, f[1], pf[nt][1][0], pf[nt][1][1]);
+#pragma unroll
+              for (int k = 0; k < 4; ++k) o[nt][j][k] = fmaf(acc[k], vs, o[nt][j][k] * alpha[nt][k & 1]);
+            }
           }
         }
 
-        // ---- join the set's four warps.  A row's 32 chunks of four dims lie permuted, so that neither the writers (rows
-        // 2 t + k, chunks 4 perm + jj) nor the readers (one row, all chunks) meet in a bank.
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-#pragma unroll
-          for (int sh = 4; sh <= 16; sh <<= 1) l[k] += __shfl_xor_sync(0xffffffffu, l[k], sh);
-        named_bar_sync(2 + set, kSetWarps * 32);  // the readers of the last group are done
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          if (gid == 0) {
-            s.red_m[set][sw][2 * t + k] = m[k];
-            s.red_l[set][sw][2 * t + k] = l[k];
-          }
-#pragma unroll
-          for (int jj = 0; jj < 4; ++jj)
-            s.red[set][sw][2 * t + k][(4 * perm + jj) ^ (t + 4 * (perm >> 2))] =
-                make_float4(o[2 * jj][k], o[2 * jj][k + 2], o[2 * jj + 1][k], o[2 * jj + 1][k + 2]);
-        }
-        named_bar_sync(2 + set, kSetWarps * 32);
+        // ---- join the four warps, eight rows at a time.  A row's 32 chunks of four dims lie permuted, so that neither the
+        // writers (rows 2 t + k, chunks 4 perm + jj) nor the readers (one row, all chunks) meet in a bank.
         const bool whole = g.p0 == 0 && g.p1 == g.pages;
         const int my_slot = whole ? 0 : partial_slot(cut, g.g0, cut.cta_of(g.g0), cta);
-        for (int r = sw; r < 8; r += kSetWarps) {  // a warp per row, four dims per lane
-          const int row = first_row + r;
-          if (row >= w.rows) break;
-          float mw[kSetWarps], top = -INFINITY, sum = 0.f;
 #pragma unroll
-          for (int i = 0; i < kSetWarps; ++i) top = fmaxf(top, mw[i] = s.red_m[set][i][r]);
-          float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int nt = 0; nt < kTiles; ++nt) {
 #pragma unroll
-          for (int i = 0; i < kSetWarps; ++i) {
-            if (mw[i] == -INFINITY) continue;  // saw nothing for this row: adds nothing, whatever its masked places held
-            const float f = ex2(mw[i] - top);
-            sum = fmaf(s.red_l[set][i][r], f, sum);
-            const float4 v = s.red[set][i][r][lane ^ ((r >> 1) + 4 * (lane >> 4))];
-            acc.x = fmaf(v.x, f, acc.x);
-            acc.y = fmaf(v.y, f, acc.y);
-            acc.z = fmaf(v.z, f, acc.z);
-            acc.w = fmaf(v.w, f, acc.w);
+          for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int sh = 4; sh <= 16; sh <<= 1) l[nt][k] += __shfl_xor_sync(0xffffffffu, l[nt][k], sh);
+          named_bar_sync(1, kWarps * 32);  // the readers of the rows before are done
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            if (gid == 0) {
+              s.red_m[warp][2 * t + k] = m[nt][k];
+              s.red_l[warp][2 * t + k] = l[nt][k];
+            }
+#pragma unroll
+            for (int jj = 0; jj < 4; ++jj)
+              s.red[warp][2 * t + k][(4 * perm + jj) ^ (t + 4 * (perm >> 2))] =
+                  make_float4(o[nt][2 * jj][k], o[nt][2 * jj][k + 2], o[nt][2 * jj + 1][k], o[nt][2 * jj + 1][k + 2]);
           }
-          if (whole) {
-            write_row(a.out, it.t0, g.head, row, lane, acc, top, sum);
-          } else {
-            const int at = my_slot * kMaxRows + 8 * set + r;
-            reinterpret_cast<float4*>(a.w.o + static_cast<size_t>(at) * kHeadDim)[lane] = acc;
-            if (lane == 0) a.w.ml[at] = make_float2(top, sum);
+          named_bar_sync(1, kWarps * 32);
+          for (int r = warp; r < 8; r += kWarps) {  // a warp per row, four dims per lane
+            const int row = first_row + 8 * nt + r;
+            if (row >= w.rows) break;
+            float mw[kWarps], top = -INFINITY, sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < kWarps; ++i) top = fmaxf(top, mw[i] = s.red_m[i][r]);
+            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int i = 0; i < kWarps; ++i) {
+              if (mw[i] == -INFINITY) continue;  // saw nothing for this row: adds nothing, whatever its masked places held
+              const float f = ex2(mw[i] - top);
+              sum = fmaf(s.red_l[i][r], f, sum);
+              const float4 v = s.red[i][r][lane ^ ((r >> 1) + 4 * (lane >> 4))];
+              acc.x = fmaf(v.x, f, acc.x);
+              acc.y = fmaf(v.y, f, acc.y);
+              acc.z = fmaf(v.z, f, acc.z);
+              acc.w = fmaf(v.w, f, acc.w);
+            }
+            if (whole) {
+              write_row(a.out, it.t0, g.head, row, lane, acc, top, sum);
+            } else {
+              const int at = my_slot * kMaxRows + 8 * nt + r;
+              reinterpret_cast<float4*>(a.w.o + static_cast<size_t>(at) * kHeadDim)[lane] = acc;
+              if (lane == 0) a.w.ml[at] = make_float2(top, sum);
+            }
           }
         }
-        const JoinDesc d = join_desc(cut, g, cta, it.t0, g.tile * kRowTile, min(kRowTile, w.rows - g.tile * kRowTile));
+        const JoinDesc d = join_desc(cut, g, cta, it.t0, first_row, min(kRowTile, w.rows - first_row));
         if (d.rows > 0) todo = d;
       }
       if (w.g_end >= u1) break;
@@ -499,18 +519,18 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
   __syncthreads();
 }
 
-template <int kFormat, int kSets>
+template <int kFormat, int kTiles>
 int launch_decode(const CUtensorMap& tk, const CUtensorMap& tv, const AttnArgs& a, int n_sm, cudaStream_t stream) {
-  const size_t smem = sizeof(DecodeSmem<kSets>) + 1024;
-  static_assert((sizeof(DecodeSmem<kSets>) + 2048) * ctas_per_sm(kSets) <= 228 * 1024, "shared memory of an SM");
-  CRISP_CUDA_TRY(cudaFuncSetAttribute(cache_decode_kernel<kFormat, kSets>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+  const size_t smem = sizeof(DecodeSmem<kTiles>) + 1024;
+  static_assert((sizeof(DecodeSmem<kTiles>) + 2048) * ctas_per_sm(kTiles) <= 228 * 1024, "shared memory of an SM");
+  CRISP_CUDA_TRY(cudaFuncSetAttribute(cache_decode_kernel<kFormat, kTiles>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                       static_cast<int>(smem)),
                  "cache_attention: smem attribute");
-  const int grid = ctas_per_sm(kSets) * n_sm < kMaxCtas ? ctas_per_sm(kSets) * n_sm : kMaxCtas;
-  CRISP_KERNEL("cache_decode", stream, launch_pdl(cache_decode_kernel<kFormat, kSets>, dim3(grid), dim3(threads_of(kSets)),
-                                                  smem, stream, tk, tv, a));
+  const int grid = ctas_per_sm(kTiles) * n_sm < kMaxCtas ? ctas_per_sm(kTiles) * n_sm : kMaxCtas;
+  CRISP_KERNEL("cache_decode", stream, launch_pdl(cache_decode_kernel<kFormat, kTiles>, dim3(grid), dim3(kThreads), smem,
+                                                  stream, tk, tv, a));
   CRISP_CUDA_TRY(cudaGetLastError(), "cache_attention: launch");
-  return launch_cache_join(a.w, a.out, 8 * kSets, grid, stream);
+  return launch_cache_join(a.w, a.out, 8 * kTiles, grid, stream);
 }
 
 template <int kFormat>
