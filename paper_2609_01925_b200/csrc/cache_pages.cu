@@ -194,7 +194,23 @@ __device__ __forceinline__ int block_exponent(uint32_t amax) {
   return e < -126 ? -126 : e;
 }
 
-// four values in units of the scale -> four bytes
+// Four finite bf16 values (two words of two) times f, a power of two that brings them within the format -> four bytes.
+// int8: x f + 1.5 2^23 is one exact product and one rounding to an integer (ties to even), whose low byte is the code;
+// a conversion instruction per value would be bound by its pipe's quarter rate.
+template <int kFormat>
+__device__ __forceinline__ uint32_t encode_finite4(uint32_t w0, uint32_t w1, float f) {
+  const float a = __uint_as_float(w0 << 16), b = __uint_as_float(w0 & 0xffff0000u);
+  const float c = __uint_as_float(w1 << 16), d = __uint_as_float(w1 & 0xffff0000u);
+  if (kFormat == CRISP_CACHE_E4M3) {
+    const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(a * f, b * f), __NV_SATFINITE, __NV_E4M3);
+    const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(c * f, d * f), __NV_SATFINITE, __NV_E4M3);
+    return __byte_perm(lo, hi, 0x5410);
+  }
+  auto whole = [&](float x) { return __float_as_uint(fmaf(x, f, 12582912.0f)); };
+  return __byte_perm(__byte_perm(whole(a), whole(b), 0x0040), __byte_perm(whole(c), whole(d), 0x0040), 0x5410);
+}
+
+// four values in units of the scale -> four bytes, infinities and NaN among them
 template <int kFormat>
 __device__ __forceinline__ uint32_t encode4(float a, float b, float c, float d) {
   if (kFormat == CRISP_CACHE_E4M3) {
@@ -306,18 +322,32 @@ cache_append_kernel(const CacheView c, int layer, const CacheBatch b, const __nv
       x[j][0] = x[j][1] = make_uint4(0, 0, 0, 0);
     }
   }
+  uint32_t top2 = 0;
 #pragma unroll
   for (int j = 0; j < 4; ++j)
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const uint32_t wd[4] = {x[j][u].x, x[j][u].y, x[j][u].z, x[j][u].w};
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const uint32_t lo = wd[g] & 0x7fffu, hi = (wd[g] >> 16) & 0x7fffu;
-        if (lo < 0x7f80u) amax = max(amax, lo);  // infinities and NaN do not set the scale
-        if (hi < 0x7f80u) amax = max(amax, hi);
-      }
+      for (int g = 0; g < 4; ++g) top2 = __vmaxu2(top2, wd[g] & 0x7fff7fffu);
     }
+  amax = max(top2 & 0xffffu, top2 >> 16);
+  const bool finite = amax < 0x7f80u;
+  if (!finite) {  // infinities and NaN do not set the scale
+    amax = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const uint32_t wd[4] = {x[j][u].x, x[j][u].y, x[j][u].z, x[j][u].w};
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const uint32_t lo = wd[g] & 0x7fffu, hi = (wd[g] >> 16) & 0x7fffu;
+          if (lo < 0x7f80u) amax = max(amax, lo);
+          if (hi < 0x7f80u) amax = max(amax, hi);
+        }
+      }
+  }
   amax = __reduce_max_sync(0xffffffffu, amax);
   __shared__ uint32_t warp_max[kAppendThreads / 32];
   if (lane == 0) warp_max[warp] = amax;
@@ -336,14 +366,19 @@ cache_append_kernel(const CacheView c, int layer, const CacheBatch b, const __nv
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const uint32_t wd[4] = {x[j][u].x, x[j][u].y, x[j][u].z, x[j][u].w};
-      float y[8];
+      if (finite) {
+        out[2 * u] = encode_finite4<kFormat>(wd[0], wd[1], f);
+        out[2 * u + 1] = encode_finite4<kFormat>(wd[2], wd[3], f);
+      } else {
+        float y[8];
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        y[2 * g] = __uint_as_float(wd[g] << 16) * f;
-        y[2 * g + 1] = __uint_as_float(wd[g] & 0xffff0000u) * f;
+        for (int g = 0; g < 4; ++g) {
+          y[2 * g] = __uint_as_float(wd[g] << 16) * f;
+          y[2 * g + 1] = __uint_as_float(wd[g] & 0xffff0000u) * f;
+        }
+        out[2 * u] = encode4<kFormat>(y[0], y[1], y[2], y[3]);
+        out[2 * u + 1] = encode4<kFormat>(y[4], y[5], y[6], y[7]);
       }
-      out[2 * u] = encode4<kFormat>(y[0], y[1], y[2], y[3]);
-      out[2 * u + 1] = encode4<kFormat>(y[4], y[5], y[6], y[7]);
     }
     reinterpret_cast<uint4*>(codes + static_cast<size_t>(held + r) * kHeadDim)[part] =
         make_uint4(out[0], out[1], out[2], out[3]);
