@@ -40,6 +40,7 @@ class CrispLayer:
         self.nnz = torch.zeros(1, dtype=torch.int64, device=dev)
         self.o = torch.empty(n, hq, params.head_dim, dtype=torch.bfloat16, device=dev)
         self.lse = torch.empty(hq, n, dtype=torch.float32, device=dev) if with_lse else None
+        self.n_tokens = torch.full((1,), n, dtype=torch.int32, device=dev)
 
     def route(self, q, k, stream=None):
         B.check(B.crisp_route(self.p, q, k, self.route_ws, self.c_struct, self.pattern, self.p_v,
@@ -65,6 +66,15 @@ class CrispLayer:
                                 self.pattern, self.p_v, self.p_s, self.row_ptr, self.col_idx, self.capacity,
                                 self.nnz, self.o, self.lse, dense_below_tokens, stream), "crisp_forward")
         return self.o
+
+    def store(self, k, v, cache, seq_ids, cache_layer: int = 0, stream=None):
+        """Keeps the prompt's K and V for the answer: sequence seq_ids[0] of `cache` (a CrispCache) grows by the prompt,
+        once for all layers (at cache_layer 0), and this layer's part of it is written."""
+        if seq_ids.shape != (1,):
+            raise ValueError("seq_ids must name one sequence")
+        if cache_layer == 0:
+            cache.reserve(seq_ids, self.n_tokens, stream)
+        cache.append(k, v, seq_ids, layer=cache_layer, stream=stream)
 
     def poll(self, stream=None):
         for ws, name in ((self.route_ws, "route"), (self.select_ws, "select"), (self.prefill_ws, "prefill")):

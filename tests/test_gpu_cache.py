@@ -89,7 +89,7 @@ def check_rows(o, lse, reference, rows, untouched=7.0):
     none = np.isnan(want)
     assert (o[none] == untouched).all() and (lse[np.isnan(want_lse)] == untouched).all()
     # weights are rounded to fp16 (2^-11) by the kernel for few rows, to bf16 (2^-8) by the one for many
-    tol = ref.tolerance(want, slack, 2.0 ** -11 if rows <= 16 else 2.0 ** -8, 64)
+    tol = ref.tolerance(want, slack, 2.0 ** -11 if rows <= 24 else 2.0 ** -8, 64)
     bad = ~none & ~(np.abs(o - want) <= tol)
     assert not bad.any(), (int(bad.sum()), np.argwhere(bad)[:4], np.nanmax(np.abs(o - want) / tol))
     fin = np.isfinite(want_lse)
@@ -389,7 +389,9 @@ def test_prompt_answer_branch_and_compact(fmt):
         both.ref.reserve(ids, n)
         both.ref.append(k.double().cpu().numpy(), v.double().cpu().numpy(), ids, cu)
 
-    write([0], [0, 700], k, v)
+    layer.store(k, v, both.gpu, i32([0]))
+    both.ref.reserve([0], [700])
+    both.ref.append(k.double().cpu().numpy(), v.double().cpu().numpy(), [0], [0, 700])
     for step in range(3):
         write([0], [0, 1], tokens(1, hkv, 200 + step), tokens(1, hkv, 210 + step))
         both.check_attention(hq, [0], [1], 220 + step)
@@ -404,6 +406,94 @@ def test_prompt_answer_branch_and_compact(fmt):
     both.check_attention(hq, [1, 3], [1, 1], 242)
     both.check_tables()
     both.check_contents()
+
+
+def test_a_prompt_of_several_layers_is_stored_once():
+    """CrispLayer.store reserves at the first layer and writes each layer's K/V."""
+    from workloads import synth
+    both = Both("e4m3", 1, pages=8, max_seqs=2, max_pages=4, layers=2)
+    q, k, v = synth.random_qkv(300, 4, 1, seed=3, device=DEV)
+    layer = crisp.CrispLayer(crisp.make_params(300, 4, 1, sink_tokens=4))
+    layer.forward(q, k, v, dense_below_tokens=512)
+    for x in range(2):
+        layer.store(k * (x + 1), v, both.gpu, i32([1]), cache_layer=x)
+    both.ref.reserve([1], [300])
+    for x in range(2):
+        both.ref.append((k * (x + 1)).double().cpu().numpy(), v.double().cpu().numpy(), [1], [0, 300], layer=x)
+    layer.poll()
+    both.check_tables()
+    both.check_contents()
+    # attention of all 300 queries over the stored prompt against the dense kernel on what was given: the codes' rounding
+    # (2^-4 of a value for e4m3) is the difference, so only its size is checked
+    o = both.gpu.attention(q, i32([1]))
+    rel = (o.float() - layer.o.float()).norm() / layer.o.float().norm()
+    assert rel < 2.0 ** -4
+    with pytest.raises(ValueError):
+        layer.store(k, v, both.gpu, i32([0, 1]))
+
+
+def test_pages_beyond_four_gigabytes():
+    """A pool whose code offsets pass 2^32 bytes: the pages in use are its last ones."""
+    n_pages = (1 << 32) // (128 * 128) + 40
+    both = Both("e4m3", 1, pages=n_pages, max_seqs=3, max_pages=8, garbage=False)
+    both.ref.codes = {x: np.zeros((1, 1), np.uint8) for x in "kv"}        # (the reference keeps only the last pages)
+    taken = n_pages - 30
+    both.gpu.page_refs[:taken] = 1
+    small = ref.RefCache(1, 30, 1, 3, 8, "e4m3")
+    lens = [700, 130]
+    k, v = tokens(830, 1, 401), tokens(830, 1, 402)
+    both.gpu.reserve(i32([0, 2]), i32(lens))
+    both.gpu.append(k.to(DEV), v.to(DEV), i32([0, 2]), i32([0, 700, 830]))
+    both.gpu.fork(i32([0]), i32([1]), i32([650]))
+    small.reserve([0, 2], lens)
+    small.append(k.double().numpy(), v.double().numpy(), [0, 2], [0, 700, 830])
+    small.fork([0], [1], [650])
+    both.gpu.poll()
+    table = both.gpu.page_table.cpu().numpy()
+    assert np.array_equal(np.where(table >= 0, table - taken, -1), small.table)
+    for new in (1, 40):
+        q = tokens(3 * new, 4, 403 + new)
+        lse = torch.empty(4, 3 * new, device=DEV)
+        o = both.gpu.attention(q.to(DEV), i32([2, 0, 1]), lse=lse)
+        cu = [0, new, 2 * new, 3 * new]
+        check_rows(o, lse, small.attention(q.double().numpy(), [2, 0, 1], cu), new * 4)
+    both.gpu.poll()
+
+
+def test_the_largest_batch():
+    """1024 sequences of one to three tokens, in one call of each kind."""
+    n = B.CACHE_MAX_BATCH
+    both = Both("int8", 1, pages=n + 2, max_seqs=n, max_pages=1)
+    rng = np.random.RandomState(5)
+    lens = rng.randint(1, 4, n).tolist()
+    ids = rng.permutation(n).tolist()
+    both.grow(ids, lens, 501)
+    both.check_tables()
+    both.check_attention(2, ids, [1] * n, 502)
+    both.check_attention(2, ids, [13 if i % 300 == 0 else 1 for i in range(n)], 503)
+    both.gpu.free(i32(ids[::2]))
+    both.ref.free(ids[::2])
+    assert int(both.gpu.compact().item()) == both.ref.compact()
+    both.check_tables()
+    both.check_contents()
+
+
+@pytest.mark.parametrize("seed", range(16))
+def test_random_batches(seed):
+    """Random shapes, formats, lengths and numbers of new tokens, with padding entries and queries without keys."""
+    rng = np.random.RandomState(1000 + seed)
+    hkv = int(rng.choice([1, 2, 3]))
+    hq = hkv * int(rng.choice([1, 2, 4, 5, 7, 8, 16]))
+    batch = int(rng.randint(1, 7))
+    top = int(rng.choice([3, 150, 1400]))
+    lens = [int(x) for x in rng.randint(0, top + 1, batch)]
+    both = Both(str(rng.choice(["e4m3", "int8"])), hkv, pages=batch * 12, max_seqs=batch, max_pages=11)
+    both.grow(list(range(batch)), lens, 2000 + 10 * seed, spread=float(rng.choice([0, 6])))
+    ids = [int(x) if rng.rand() < 0.85 else -1 for x in rng.permutation(batch)]
+    new = [int(x) for x in rng.randint(0, int(rng.choice([1, 3, 20, 260])) + 1, batch)]
+    if max(new) == 0:
+        new[0] = 1
+    both.check_attention(hq, ids, new, 2005 + 10 * seed)
 
 
 def test_step_in_a_graph_and_on_another_stream():
