@@ -163,10 +163,13 @@ class CrispCache:
             if lse.shape != (hq, n):
                 raise ValueError(f"lse must be [{hq}, {n}]")
             plse = lse.data_ptr()
-        if o is None:
-            o = self._new(q.shape, torch.bfloat16, stream)
-        self._call("crisp_cache_attention", stream, layer, ids, cu, batch, n, max_new, hq, softmax_scale, pq,
-                   self._tokens("o", o, n, hq), plse, *self._attention_ws)
+        if o is not None:
+            po = self._tokens("o", o, n, hq)
+        else:
+            o = torch.empty_like(q) if stream is None else self._new(q.shape, torch.bfloat16, stream)
+            po = o.data_ptr()
+        self._call("crisp_cache_attention", stream, layer, ids, cu, batch, n, max_new, hq, softmax_scale, pq, po, plse,
+                   *self._attention_ws)
         return o
 
     def _new(self, shape, dtype, stream):

@@ -187,6 +187,17 @@ int current_sm_count(int* n_sm) {
   return CRISP_OK;
 }
 
+int allow_smem(const void* kernel, size_t bytes, std::atomic<unsigned long long>* done) {
+  int dev = 0;
+  CRISP_CUDA_TRY(cudaGetDevice(&dev), "device");
+  const unsigned long long bit = dev >= 0 && dev < 64 ? 1ull << dev : 0;
+  if (done->load(std::memory_order_relaxed) & bit) return CRISP_OK;
+  CRISP_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes)),
+                 "smem attribute");
+  done->fetch_or(bit, std::memory_order_relaxed);
+  return CRISP_OK;
+}
+
 // ---- the 8-bit cache: host-side checks (what lives on the device is checked by the kernels)
 int check_cache(const crisp_cache* c, CacheView* v) {
   if (!c || c->struct_size != static_cast<int32_t>(sizeof(crisp_cache))) return CRISP_ERR_INVALID_ARG;
@@ -234,6 +245,8 @@ int check_batch(const int32_t* seq_ids, const int32_t* cu, int32_t batch, int32_
   b->n_tokens = n_tokens;
   b->per = batch > 0 && !cu ? n_tokens / batch : 0;
   b->max_new = max_new < n_tokens ? max_new : n_tokens;
+  b->lo = 0;
+  b->hi = n_tokens;
   if (!cu && b->per > b->max_new) return CRISP_ERR_INVALID_ARG;
   return CRISP_OK;
 }
@@ -823,16 +836,28 @@ int crisp_cache_attention(const crisp_cache* c, int32_t layer, const int32_t* se
   rc = current_sm_count(&n_sm);
   if (rc != CRISP_OK) return rc;
   const size_t decode_off = kWsHeader, prefill_off = cache_decode_ws(nullptr, decode_off);
-  // Up to 16 rows per KV head (new tokens x query heads of its group) are two fragments of the kernel that reads the
-  // cache at HBM speed; more rows would make it read the cache again.
-  const bool few = static_cast<long long>(b.max_new) * (n_q_heads / v.heads) <= kDecodeRows;
-  CUtensorMap tk, tv;
+  // Rows per KV head: an item's new tokens x the query heads of the KV head's group.  Up to 24 are three fragments of the
+  // kernel that reads the cache near HBM speed (a page takes an SM 0.5 us with 8 rows, 1.5 us with 24); the tensor-core
+  // kernel takes 2.5 us per page for anything up to 256.  A batch of both kinds is split: its items of up to 8 rows (16
+  // with larger groups) go to the first kernel, which costs about 5 us when there are none.
+  const int group = n_q_heads / v.heads;
+  const bool few = static_cast<long long>(b.max_new) * group <= kDecodeRows;
+  const bool split = !few && b.cu != nullptr && b.batch > 1;
   const size_t code_rows = static_cast<size_t>(v.layers) * v.pages * v.heads * kPage;
-  rc = make_tmap_codes(&tk, v.k_codes, code_rows, few ? kPage : kPage / 2);
-  if (rc == CRISP_OK) rc = make_tmap_codes(&tv, v.v_codes, code_rows, few ? kPage : kPage / 2);
+  CUtensorMap tk, tv;
+  if (few || split) {
+    CacheBatch part = b;
+    if (split) part.hi = (group <= 8 ? 8 : 16) / group;
+    rc = make_tmap_codes(&tk, v.k_codes, code_rows, kPage);
+    if (rc == CRISP_OK) rc = make_tmap_codes(&tv, v.v_codes, code_rows, kPage);
+    if (rc == CRISP_OK)
+      rc = launch_cache_decode(v, layer, part, n_q_heads, scale, q, o, lse, ws, decode_off, tk, tv, n_sm, st);
+    if (rc != CRISP_OK || few) return rc;
+    b.lo = part.hi + 1;
+  }
+  rc = make_tmap_codes(&tk, v.k_codes, code_rows, kPage / 2);
+  if (rc == CRISP_OK) rc = make_tmap_codes(&tv, v.v_codes, code_rows, kPage / 2);
   if (rc != CRISP_OK) return rc;
-  if (few)
-    return launch_cache_decode(v, layer, b, n_q_heads, scale, q, o, lse, ws, decode_off, tk, tv, n_sm, st);
   return launch_cache_prefill(v, layer, b, n_q_heads, scale, q, o, lse, ws, prefill_off, tk, tv, n_sm, st);
 }
 

@@ -1,5 +1,7 @@
 // Shared declarations of the 8-bit paged K/V cache (cache_pages.cu, cache_attention.cu).
 #pragma once
+#include <atomic>
+
 #include "common.cuh"
 
 namespace crisp {
@@ -25,10 +27,14 @@ struct CacheBatch {
   const int32_t* seq_ids;
   const int32_t* cu;
   int batch, n_tokens, per, max_new;
+  int lo, hi;  // items with fewer than lo or more than hi tokens are another kernel's
 };
 
 // Multiprocessors of the current device (asked once per device).
 int current_sm_count(int* n_sm);
+
+// cudaFuncSetAttribute of a kernel's dynamic shared memory, once per device (`done`: a bit per device, the kernel's own).
+int allow_smem(const void* kernel, size_t bytes, std::atomic<unsigned long long>* done);
 
 int check_cache(const crisp_cache* c, CacheView* v);
 int check_batch(const int32_t* seq_ids, const int32_t* cu, int32_t batch, int32_t n_tokens,
@@ -81,8 +87,8 @@ __device__ __forceinline__ CacheItem load_item(const CacheView& c, const CacheBa
     it.len = c.seq_lens[it.seq];
     bad = it.len < 0 || it.len > c.max_pages * kPage;
   }
-  if (bad) {
-    cache_fail(status, CRISP_ERR_BAD_CACHE);
+  if (bad) cache_fail(status, CRISP_ERR_BAD_CACHE);
+  if (bad || it.n < b.lo || it.n > b.hi) {
     it.seq = -1;
     it.len = 0;
   }

@@ -523,9 +523,9 @@ template <int kFormat, int kTiles>
 int launch_decode(const CUtensorMap& tk, const CUtensorMap& tv, const AttnArgs& a, int n_sm, cudaStream_t stream) {
   const size_t smem = sizeof(DecodeSmem<kTiles>) + 1024;
   static_assert((sizeof(DecodeSmem<kTiles>) + 2048) * ctas_per_sm(kTiles) <= 228 * 1024, "shared memory of an SM");
-  CRISP_CUDA_TRY(cudaFuncSetAttribute(cache_decode_kernel<kFormat, kTiles>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                      static_cast<int>(smem)),
-                 "cache_attention: smem attribute");
+  static std::atomic<unsigned long long> done{0};
+  const int rc = allow_smem(reinterpret_cast<const void*>(&cache_decode_kernel<kFormat, kTiles>), smem, &done);
+  if (rc != CRISP_OK) return rc;
   const int grid = ctas_per_sm(kTiles) * n_sm < kMaxCtas ? ctas_per_sm(kTiles) * n_sm : kMaxCtas;
   CRISP_KERNEL("cache_decode", stream, launch_pdl(cache_decode_kernel<kFormat, kTiles>, dim3(grid), dim3(kThreads), smem,
                                                   stream, tk, tv, a));
@@ -535,7 +535,7 @@ int launch_decode(const CUtensorMap& tk, const CUtensorMap& tv, const AttnArgs& 
 
 template <int kFormat>
 int launch_format(const CUtensorMap& tk, const CUtensorMap& tv, const AttnArgs& a, int n_sm, cudaStream_t stream) {
-  const long long rows = static_cast<long long>(a.b.max_new) * a.group;
+  const long long rows = static_cast<long long>(a.b.max_new < a.b.hi ? a.b.max_new : a.b.hi) * a.group;
   if (rows <= 8) return launch_decode<kFormat, 1>(tk, tv, a, n_sm, stream);
   if (rows <= 16) return launch_decode<kFormat, 2>(tk, tv, a, n_sm, stream);
   return launch_decode<kFormat, 3>(tk, tv, a, n_sm, stream);

@@ -634,9 +634,9 @@ cache_prefill_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
 template <int kFormat>
 int launch_tiles(const CUtensorMap& tk, const CUtensorMap& tv, const TileArgs& a, int n_sm, cudaStream_t stream) {
   const size_t smem = sizeof(TileSmem) + 1024;
-  CRISP_CUDA_TRY(cudaFuncSetAttribute(cache_prefill_kernel<kFormat>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                      static_cast<int>(smem)),
-                 "cache_attention: smem attribute");
+  static std::atomic<unsigned long long> done{0};
+  const int rc = allow_smem(reinterpret_cast<const void*>(&cache_prefill_kernel<kFormat>), smem, &done);
+  if (rc != CRISP_OK) return rc;
   const int grid = n_sm < kMaxTileCtas ? n_sm : kMaxTileCtas;
   CRISP_KERNEL("cache_prefill", stream, launch_pdl(cache_prefill_kernel<kFormat>, dim3(grid), dim3(kPrefillThreads), smem,
                                                    stream, tk, tv, a));
