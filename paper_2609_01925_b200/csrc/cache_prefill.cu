@@ -12,6 +12,14 @@
 //    largest); that power and the page's K scale multiply the logits.  P V is bf16, P rounded to bf16 as in prefill.cu.
 // The work is cut into equal runs of pages, one per CTA, and partial results are joined (cache_split.cuh).
 //
+// What bounds it: 4650 cycles per page of 256 rows (2048 new tokens over 32768, 32/8 heads, e4m3: 1.10 ms, 0.97 PFLOP/s).
+// The softmax warps are busy for 4200 of them; the tensor pipe needs 2880 (its N = 64 products are bound by operand fetch)
+// and the shared memory port about 3100 (256 KB of operands, 96 KB of conversion, 32 KB of codes).  Tried and slower: two
+// warpgroups per tile, one for each half of the keys, with a shared running maximum (1180 us); Q K^T of whole pages behind
+// P V, with either (1360 to 1410 us: the chain from S to S is what it lengthens); pacing the two tiles' exponentials or
+// computing part of them on the FMA pipe (1125 to 1195 us).  Code size matters more than any of these: with the converters'
+// loops unrolled eight and four times the same kernel takes 1480 us, because the roles' code misses the instruction caches.
+//
 // Warps (512 threads): 0-3, 4-7 softmax of tile 0, 1 (a thread per row); 8 TMA producer; 9, 10 issuers; 11 idle;
 // 12-15 converters.  TMEM: S_0 | S_1 | O_0 | O_1, 128 columns each.
 #include <cuda_fp16.h>
