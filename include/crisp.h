@@ -342,10 +342,13 @@ int crisp_cache_append(const crisp_cache* c, int32_t layer, const int32_t* seq_i
  *   o = sum_j softmax_j(q . k_j * scale) v_j,  scale = softmax_scale or 1 / sqrt(128) when that is 0.
  * A query that sees nothing (n > L) gets o = 0 and lse = -inf.  lse: optional, [n_q_heads][n_tokens] f32, natural log.
  * max_new bounds every item's number of tokens (HOST; an item above it is refused on the device); it picks the
- * kernel: one or a few tokens read the cache once at HBM speed, longer pieces run on the tensor cores.  Tokens of
- * skipped or refused items and tokens behind the last item are left as they are.  A sequence may be listed more than
- * once.  n_q_heads / n_kv_heads <= 16.  A NaN among a sequence's cached V may reach every row of its items.
- * Row results depend on the batch only through the order of fp32 sums; the same call gives the same bits.
+ * kernels: one or a few tokens read the cache once near HBM speed, longer pieces run on the tensor cores, and a batch
+ * with cu_tokens that may hold both kinds is split between the two.  Tokens of skipped or refused items and tokens
+ * behind the last item are left as they are.  A sequence may be listed more than once.  n_q_heads / n_kv_heads <= 16.
+ * What lies behind a sequence's end, or is hidden from a row, does not reach it, NaN among the codes included; only a
+ * NaN among a sequence's own cached V may reach every row of its items.
+ * max_new and the rest of the batch change a row's result only through roundings and the order of fp32 sums; the same
+ * call gives the same bits.
  */
 int crisp_cache_attention(const crisp_cache* c, int32_t layer, const int32_t* seq_ids, const int32_t* cu_tokens,
                           int32_t batch, int32_t n_tokens, int32_t max_new, int32_t n_q_heads, float softmax_scale,

@@ -25,7 +25,9 @@ class CrispCache:
 
     Lists of sequences are int32 tensors on the cache's device (negative entries are padding).  All calls enqueue on
     `stream` (default: the current stream of the cache's device) and may be captured into a CUDA graph; mistakes that
-    only the device can see (no free page, a sequence listed twice, ...) are raised by poll().
+    only the device can see (no free page, a sequence listed twice, ...) are raised by poll().  Calls of one object must
+    not overlap in time (they share its workspaces): use one stream, or order the streams with events.  Objects over the
+    same tensors may read them (attention) at the same time.
     """
 
     def __init__(self, k_codes, v_codes, k_scale, v_scale, page_table, seq_lens, page_refs, *, fmt: str = "e4m3"):

@@ -469,6 +469,7 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
             if (gid == 0) {
+              if (l[nt][k] != l[nt][k]) m[nt][k] = 0.f;  // NaN among the row's logits: its maximum may be none, but it has been seen
               s.red_m[warp][2 * t + k] = m[nt][k];
               s.red_l[warp][2 * t + k] = l[nt][k];
             }

@@ -78,8 +78,9 @@ class Both:
         out = self.gpu.attention(q.to(DEV), i32(ids), i32(cu), max_new=max(n_new), layer=layer, o=o, lse=lse, **kw)
         assert out is o
         self.gpu.poll()
+        rows = max(n_new) * hq // self.ref.heads
         want = self.ref.attention(q.double().numpy(), ids, cu, layer)
-        check_rows(o, lse, want, max(n_new) * hq // self.ref.heads)
+        check_rows(o, lse, want, rows)
         return o, lse
 
 
@@ -234,7 +235,29 @@ def test_very_different_scales_between_pages():
     for new in (2, 20):
         q = tokens(new, 4, 60)
         q[0] *= 2.0 ** -120
+        q[1, :, ::3] *= 2.0 ** -9        # elements far below the row's largest
         both.check_attention(4, [0], [new], 0, q=q)
+
+
+@pytest.mark.parametrize("new", [1, 5, 20])
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+def test_not_finite_queries_and_keys_reach_their_rows_only(fmt, new):
+    """A row of Q with an infinity or NaN gives NaN in its own output; in e4m3 a NaN key reaches the rows that see it."""
+    both = Both(fmt, 1, pages=8, max_seqs=2, max_pages=4)
+    both.grow([0, 1], [300, 200], 61)
+    q = tokens(2 * new, 4, 62)
+    clean = both.gpu.attention(q.to(DEV), i32([0, 1]), max_new=new)
+    q[0, 1, 5], q[new, 3, 7] = float("nan"), float("inf")
+    o = both.gpu.attention(q.to(DEV), i32([0, 1]), max_new=new)
+    bad = torch.zeros(2 * new, 4, dtype=torch.bool)
+    bad[0, 1] = bad[new, 3] = True
+    assert o[bad].isnan().all() and torch.equal(o[~bad], clean[~bad])
+    if fmt == "e4m3":
+        page = both.ref.table[0, 2]
+        both.gpu.k_codes[0, page, 0, 300 - 256 - 1, 9] = 0x7f        # the last token: seen by the last query only
+        o = both.gpu.attention(q.to(DEV), i32([0, 1]), max_new=new)
+        bad[new - 1] = True
+        assert o[bad].isnan().all() and torch.equal(o[~bad], clean[~bad])
 
 
 def test_layers_and_scale_and_repeats():
@@ -541,6 +564,41 @@ def test_step_in_a_graph_and_on_another_stream():
     both.gpu.poll()
     other.gpu.poll()
     assert both.gpu.seq_lens.tolist() == [131, 305, 10]
+
+
+def test_two_graphs_and_two_objects_over_one_cache():
+    """Two captured calls that share a workspace, replayed in turn; two objects over the same tensors at the same time."""
+    both = Both("int8", 2, pages=120, max_seqs=3, max_pages=60)
+    both.grow([0, 1, 2], [7000, 300, 1000], 601)
+    c = both.gpu
+    twin = crisp.CrispCache(c.k_codes, c.v_codes, c.k_scale, c.v_scale, c.page_table, c.seq_lens, c.page_refs, fmt="int8")
+    ids = i32([1, 0, 2])
+    jobs = [(tokens(3, 8, 602).to(DEV), 1), (tokens(120, 8, 603).to(DEV), 40), (tokens(9, 8, 604).to(DEV), 3)]
+    want = [c.attention(q, ids) for q, _ in jobs]
+    out = [torch.empty_like(q) for q, _ in jobs]
+    graphs = []
+    for (q, _), o in zip(jobs, out):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            c.attention(q, ids, o=o)
+        graphs.append(g)
+    for turn in ([0, 1, 2], [2, 2, 1, 0], [1, 0, 1]):
+        for o in out:
+            o.fill_(7.0)
+        for k in turn:
+            graphs[k].replay()
+        torch.cuda.synchronize()
+        for k in set(turn):
+            assert torch.equal(out[k], want[k])
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = [[x.attention(q, ids, stream=st) for _ in range(20) for q, _ in jobs] for x, st in zip((c, twin), streams)]
+    torch.cuda.synchronize()
+    for g in got:
+        for i, o in enumerate(g):
+            assert torch.equal(o, want[i % 3])
+    c.poll()
+    twin.poll()
 
 
 def test_arguments_are_checked():
