@@ -24,10 +24,10 @@ class CrispCache:
     page_table        int32 [max_seqs, max_pages];  seq_lens int32 [max_seqs];  page_refs int32 [pages]
 
     Lists of sequences are int32 tensors on the cache's device (negative entries are padding).  All calls enqueue on
-    `stream` (default: the current stream of the cache's device) and may be captured into a CUDA graph; mistakes that
-    only the device can see (no free page, a sequence listed twice, ...) are raised by poll().  Calls of one object must
-    not overlap in time (they share its workspaces): use one stream, or order the streams with events.  Objects over the
-    same tensors may read them (attention) at the same time.
+    `stream` (a torch stream or its handle; default: the current stream of the cache's device) and may be captured into a
+    CUDA graph; mistakes that only the device can see (no free page, a sequence listed twice, ...) are raised by poll().
+    Calls of one object must not overlap in time (they share its workspaces): use one stream, or order the streams with
+    events.  Objects over the same tensors may read them (attention) at the same time.
     """
 
     def __init__(self, k_codes, v_codes, k_scale, v_scale, page_table, seq_lens, page_refs, *, fmt: str = "e4m3"):
@@ -175,9 +175,12 @@ class CrispCache:
         return o
 
     def _new(self, shape, dtype, stream):
-        """An output, allocated on the stream that will write it."""
-        if stream is None or not isinstance(stream, torch.cuda.Stream):
+        """An output, allocated on the stream that will write it (memory that the current stream freed may still be in
+        use there)."""
+        if stream is None:
             return torch.empty(shape, dtype=dtype, device=self.device)
+        if isinstance(stream, int):
+            stream = torch.cuda.ExternalStream(stream, device=self.device)
         with torch.cuda.stream(stream):
             return torch.empty(shape, dtype=dtype, device=self.device)
 

@@ -601,6 +601,56 @@ def test_two_graphs_and_two_objects_over_one_cache():
     twin.poll()
 
 
+def test_outputs_belong_to_the_stream_that_writes_them():
+    """An output that the call allocates for a stream given as a handle is not memory that the current stream still reads."""
+    both = Both("e4m3", 2, pages=4, max_seqs=1, max_pages=4)
+    both.grow([0], [300], 611)
+    c, ids, q = both.gpu, i32([0]), tokens(300, 8, 612).to(DEV)
+    want = c.attention(q, ids)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for call, like in ((lambda: c.attention(q, ids, stream=side.cuda_stream), q),
+                       (lambda: c.compact(stream=side.cuda_stream), torch.empty(1, dtype=torch.int32, device=DEV))):
+        old = torch.full_like(like, 7)
+        seen = torch.empty_like(like)
+        torch.cuda.synchronize()
+        torch.cuda._sleep(100_000_000)     # keeps the current stream busy for some tens of milliseconds
+        seen.copy_(old)
+        del old
+        out = call()
+        torch.cuda.synchronize()
+        assert (seen == 7).all()
+        assert torch.equal(out, want) if out.shape == want.shape else out.item() == 3
+    c.poll()
+
+
+def test_the_binding_s_calls_are_the_object_s():
+    """The functions of binding.py on a descriptor do what the methods do."""
+    a, b = (Both("int8", 2, pages=16, max_seqs=4, max_pages=4, garbage=False) for _ in range(2))
+    ids, n_new, cu = i32([1, 3]), i32([200, 5]), i32([0, 200, 205])
+    q, k, v = (tokens(205, h, 620 + h + j).to(DEV) for j, h in enumerate((8, 2, 2)))
+    src, dst, cut = i32([1]), i32([0]), i32([150])
+    c, d = a.gpu, b.gpu
+    c.reserve(ids, n_new)
+    c.append(k, v, ids, cu)
+    want = c.attention(q, ids, cu)
+    c.fork(src, dst, cut, share=False)
+    c.free(ids[1:])
+    used = c.compact()
+    o, lse, n = torch.empty_like(q), torch.empty(8, 205, device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV)
+    assert B.crisp_cache_reserve(d.desc, ids, n_new, 2, d.pages_ws) == B.OK
+    assert B.crisp_cache_append(d.desc, 0, ids, cu, 2, 205, k, v, d.pages_ws) == B.OK
+    assert B.crisp_cache_attention(d.desc, 0, ids, cu, 2, 205, 205, 8, 0.0, q, o, lse, d.attention_ws) == B.OK
+    assert B.crisp_cache_fork(d.desc, src, dst, cut, 1, False, d.pages_ws) == B.OK
+    assert B.crisp_cache_free(d.desc, ids[1:], 1, d.pages_ws) == B.OK
+    assert B.crisp_cache_compact(d.desc, n, d.pages_ws) == B.OK
+    c.poll()
+    d.poll()
+    assert torch.equal(o, want) and n.item() == used.item() == 4
+    for name in ("page_table", "seq_lens", "page_refs"):
+        assert torch.equal(getattr(c, name), getattr(d, name))
+
+
 def test_arguments_are_checked():
     c = crisp.CrispCache.allocate(4, 2, 2, 2)
     q = tokens(2, 4, 1).to(DEV)
