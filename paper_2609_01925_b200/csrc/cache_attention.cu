@@ -17,10 +17,10 @@
 //    shared-memory phase always touch eight different 16-byte banks of the 128-byte-swizzled tile.
 //  * Scales are one per page and head: K's multiplies the logits, V's the page's P V product (O is accumulated in
 //    fp32 per page, which also applies the running maximum's correction).
-// Measured: 4 sequences of 65k to 131k tokens, 32/8 heads, int8: 131 us, 6.1 TB/s (150 us once the board has settled at its
-// power cap's clock); 262144 tokens, 28/4 heads, e4m3: 55 us, of which about 10 are the start and the join; 32 sequences of
+// Measured: 4 sequences of 65k to 131k tokens, 32/8 heads, int8: 133 us, 6.0 TB/s (150 us once the board has settled at its
+// power cap's clock); 262144 tokens, 28/4 heads, e4m3: 56 us, of which about 10 are the start and the join; 32 sequences of
 // 1 to 8192 tokens: 22 us for 82 MB; 300 tokens, 4/1 heads: 7 us.  With 24 rows (five tokens, groups of four) a page costs
-// three times the products and softmax, and the latency of its chain bounds the kernel: 92 us for 224 MB.
+// three times the products and softmax, and the latency of its chain bounds the kernel: 93 us for 224 MB.
 #include <cuda_fp16.h>
 
 #include "cache_codes.cuh"
