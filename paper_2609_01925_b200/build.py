@@ -10,7 +10,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcrisp.so")
 SOURCES = ["api.cu", "route.cu", "select.cu", "prefill.cu", "cache_pages.cu", "cache_attention.cu", "cache_prefill.cu",
            "cache_join.cu", "selftest.cu"]
-HEADERS = ["common.cuh", "cache.cuh", "cache_split.cuh", "cache_codes.cuh", "softmax_rows.cuh",
+HEADERS = ["common.cuh", "cache.cuh", "cache_split.cuh", "cache_codes.cuh", "cache_ring.h", "softmax_rows.cuh",
            "sm100_ptx.cuh", os.path.join("..", "..", "include", "crisp.h")]
 
 

@@ -26,6 +26,7 @@
 
 #include "cache_split.cuh"
 #include "cache_codes.cuh"
+#include "cache_ring.h"
 #include "softmax_rows.cuh"
 
 namespace crisp {
@@ -34,8 +35,6 @@ namespace {
 // K and V move in halves of a page, 64 tokens, in the order in which the products use them:
 //   K_A(0) K_B(0) | V_A(0) K_A(1) V_B(0) K_B(1) | V_A(1) K_A(2) V_B(1) K_B(2) | ... | V_A(n-1) V_B(n-1)
 constexpr int kHalf = kPage / 2;
-constexpr int kRaw = 6;            // ring of halves as codes (8 KB)
-constexpr int kConv = 6;           // ring of converted halves (16 KB)
 constexpr int kInfo = 16;          // words per load or page under way; more than there can be
 constexpr int kIsK = -0x40000000;  // marks a load of K where V's has the number of its tokens that exist
 constexpr int kTileRows = 256;     // rows of a group of work
@@ -567,8 +566,8 @@ cache_prefill_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
       }
     }
   } else {
-    // =============================================================== converters: two pairs of warps, each takes every
-    // second pair of halves (one of V and one of K)
+    // =============================================================== converters: two pairs of warps, each with its own
+    // slots of both rings (cache_ring.h says why)
     reg_dealloc<kRegsConv>();
     const int ct = tid & 63, chunk = ct & 7, row_of = ct >> 3;  // eight threads per token, 16 codes each
     const uint32_t pair = (tid >> 6) & 1;
@@ -585,16 +584,22 @@ cache_prefill_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
     const int dst_off = (chunk >> 2) * 8192 + row_of * 128;
     const int dst_a = dst_off + (((c0 + swap) ^ row_of) << 4), dst_b = dst_off + (((c0 + 1 - swap) ^ row_of) << 4);
     bool ok = true;
-    for (uint32_t i = 0; 2 * pair + (i & 1) + 4 * (i >> 1) < n_loads; ++i) {
-      const uint32_t load = 2 * pair + (i & 1) + 4 * (i >> 1);
-      const int raw = load % kRaw, conv = load % kConv;
-      ok = mbar_wait_warp(&s.raw_full[raw], (load / kRaw) & 1, abort_flag);
-      if (ok && load >= kConv) ok = mbar_wait_warp(&s.conv_empty[conv], (load / kConv - 1) & 1, abort_flag);
+    uint32_t slot = 0, phase = 0;  // of the load, in both rings
+    auto next_slot = [&]() {
+      if (++slot == kRaw) {
+        slot = 0;
+        phase ^= 1u;
+      }
+    };
+    for (uint32_t load = 0; load < n_loads; ++load, next_slot()) {
+      if ((kPairOfSlot >> slot & 1u) != pair) continue;
+      ok = mbar_wait_warp(&s.raw_full[slot], phase, abort_flag);
+      if (ok && load >= kConv) ok = mbar_wait_warp(&s.conv_empty[slot], phase ^ 1u, abort_flag);
       if (!ok) break;
       const float scale = *reinterpret_cast<volatile float*>(&s.load_scale[load % kInfo]);
       const int exist = *reinterpret_cast<volatile int*>(&s.load_rows[load % kInfo]);
-      const uint8_t* src = s.raw[raw];
-      uint8_t* dst = s.conv[conv][0];
+      const uint8_t* src = s.raw[slot];
+      uint8_t* dst = s.conv[slot][0];
       // (short loops on purpose: unrolled eight and four times they made the kernel 27 % slower, because the roles' code no
       // longer fits the instruction caches)
       if (exist == kIsK) {
@@ -628,8 +633,8 @@ cache_prefill_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) {
-        mbar_arrive(&s.raw_empty[raw]);
-        mbar_arrive(&s.conv_full[conv]);
+        mbar_arrive(&s.raw_empty[slot]);
+        mbar_arrive(&s.conv_full[slot]);
       }
     }
   }

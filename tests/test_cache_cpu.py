@@ -3,6 +3,7 @@ GPU tests compare with, checked against closed forms."""
 import ctypes
 import os
 import re
+import subprocess
 
 import numpy as np
 import pytest
@@ -98,6 +99,26 @@ def test_cache_refuses_to_run_without_cuda():
     with pytest.raises(RuntimeError):
         crisp.CrispCache(codes, codes, scale, scale, torch.zeros(1, 4, dtype=torch.int32),
                          torch.zeros(1, dtype=torch.int32), torch.zeros(4, dtype=torch.int32))
+
+
+# ------------------------------------------------------------------------------------------------ the tile kernel's rings
+def ring_model(tmp_path, *flags):
+    """Output of cache_ring_model.cpp, built with the kernel's own constants."""
+    exe = str(tmp_path / "model")
+    subprocess.run(["g++", "-std=c++17", "-O2", "-I", os.path.join(ROOT, "paper_2609_01925_b200", "csrc"), *flags, "-o", exe,
+                    os.path.join(ROOT, "tests", "cache_ring_model.cpp")], check=True)
+    return subprocess.run([exe], check=True, capture_output=True, text=True, timeout=120).stdout.strip()
+
+
+def test_converters_never_take_another_load_s_codes(tmp_path):
+    """Copies that land late or out of order do not let a pair of converter warps pass a barrier's earlier phase."""
+    assert ring_model(tmp_path) == "ok"
+
+
+def test_the_ring_model_sees_a_slot_that_changes_hands(tmp_path):
+    """Loads dealt in turns of two: a slot of six changes hands, and its new pair takes the parity of a phase that it has not
+    seen for the one it waits for."""
+    assert "(seed" in ring_model(tmp_path, "-DOWNER(load)=((load)>>1&1u)")
 
 
 # ------------------------------------------------------------------------------------------------ the reference itself
