@@ -288,7 +288,8 @@ int crisp_forward_host(const crisp_params* p, const void* q_host, const void* k_
  * CRISP_ERR_NO_PAGES.  Unlike the calls above, cache calls do not clear that word: the first error stays until
  * crisp_poll_device_status, so a run of calls needs one poll.  The caller therefore zeroes the first 256 bytes of a
  * workspace once before its first use.  Calls that use one workspace must not overlap in time, and neither must calls
- * that change one cache.
+ * that change one cache.  The reserve, append, fork and compact calls of a cache share one workspace of its own: it also holds
+ * which sequences' latest reserve was refused.
  */
 #define CRISP_CACHE_E4M3 0
 #define CRISP_CACHE_INT8 1
@@ -317,8 +318,10 @@ int crisp_cache_workspace_bytes(const crisp_cache* c, size_t* pages_ws, size_t* 
 /*
  * Makes room for n_new[i] (NULL: 1) more tokens of every listed sequence and adds them to its length: new pages are
  * the lowest free ones, in the order of the list.  All or nothing: with too few free pages, a row of page_table that
- * is too short (CRISP_ERR_NO_PAGES), or a sequence listed twice (CRISP_ERR_BAD_CACHE), nothing changes.  The new
- * tokens' contents are undefined until crisp_cache_append has written them, for each layer.
+ * is too short (CRISP_ERR_NO_PAGES), or a sequence listed twice (CRISP_ERR_BAD_CACHE), nothing changes, and appends to
+ * the sequences that were to grow write nothing until a reserve that lists them succeeds: a step that is already enqueued
+ * behind a refused reserve leaves the cache as it was, and can be tried again.  The new tokens' contents are undefined until
+ * crisp_cache_append has written them, for each layer.
  */
 int crisp_cache_reserve(const crisp_cache* c, const int32_t* seq_ids, const int32_t* n_new, int32_t batch, void* ws,
                         size_t ws_bytes, void* cuda_stream);
@@ -329,7 +332,8 @@ int crisp_cache_reserve(const crisp_cache* c, const int32_t* seq_ids, const int3
  * most n_tokens; NULL: n_tokens / batch each, which must divide), and they are the last positions that the
  * sequence's length covers (crisp_cache_reserve has counted them in).  Earlier tokens of a page whose scale grows
  * are rescaled.  A sequence may be listed only once (CRISP_ERR_BAD_CACHE; its new tokens are then undefined), and the
- * pages written must be held by it alone.
+ * pages written must be held by it alone.  A sequence whose latest reserve through this workspace was refused is left as it
+ * is, and the reserve's status is set again.
  */
 int crisp_cache_append(const crisp_cache* c, int32_t layer, const int32_t* seq_ids, const int32_t* cu_tokens,
                        int32_t batch, int32_t n_tokens, const void* k, const void* v, void* ws, size_t ws_bytes,

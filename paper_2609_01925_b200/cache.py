@@ -115,7 +115,8 @@ class CrispCache:
 
     # ---- pages
     def reserve(self, seq_ids, n_new: Optional[torch.Tensor] = None, stream=None) -> None:
-        """Adds n_new[i] (None: one) tokens to sequence seq_ids[i] and gives it the pages for them."""
+        """Adds n_new[i] (None: one) tokens to sequence seq_ids[i] and gives it the pages for them.  All or nothing; while
+        a refused call stands (until one that lists the sequence succeeds), append leaves the sequence as it is."""
         ids, n = self._list("seq_ids", seq_ids), seq_ids.shape[0]
         self._call("crisp_cache_reserve", stream, ids, self._list("n_new", n_new, n), n, *self._pages_ws)
 

@@ -19,11 +19,22 @@ struct Move {
   int src, dst, rows;  // pages and how many of their tokens are copied
 };
 
+// Which sequences' latest reserve was refused.  An append takes its place from the sequence's length, so behind a reserve that
+// changed nothing it would overwrite the newest tokens; it asks here first.  The codes are kept in the workspace, for the
+// cache whose page_table `owner` is; another cache that plans in the same workspace drops them.
+struct alignas(16) Refusals {
+  const int32_t* owner;
+  int any;  // 0: no code is set and the array may hold anything
+  int pad;
+};
+
 struct PagesWs {
-  int* status;   // the workspace's first word
-  int* n_moves;  // word 16 of the header
-  int* n_left;   // word 17: pages in use after a compaction
-  int* marks;    // [max_seqs]
+  int* status;         // the workspace's first word
+  int* n_moves;        // word 16 of the header
+  int* n_left;         // word 17: pages in use after a compaction
+  Refusals* refusals;  // words 20 .. 23
+  int* refused;        // [max_seqs] status codes, 0 = not refused
+  int* marks;          // [max_seqs]
   int* found;    // [n_pages] pages picked by a scan
   int* remap;    // [n_pages]
   Move* moves;   // [n_pages]
@@ -35,12 +46,14 @@ PagesWs carve(const CacheView& v, void* ws, size_t* total) {
   w.status = reinterpret_cast<int*>(base);
   w.n_moves = w.status + 16;
   w.n_left = w.status + 17;
+  w.refusals = reinterpret_cast<Refusals*>(w.status + 20);
   size_t off = kWsHeader;
   auto take = [&](size_t bytes) {
     void* p = base + off;
     off += align_up(bytes, 256);
     return p;
   };
+  w.refused = static_cast<int*>(take(sizeof(int) * static_cast<size_t>(v.max_seqs)));
   w.marks = static_cast<int*>(take(sizeof(int) * static_cast<size_t>(v.max_seqs)));
   w.found = static_cast<int*>(take(sizeof(int) * static_cast<size_t>(v.pages)));
   w.remap = static_cast<int*>(take(sizeof(int) * static_cast<size_t>(v.pages)));
@@ -101,6 +114,15 @@ __device__ __forceinline__ int find_item(const int* start, int n, int x) {
   return lo;
 }
 
+// One thread, before a plan of cache c uses the workspace's arrays.
+__device__ __forceinline__ void drop_others_refusals(const CacheView& c, const PagesWs& w) {
+  if (w.refusals->owner != c.page_table) w.refusals->any = 0;
+}
+// The code that the latest reserve of sequence s was refused with, 0 if it was not.
+__device__ __forceinline__ int refusal_of(const CacheView& c, const Refusals& r, const int* refused, int s) {
+  return r.any != 0 && r.owner == c.page_table ? refused[s] : 0;
+}
+
 // ---------------------------------------------------------------- reserve
 __global__ void __launch_bounds__(kPlanThreads)
 cache_reserve_kernel(const CacheView c, const int32_t* __restrict__ seq_ids, const int32_t* __restrict__ n_new, int batch,
@@ -109,11 +131,13 @@ cache_reserve_kernel(const CacheView c, const int32_t* __restrict__ seq_ids, con
   __shared__ long long scratch[33];
   __shared__ int off[kMaxCacheBatch + 1];  // first of an item's new pages in the list of found ones
   const int tid = threadIdx.x;
+  if (tid == 0) drop_others_refusals(c, w);
   for (int i = tid; i < batch; i += kPlanThreads) {
     const int s = seq_ids ? seq_ids[i] : i;
     if (s >= 0 && s < c.max_seqs) w.marks[s] = i;
   }
   __syncthreads();
+  const bool any_refused = w.refusals->any != 0;
   int error = 0;
   long long carry = 0;
   for (int base = 0; base < batch; base += kPlanThreads) {
@@ -157,9 +181,25 @@ cache_reserve_kernel(const CacheView c, const int32_t* __restrict__ seq_ids, con
       scan_pages(c.page_refs, 0, c.pages, true, need_all, need_all, w.found, scratch) < need_all)
     error = CRISP_ERR_NO_PAGES;
   if (error != 0) {
-    if (tid == 0) cache_fail(w.status, error);
+    if (!any_refused)
+      for (int s = tid; s < c.max_seqs; s += kPlanThreads) w.refused[s] = 0;
+    __syncthreads();
+    for (int i = tid; i < batch; i += kPlanThreads) {
+      const int s = seq_ids ? seq_ids[i] : i;
+      if (s >= 0 && s < c.max_seqs && (n_new == nullptr || n_new[i] != 0)) w.refused[s] = error;
+    }
+    if (tid == 0) {
+      w.refusals->owner = c.page_table;
+      w.refusals->any = 1;
+      cache_fail(w.status, error);
+    }
     return;
   }
+  if (any_refused)
+    for (int i = tid; i < batch; i += kPlanThreads) {
+      const int s = seq_ids ? seq_ids[i] : i;
+      if (s >= 0) w.refused[s] = 0;
+    }
   for (int k = tid; k < need_all; k += kPlanThreads) {
     const int i = find_item(off, batch, k);
     const int s = seq_ids ? seq_ids[i] : i;
@@ -254,8 +294,10 @@ constexpr int kAppendThreads = 256;
 template <int kFormat>
 __global__ void __launch_bounds__(kAppendThreads)
 cache_append_kernel(const CacheView c, int layer, const CacheBatch b, const __nv_bfloat16* __restrict__ k,
-                    const __nv_bfloat16* __restrict__ v, int slots_per_item, int* status) {
+                    const __nv_bfloat16* __restrict__ v, int slots_per_item, const PagesWs w) {
   pdl_enter();
+  int* status = w.status;
+  const Refusals refusals = *w.refusals;  // (beside the loads of the search below)
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int head = blockIdx.y, kind = blockIdx.z;
   // ---- which item and which of its pages: item i owns the slots floor(cu[i] / 128) + 2 i .., which are at least as
@@ -283,6 +325,10 @@ cache_append_kernel(const CacheView c, int layer, const CacheBatch b, const __nv
   }
   const CacheItem it = load_item(c, b, i, status);
   if (it.seq < 0 || it.n == 0) return;
+  if (const int code = refusal_of(c, refusals, w.refused, it.seq)) {
+    if (tid == 0) cache_fail(status, code);
+    return;
+  }
   if (it.n > it.len) {
     if (tid == 0) cache_fail(status, CRISP_ERR_BAD_CACHE);
     return;
@@ -389,12 +435,12 @@ cache_append_kernel(const CacheView c, int layer, const CacheBatch b, const __nv
     const float shrink = pow2i(max(old - e, -126));
     for (int r = row0; r < held; r += kAppendThreads / 8) {
       uint4* p = reinterpret_cast<uint4*>(codes + static_cast<size_t>(r) * kHeadDim) + part;
-      uint4 w = *p;
-      w.x = rescale4<kFormat>(w.x, shrink);
-      w.y = rescale4<kFormat>(w.y, shrink);
-      w.z = rescale4<kFormat>(w.z, shrink);
-      w.w = rescale4<kFormat>(w.w, shrink);
-      *p = w;
+      uint4 old_codes = *p;
+      old_codes.x = rescale4<kFormat>(old_codes.x, shrink);
+      old_codes.y = rescale4<kFormat>(old_codes.y, shrink);
+      old_codes.z = rescale4<kFormat>(old_codes.z, shrink);
+      old_codes.w = rescale4<kFormat>(old_codes.w, shrink);
+      *p = old_codes;
     }
   }
   if (tid == 0) *scale = pow2i(e);
@@ -409,6 +455,7 @@ cache_fork_kernel(const CacheView c, const int32_t* __restrict__ src, const int3
   __shared__ int own_off[kMaxCacheBatch + 1];  // first of an item's own (copied) pages in the list of found ones
   __shared__ int all_off[kMaxCacheBatch + 1];  // first of an item's pages among those of all items
   const int tid = threadIdx.x;
+  if (tid == 0) drop_others_refusals(c, w);
   for (int i = tid; i < count; i += kPlanThreads)
     if (src[i] >= 0 && dst[i] >= 0 && dst[i] < c.max_seqs) w.marks[dst[i]] = i;
   __syncthreads();
@@ -575,6 +622,7 @@ cache_compact_kernel(const CacheView c, int32_t* n_used, PagesWs w) {
   pdl_enter();
   __shared__ long long scratch[33];
   const int tid = threadIdx.x, most = c.pages;
+  if (tid == 0) drop_others_refusals(c, w);
   const int left = scan_pages(c.page_refs, 0, c.pages, false, 0x7fffffff, 0, nullptr, scratch);
   // the free pages below `left` are as many as the used ones from it on
   const int n = scan_pages(c.page_refs, 0, left, true, 0x7fffffff, most, w.found, scratch);
@@ -624,13 +672,14 @@ int launch_cache_append(const CacheView& v, int layer, const CacheBatch& b, cons
   const dim3 grid(static_cast<unsigned>(slots), v.heads, 2), block(kAppendThreads);
   const auto* kp = static_cast<const __nv_bfloat16*>(k);
   const auto* vp = static_cast<const __nv_bfloat16*>(vv);
-  int* status = static_cast<int*>(ws);
+  size_t total;
+  const PagesWs w = carve(v, ws, &total);
   if (v.format == CRISP_CACHE_E4M3) {
     CRISP_KERNEL("cache_append", stream, launch_pdl(cache_append_kernel<CRISP_CACHE_E4M3>, grid, block, 0, stream, v, layer, b,
-                                                    kp, vp, slots_per_item, status));
+                                                    kp, vp, slots_per_item, w));
   } else {
     CRISP_KERNEL("cache_append", stream, launch_pdl(cache_append_kernel<CRISP_CACHE_INT8>, grid, block, 0, stream, v, layer, b,
-                                                    kp, vp, slots_per_item, status));
+                                                    kp, vp, slots_per_item, w));
   }
   CRISP_CUDA_TRY(cudaGetLastError(), "cache_append: launch");
   return CRISP_OK;

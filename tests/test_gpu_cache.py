@@ -350,6 +350,109 @@ def test_calls_that_do_not_fit_change_nothing():
     refused(B.ERR_BAD_CACHE, both.gpu.free, i32([9]))
 
 
+def tensors(c):
+    return (c.page_table, c.seq_lens, c.page_refs, c.k_codes, c.v_codes, c.k_scale, c.v_scale)
+
+
+def raises_at_poll(c, code):
+    with pytest.raises(crisp.CrispError) as e:
+        c.poll()
+    assert e.value.status == code
+    c.poll()
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+def test_a_step_behind_a_refused_reserve_leaves_the_cache_as_it_was(fmt):
+    """reserve (no page for one of its sequences), append of two layers, attention, without a poll between; then a page is
+    freed and the same step succeeds."""
+    both = Both(fmt, heads=2, pages=5, max_seqs=4, max_pages=3, layers=2)
+    both.grow([0, 1, 2], [128, 130, 90], 701)
+    both.grow([3], [5], 703)
+    c = both.gpu
+    before = [t.clone() for t in tensors(c)]
+    k, v, q = (tokens(3, h, 705 + j).to(DEV) * 64 for j, h in enumerate((2, 2, 8)))     # (the scales would grow)
+    ids = i32([1, 0, 2])
+
+    def step():
+        c.reserve(ids)                       # sequence 0 needs a new page, and there is none
+        for layer in range(2):
+            c.append(k, v, ids, layer=layer)
+        return c.attention(q, ids, layer=1)
+
+    step()
+    raises_at_poll(c, B.ERR_NO_PAGES)
+    step()                                    # again, after the poll
+    raises_at_poll(c, B.ERR_NO_PAGES)
+    c.append(k, v, ids)                       # an append without a new reserve
+    raises_at_poll(c, B.ERR_NO_PAGES)
+    assert all(torch.equal(a, b) for a, b in zip(before, tensors(c)))
+    c.free(i32([3]))
+    both.ref.free([3])
+    step()
+    both.ref.reserve([1, 0, 2], [1, 1, 1])
+    for layer in range(2):
+        both.ref.append(k.double().cpu().numpy(), v.double().cpu().numpy(), [1, 0, 2], [0, 1, 2, 3], layer)
+    both.check_tables()
+    both.check_contents()
+
+
+def test_a_refused_reserve_stops_only_the_sequences_that_it_lists():
+    both = Both("e4m3", heads=1, pages=4, max_seqs=4, max_pages=3)
+    both.grow([0, 1, 2], [100, 130, 60], 711)
+    c = both.gpu
+    k = tokens(1, 1, 713).to(DEV)
+    before = [t.clone() for t in tensors(c)]
+    c.reserve(i32([1, 0, 3]), i32([300, 0, 1]))      # too much for a row; nothing for sequence 0
+    c.append(k, k, i32([1]))
+    c.append(k, k, i32([1, 1]), i32([0, 1, 1]))
+    assert all(torch.equal(a, b) for a, b in zip(before, tensors(c)))
+    both.ref.reserve([2], [1])
+    c.reserve(i32([2]))
+    c.append(k, k, i32([2]))
+    both.ref.append(k.double().cpu().numpy(), k.double().cpu().numpy(), [2], [0, 1])
+    c.append(k, k, i32([0]))                         # was to grow by nothing: its newest token may be written again
+    both.ref.append(k.double().cpu().numpy(), k.double().cpu().numpy(), [0], [0, 1])
+    raises_at_poll(c, B.ERR_NO_PAGES)
+    c.reserve(i32([1, 1]))                           # listed twice
+    c.append(k, k, i32([1]))
+    raises_at_poll(c, B.ERR_BAD_CACHE)
+    both.check_tables()
+    both.check_contents()
+    both.grow([1], [3], 715)
+    both.check_tables()
+    both.check_contents()
+
+
+def test_a_prompt_that_does_not_fit_overwrites_nothing():
+    """CrispLayer.store onto a sequence that already holds as many tokens as the prompt has."""
+    from workloads import synth
+    both = Both("int8", 1, pages=4, max_seqs=2, max_pages=8)
+    both.grow([1], [300], 721)
+    q, k, v = synth.random_qkv(300, 4, 1, seed=4, device=DEV)
+    layer = crisp.CrispLayer(crisp.make_params(300, 4, 1, sink_tokens=4))
+    layer.store(k, v, both.gpu, i32([1]))
+    raises_at_poll(both.gpu, B.ERR_NO_PAGES)
+    both.check_tables()
+    both.check_contents()
+
+
+def test_two_caches_in_one_workspace_do_not_take_each_other_s_refusals():
+    """The calls of two caches, one after the other, through one workspace (sized for the larger one)."""
+    a = Both("e4m3", heads=1, pages=2, max_seqs=2, max_pages=2)
+    b = Both("e4m3", heads=1, pages=90, max_seqs=40, max_pages=4)
+    a.gpu._pages_ws, a.gpu.pages_ws = b.gpu._pages_ws, b.gpu.pages_ws
+    a.grow([0, 1], [128, 100], 731)
+    k = tokens(1, 1, 733).to(DEV)
+    a.gpu.reserve(i32([0, 1]))
+    a.gpu.append(k, k, i32([0]))
+    raises_at_poll(a.gpu, B.ERR_NO_PAGES)
+    b.grow(list(range(40)), [1 + 6 * i for i in range(40)], 735)
+    b.check_tables()
+    b.check_contents()
+    a.check_tables()
+    a.check_contents()
+
+
 def test_append_refuses_what_it_must_not_write():
     both = Both("e4m3", heads=1, pages=8, max_seqs=4, max_pages=3)
     both.grow([0], [256], 95)
