@@ -33,7 +33,15 @@ __device__ __forceinline__ void decode4(uint32_t w, uint32_t& lo, uint32_t& hi) 
   }
 }
 
-// Four codes times their block's scale (a power of two) to two pairs of bf16.
+// Two fp32 values to bf16, clamped to the largest finite one; NaN stays NaN.
+__device__ __forceinline__ uint32_t pack_bf16_finite(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.satfinite.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
+// Four codes times their block's scale (a power of two) to two pairs of bf16, exactly.  The one exception: a value above
+// 255/256 of 2^128 may have been rounded to the code for 2^128, which is clamped, so that a weight of zero hides it.
 template <int kFormat>
 __device__ __forceinline__ void decode_values4(uint32_t w, float scale, uint32_t& lo, uint32_t& hi) {
   float f[4];
@@ -47,15 +55,14 @@ __device__ __forceinline__ void decode_values4(uint32_t w, float scale, uint32_t
       f[2 * k + 1] = v.y * scale;
     }
   } else {
-    // 0x4b000000 + u is the fp32 number 2^23 + u; with u = code + 128, (2^23 + u) scale - (2^23 + 128) scale is exact
+    // 0x4b000000 + u is the fp32 number 2^23 + u; with u = code + 128, subtracting 2^23 + 128 leaves the code.  (The scale
+    // comes after: (2^23 + 128) scale would overflow from 2^105 on.)
     const uint32_t u = w ^ 0x80808080u;
-    const float off = -8388736.0f * scale;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) f[k] = fmaf(__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7440 + k)), scale, off);
+    for (int k = 0; k < 4; ++k) f[k] = (__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7440 + k)) - 8388736.0f) * scale;
   }
-  const __nv_bfloat162 a = __floats2bfloat162_rn(f[0], f[1]), b = __floats2bfloat162_rn(f[2], f[3]);
-  lo = *reinterpret_cast<const uint32_t*>(&a);
-  hi = *reinterpret_cast<const uint32_t*>(&b);
+  lo = pack_bf16_finite(f[0], f[1]);
+  hi = pack_bf16_finite(f[2], f[3]);
 }
 
 }  // namespace

@@ -239,6 +239,43 @@ def test_very_different_scales_between_pages():
         both.check_attention(4, [0], [new], 0, q=q)
 
 
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+def test_very_large_values(fmt):
+    """V up to 2^119: scales beyond 2^105, in both kernels."""
+    both = Both(fmt, 1, pages=4, max_seqs=1, max_pages=4)
+    for i, ev in enumerate((117, 105, 111)):
+        n = 128 if i < 2 else 70
+        k, v = tokens(n, 1, 63 + 2 * i), tokens(n, 1, 64 + 2 * i) * 2.0 ** ev
+        both.gpu.reserve(i32([0]), i32([n]))
+        both.ref.reserve([0], [n])
+        both.gpu.append(k.to(DEV), v.to(DEV), i32([0]))
+        both.ref.append(k.double().numpy(), v.double().numpy(), [0], [0, n])
+    assert both.ref.exps["v"][0, :3, 0].min() > 95
+    for new in (2, 20):
+        both.check_attention(4, [0], [new], 69 + new)
+
+
+@pytest.mark.parametrize("new", [2, 20])
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+def test_the_largest_value_is_hidden_like_any_other(fmt, new):
+    """The last token's V is the largest bf16 number, whose nearest code stands for 2^128: the rows before do not see it."""
+    both = Both(fmt, 1, pages=4, max_seqs=1, max_pages=4)
+    k, v = tokens(148, 1, 65), tokens(148, 1, 66)
+    v[128:147] *= 2.0 ** 112
+    v[147] = torch.finfo(torch.bfloat16).max
+    both.gpu.reserve(i32([0]), i32([148]))
+    both.ref.reserve([0], [148])
+    both.gpu.append(k.to(DEV), v.to(DEV), i32([0]))
+    both.ref.append(k.double().numpy(), v.double().numpy(), [0], [0, 148])
+    assert both.ref.states("v", 0)[147].max() == 2.0 ** 128
+    q = tokens(new, 4, 67)
+    lse = torch.full((4, new), 7.0, device=DEV)
+    o = both.gpu.attention(q.to(DEV), i32([0]), lse=lse)
+    both.gpu.poll()
+    want, want_lse, slack, dots = both.ref.attention(q.double().numpy(), [0], [0, new])
+    check_rows(o[:-1], lse[:, :-1], (want[:-1], want_lse[:, :-1], slack[:-1], dots[:, :-1]), 4 * new)
+
+
 @pytest.mark.parametrize("new", [1, 5, 20])
 @pytest.mark.parametrize("fmt", ["e4m3", "int8"])
 def test_not_finite_queries_and_keys_reach_their_rows_only(fmt, new):
