@@ -4,6 +4,7 @@
 #include <cuda_fp16.h>
 
 #include "cache.cuh"
+#include "softmax_rows.cuh"
 
 namespace crisp {
 namespace {
@@ -56,10 +57,13 @@ __device__ __forceinline__ void decode_values4(uint32_t w, float scale, uint32_t
     }
   } else {
     // 0x4b000000 + u is the fp32 number 2^23 + u; with u = code + 128, subtracting 2^23 + 128 leaves the code.  (The scale
-    // comes after: (2^23 + 128) scale would overflow from 2^105 on.)
+    // comes after: (2^23 + 128) scale would overflow from 2^105 on.  In pairs: eight pieces of
+    // 1 to 700 tokens over up to 20000, 28/4 heads, take 293 us; one by one 297, through decode4 308.)
     const uint32_t u = w ^ 0x80808080u;
+    auto number = [&](int k) { return __uint_as_float(__byte_perm(u, 0x4b000000u, 0x7440 + k)); };
 #pragma unroll
-    for (int k = 0; k < 4; ++k) f[k] = (__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7440 + k)) - 8388736.0f) * scale;
+    for (int k = 0; k < 4; k += 2)
+      unpack2(mul2(add2(pack2(number(k), number(k + 1)), pack2(-8388736.0f, -8388736.0f)), pack2(scale, scale)), f[k], f[k + 1]);
   }
   lo = pack_bf16_finite(f[0], f[1]);
   hi = pack_bf16_finite(f[2], f[3]);
