@@ -11,7 +11,11 @@
 //    that the padded dimension, N = 8, is the few query rows.  (tcgen05 has no shape for so few rows without
 //    the codes going through shared memory a second time, and the tensor pipe is not what bounds this kernel.)
 //    fp16 holds every code of both formats exactly; Q is brought to fp16 by a power of two per row (exact but for
-//    elements 2^-29 below the row's largest), P in [0, 1] is rounded to fp16's 11 bits, everything else is fp32.
+//    elements 2^-29 below the row's largest), the weights are rounded to fp16's 11 bits, everything else is fp32.
+//  * A weight is computed in a unit of its page: 2^-15 of the largest among the 32 tokens that a warp takes from the page.
+//    So none loses bits down to 2^-29 of that one, however much other tokens of the row weigh (a sink, say) and however far
+//    apart the pages' scales of V are.  A row's sums stand in the largest of its units so far; one factor per page and row
+//    brings either the sums or the page there, in fp32.
 //  * The order of the dims inside a dot product and of the keys inside P V is free.  A thread therefore reads whole
 //    16-byte chunks, and which chunk belongs to which fragment row is chosen so that the eight threads of a
 //    shared-memory phase always touch eight different 16-byte banks of the 128-byte-swizzled tile.
@@ -35,6 +39,7 @@ constexpr int kWarps = 4;            // consumer warps, which share a page: 32 t
 constexpr int kThreads = kWarps * 32 + 32;
 constexpr int kMaxCtas = 512;        // bound on the grid; sizes the workspace
 constexpr int kMaxRows = kDecodeRows;  // rows of a partial result
+constexpr float kWeightBits = 15.f, kWeightUnit = 1.f / 32768.f;
 constexpr int kGroupUnits = 1;       // what beginning and ending a group costs, in pages
 
 // Rows come in tiles of eight; a CTA computes kTiles of them at once, which share the loads and conversions of a page.
@@ -312,7 +317,7 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
         const int all_see = it.len - it.n + first_row / a.group;  // every row sees the keys up to here
 
         float o[kTiles][8][4];
-        float m[kTiles][2], l[kTiles][2];
+        float m[kTiles][2], l[kTiles][2];  // o: sums of weight x V, times 2^-15; m: log2 of their unit; l: sums of weights
 #pragma unroll
         for (int nt = 0; nt < kTiles; ++nt) {
           m[nt][0] = m[nt][1] = -INFINITY;
@@ -369,7 +374,7 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
           // ---- online softmax of the columns (the query rows) over the warp's 32 tokens
           const bool masked = pos0 + 31 > all_see;
           uint32_t pf[kTiles][2][2];
-          float alpha[kTiles][2];
+          float alpha[kTiles][2], beta[kTiles][2];
 #pragma unroll
           for (int nt = 0; nt < kTiles; ++nt) {
             const float2 cs = s.col_scale[nt][t];
@@ -397,27 +402,31 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
             for (int k = 0; k < 2; ++k) {
 #pragma unroll
               for (int sh = 4; sh <= 16; sh <<= 1) ref[k] = fmaxf(ref[k], __shfl_xor_sync(0xffffffffu, ref[k], sh));
-              const float m_new = fmaxf(m[nt][k], ref[k]);
-              ref[k] = m_new == -INFINITY ? 0.f : m_new;
-              alpha[nt][k] = ex2(m[nt][k] - ref[k]);  // 0 while nothing has been seen
-              m[nt][k] = m_new;
-              l[nt][k] *= alpha[nt][k];
+              const float low = __fsub_ru(ref[k], kWeightBits);  // rounded upwards: no weight comes above 2^15
+              const float d = low == m[nt][k] ? 0.f : low - m[nt][k], f = ex2(-fabsf(d));  // 0 beside a unit of -infinity
+              alpha[nt][k] = d > 0.f ? f : 1.f;
+              beta[nt][k] = d > 0.f ? 1.f : f;
+              m[nt][k] = fmaxf(m[nt][k], low);
+              ref[k] = low == -INFINITY ? 0.f : low;
             }
+            float sum[2] = {0.f, 0.f};
 #pragma unroll
             for (int mt = 0; mt < 2; ++mt) {
 #pragma unroll
               for (int k = 0; k < 4; ++k) {
                 x[nt][mt][k] = ex2(x[nt][mt][k] - ref[k & 1]);
-                l[nt][k & 1] += x[nt][mt][k];
+                sum[k & 1] += x[nt][mt][k];
               }
 #pragma unroll
               for (int half = 0; half < 2; ++half)
                 pf[nt][mt][half] = transpose8x8(half2_bits(x[nt][mt][2 * half], x[nt][mt][2 * half + 1]));
             }
+#pragma unroll
+            for (int k = 0; k < 2; ++k) l[nt][k] = fmaf(sum[k], beta[nt][k], l[nt][k] * alpha[nt][k]);
           }
           // ---- O^T += V^T P^T: eight tiles of 16 dims, two steps of 16 tokens
           ok = ok && mbar_wait_warp(&s.full[slot], phase, abort_flag);
-          const float vs = s.scale[slot];
+          const float vs = s.scale[slot] * kWeightUnit;
           uint4 vw[2][4];
           const bool tail = pos0 + 31 >= it.len;  // rows behind the last token may hold anything, NaN among it
 #pragma unroll
@@ -431,6 +440,10 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
           __syncwarp();
           if (lane == 0) mbar_arrive(&s.empty[slot]);
           next_slot();
+#pragma unroll
+          for (int nt = 0; nt < kTiles; ++nt)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) beta[nt][k] *= vs;
 #pragma unroll
           for (int j = 0; j < 8; ++j) {  // fragment rows gid, gid + 8: dims 16 perm + 2 j, + 1
             uint32_t f[2][4];
@@ -450,7 +463,7 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
               mma_f16(acc, f[0], pf[nt][0][0], pf[nt][0][1]);
               mma_f16(acc, f[1], pf[nt][1][0], pf[nt][1][1]);
 #pragma unroll
-              for (int k = 0; k < 4; ++k) o[nt][j][k] = fmaf(acc[k], vs, o[nt][j][k] * alpha[nt][k & 1]);
+              for (int k = 0; k < 4; ++k) o[nt][j][k] = fmaf(acc[k], beta[nt][k & 1], o[nt][j][k] * alpha[nt][k & 1]);
             }
           }
         }
@@ -469,6 +482,7 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_con
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
             if (gid == 0) {
+              l[nt][k] *= kWeightUnit;
               if (l[nt][k] != l[nt][k]) m[nt][k] = 0.f;  // NaN among the row's logits: its maximum may be none, but it has been seen
               s.red_m[warp][2 * t + k] = m[nt][k];
               s.red_l[warp][2 * t + k] = l[nt][k];
@@ -563,7 +577,7 @@ int launch_cache_decode(const CacheView& v, int layer, const CacheBatch& b, int 
   a.group = n_q_heads / v.heads;
   a.scale_log2 = scale * kLog2e;
   a.q = static_cast<const __nv_bfloat16*>(q);
-  a.out = Output{static_cast<__nv_bfloat16*>(o), lse, n_q_heads, a.group, b.n_tokens};
+  a.out = Output{static_cast<__nv_bfloat16*>(o), lse, n_q_heads, a.group, b.n_tokens, kWeightBits};
   a.status = static_cast<int*>(ws);
   a.w = carve_partials(ws, &ws_off, kMaxCtas, kMaxRows);
   return v.format == CRISP_CACHE_E4M3 ? launch_format<CRISP_CACHE_E4M3>(tk, tv, a, n_sm, stream)

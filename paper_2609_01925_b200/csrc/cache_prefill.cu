@@ -675,7 +675,7 @@ int launch_cache_prefill(const CacheView& v, int layer, const CacheBatch& b, int
   a.tile_tokens = kTileRows / a.group;
   a.scale_log2 = scale * kLog2e;
   a.q = static_cast<const __nv_bfloat16*>(q);
-  a.out = Output{static_cast<__nv_bfloat16*>(o), lse, n_q_heads, a.group, b.n_tokens};
+  a.out = Output{static_cast<__nv_bfloat16*>(o), lse, n_q_heads, a.group, b.n_tokens, 0.f};
   a.status = static_cast<int*>(ws);
   a.w = carve_partials(ws, &ws_off, kMaxTileCtas, kTileRows);
   return v.format == CRISP_CACHE_E4M3 ? launch_tiles<CRISP_CACHE_E4M3>(tk, tv, a, n_sm, stream)

@@ -44,7 +44,7 @@ struct JoinDesc {
 };
 
 // Partial results: two slots per CTA (2 c for a run that begins at the CTA's first unit, 2 c + 1 for one that begins
-// later), each with `rows` rows of 128 and their maximum (log2 units) and sum.
+// later), each with `rows` rows of 128 and their maximum (log2; short of Output's unit_bits) and sum.
 struct Partials {
   JoinDesc* desc;  // [ctas]
   float2* ml;
@@ -70,6 +70,7 @@ struct Output {
   __nv_bfloat16* o;
   float* lse;
   int n_q_heads, group, n_tokens;
+  float unit_bits;  // values and sums stand in units of 2^(maximum + unit_bits)
 };
 __device__ __forceinline__ void write_row(const Output& out, int t0, int head, int row, int lane, const float4& acc,
                                           float top, float sum) {
@@ -81,7 +82,7 @@ __device__ __forceinline__ void write_row(const Output& out, int t0, int head, i
   v.y = pack_bf16(acc.z * inv, acc.w * inv);
   reinterpret_cast<uint2*>(out.o + (token * out.n_q_heads + h) * kHeadDim)[lane] = v;
   if (out.lse && lane == 0)
-    out.lse[static_cast<size_t>(h) * out.n_tokens + token] = sum == 0.f ? -INFINITY : top * 0.6931471805599453f + logf(sum);
+    out.lse[static_cast<size_t>(h) * out.n_tokens + token] = sum == 0.f ? -INFINITY : (top + out.unit_bits) * 0.6931471805599453f + logf(sum);
 }
 
 namespace {

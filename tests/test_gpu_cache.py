@@ -239,6 +239,26 @@ def test_very_different_scales_between_pages():
         both.check_attention(4, [0], [new], 0, q=q)
 
 
+@pytest.mark.parametrize("new", [1, 3, 5, 20])
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+def test_a_sink_leaves_the_other_weights_their_bits(fmt, new):
+    """The first token takes all weight but 2^-22 of it and has no value.  What is left comes from weights of 2^-18 to 2^-27 in
+    its page, or from weights of about 2^-37 in a page whose values are 2^30 times larger."""
+    for page2 in (0.0, 2.0 ** 30):
+        both = Both(fmt, 1, pages=4, max_seqs=1, max_pages=4)
+        k, v = tokens(256, 1, 801), tokens(256, 1, 802)
+        k[0], v[0] = 15.5 / 128 ** 0.5, 0           # a logit of 15.5 with queries near (1, 1, ...)
+        k[128:] -= 10 / 128 ** 0.5
+        v[128:] *= page2
+        v[160:] = 0                                 # the tokens that share a warp with the sink
+        both.gpu.reserve(i32([0]), i32([256]))
+        both.ref.reserve([0], [256])
+        both.gpu.append(k.to(DEV), v.to(DEV), i32([0]))
+        both.ref.append(k.double().numpy(), v.double().numpy(), [0], [0, 256])
+        q = (1 + tokens(new, 4, 803) / 16).bfloat16()
+        both.check_attention(4, [0], [new], 0, q=q)
+
+
 @pytest.mark.parametrize("fmt", ["e4m3", "int8"])
 def test_very_large_values(fmt):
     """V up to 2^119: scales beyond 2^105, in both kernels."""
