@@ -22,6 +22,7 @@
 //
 // Warps (512 threads): 0-3, 4-7 softmax of tile 0, 1 (a thread per row); 8 TMA producer; 9, 10 issuers; 11 idle;
 // 12-15 converters.  TMEM: S_0 | S_1 | O_0 | O_1, 128 columns each.
+#include <cmath>
 #include <cuda_fp16.h>
 
 #include "cache_split.cuh"
@@ -41,7 +42,13 @@ constexpr int kTileRows = 256;     // rows of a group of work
 constexpr int kGroupUnits = 4;     // what beginning and ending a group costs, in pages
 constexpr int kMaxTileCtas = 160;  // bound on the grid; sizes the workspace
 constexpr int kPrefillThreads = 512;
-constexpr float kNothing = -1e30f;  // running maximum of a row that has seen nothing
+constexpr float kNothing = -3.402823466e38f;  // running maximum of a row that has seen nothing: the least finite number
+// A weight's exponent, x scale - m in one FMA, is off by half a unit of m in its last place, the same for all of a row: up to
+// |m| = 2^30 that is a factor of at most 2^32 on weights and sums alike.  Beyond, two fp32 logits that differ at all differ by 64
+// or more, so that the row's weights are its ties for the maximum; there the product with a power of two, which is exact, gives
+// the same weights.  It is the power above the scale, so that such logits stay beyond all others; the maximum is brought
+// back at the end (true_max).  (Scaling the logits first instead, or multiplying the difference: 2 to 10 % of the kernel.)
+constexpr float kFar = 1073741824.0f;
 constexpr float kRescaleAt = 8.0f;  // log2 units (as in prefill.cu)
 
 constexpr int kRegsSoft = 176, kRegsMisc = 72, kRegsConv = 88;
@@ -53,7 +60,7 @@ struct TileArgs {
   Partials w;
   Output out;
   int layer, group, tile_tokens;  // tile_tokens: 256 / group, the new tokens of a group of work
-  float scale_log2;
+  float scale_pow2, scale_rest;  // softmax scale x log2(e) = scale_pow2 x scale_rest, a power of two and 1/2 to 1
   const __nv_bfloat16* q;
   int* status;
 };
@@ -285,7 +292,7 @@ cache_prefill_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
           const int ex = static_cast<int>(amax >> 7);        // 255: the row holds an infinity or NaN and stays one
           const int e = ex == 255 ? 0 : min(141 - ex, 126);  // the row's largest element lands in [2^14, 2^15)
           const float f = pow2i(e);
-          row_scale = a.scale_log2 * pow2i(-e);
+          row_scale = a.scale_pow2 * pow2i(-e);
 #pragma unroll
           for (int c = 0; c < 16; ++c) {
             const uint32_t wd[4] = {x[c].x, x[c].y, x[c].z, x[c].w};
@@ -322,7 +329,10 @@ cache_prefill_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
           tmem_ld_x32(half_addr + 32, x[1]);
           if (h == 0) scale = row_scale * *reinterpret_cast<volatile float*>(&s.page_scale[page_count % kInfo]);
           tmem_ld_wait();
-          const float mx = (masked ? row_max<true>(x, lim, 0) : row_max<false>(x, lim, 0)) * scale;
+          const float top = masked ? row_max<true>(x, lim, 0) : row_max<false>(x, lim, 0);
+          const float near = scale * a.scale_rest;
+          const bool far = fabsf(top * near) > kFar;
+          const float logit_scale = far ? scale : near, mx = top * logit_scale;
           if (i == 0) {
             m_used = fmaxf(mx, kNothing);
           } else if (__any_sync(0xffffffffu, mx > m_used + kRescaleAt)) {
@@ -337,8 +347,8 @@ cache_prefill_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
             m_used = m_new;
           }
           uint32_t pk[2][16];
-          l_run += masked ? exp_pack<true>(x, lim, 0, scale, m_used, pk, no_pacing)
-                          : exp_pack<false>(x, lim, 0, scale, m_used, pk, no_pacing);
+          l_run += masked ? exp_pack<true>(x, lim, 0, logit_scale, m_used, pk, no_pacing)
+                          : exp_pack<false>(x, lim, 0, logit_scale, m_used, pk, no_pacing);
           asm volatile("" : "+f"(l_run)::"memory");  // the run of exponentials ends here
           tmem_st_x16(half_addr, pk[0]);       // P over the columns of its own S, which this warp has read
           tmem_st_x16(half_addr + 16, pk[1]);
@@ -356,6 +366,7 @@ cache_prefill_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
           const size_t token = static_cast<size_t>(it.t0) + row / a.group;
           const int h = g.head * a.group + row % a.group;
           const float inv = l_run == 0.f ? 0.f : 1.0f / l_run;
+          const float true_max = fabsf(m_used) > kFar ? m_used * a.scale_rest : m_used;
           __nv_bfloat16* orow = a.out.o + (token * a.out.n_q_heads + h) * kHeadDim;
           float* prow = a.w.o + (static_cast<size_t>(slot) * kTileRows + my_row) * kHeadDim;
 #pragma unroll
@@ -382,10 +393,10 @@ cache_prefill_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
           }
           if (my_row < rows) {
             if (!whole)
-              a.w.ml[static_cast<size_t>(slot) * kTileRows + my_row] = make_float2(m_used, l_run);
+              a.w.ml[static_cast<size_t>(slot) * kTileRows + my_row] = make_float2(true_max, l_run);
             else if (a.out.lse)
               a.out.lse[static_cast<size_t>(h) * a.out.n_tokens + token] =
-                  l_run == 0.f ? -INFINITY : m_used * 0.6931471805599453f + logf(l_run);
+                  l_run == 0.f ? -INFINITY : true_max * 0.6931471805599453f + logf(l_run);
           }
           tc_fence_before_sync();
         }
@@ -673,7 +684,9 @@ int launch_cache_prefill(const CacheView& v, int layer, const CacheBatch& b, int
   a.layer = layer;
   a.group = n_q_heads / v.heads;
   a.tile_tokens = kTileRows / a.group;
-  a.scale_log2 = scale * kLog2e;
+  int exponent;
+  a.scale_rest = std::frexp(scale * kLog2e, &exponent);
+  a.scale_pow2 = std::ldexp(1.f, exponent);
   a.q = static_cast<const __nv_bfloat16*>(q);
   a.out = Output{static_cast<__nv_bfloat16*>(o), lse, n_q_heads, a.group, b.n_tokens, 0.f};
   a.status = static_cast<int*>(ws);

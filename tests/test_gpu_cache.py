@@ -259,6 +259,33 @@ def test_a_sink_leaves_the_other_weights_their_bits(fmt, new):
         both.check_attention(4, [0], [new], 0, q=q)
 
 
+@pytest.mark.parametrize("new", [2, 20])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+def test_very_large_logits(fmt, sign, new):
+    """Logits of 1e33, 1e10, 1e9 (between 0.9 and 1.4 times 2^30 in base 2) and 1e8: the keys come in a few exact sizes, mixed or
+    a size for each half of a page, so the nearest ones share all weight."""
+    for size in (torch.arange(300) % 7, torch.arange(300) // 64):
+        k = (sign * (1 + size / 8) * 2.0 ** 40)[:, None, None].expand(300, 1, 128).bfloat16()
+        v = tokens(300, 1, 805)
+        both = Both(fmt, 1, pages=4, max_seqs=1, max_pages=4)
+        both.gpu.reserve(i32([0]), i32([300]))
+        both.ref.reserve([0], [300])
+        both.gpu.append(k.contiguous().to(DEV), v.to(DEV), i32([0]))
+        both.ref.append(k.double().numpy(), v.double().numpy(), [0], [0, 300])
+        assert np.array_equal(both.ref.states("k", 0), k.double().numpy())       # exact in both formats
+        for top in (2.0 ** 66, 2.0 ** -10, 1.75 * 2.0 ** -15, 2.0 ** -16):
+            q = torch.full((new, 4, 128), top, dtype=torch.bfloat16)
+            lse = torch.empty(4, new, device=DEV)
+            o = both.gpu.attention(q.to(DEV), i32([0]), lse=lse)
+            both.gpu.poll()
+            want, want_lse, slack, dots = both.ref.attention(q.double().numpy(), [0], [0, new])
+            # equal keys give equal logits and the others' weights are 0, so the logits' own error drops out of slack
+            tol = ref.tolerance(want, slack / (1 + dots.T[:, :, None]), 2.0 ** -11 if new <= 6 else 2.0 ** -8, 64)
+            assert (np.abs(o.double().cpu().numpy() - want) <= tol).all()
+            assert (np.abs(lse.double().cpu().numpy() - want_lse) <= ref.lse_tolerance(want_lse, dots, 64)).all()
+
+
 @pytest.mark.parametrize("fmt", ["e4m3", "int8"])
 def test_very_large_values(fmt):
     """V up to 2^119: scales beyond 2^105, in both kernels."""
