@@ -180,8 +180,8 @@ class CrispCache:
         use there)."""
         if stream is None:
             return torch.empty(shape, dtype=dtype, device=self.device)
-        if isinstance(stream, int):
-            stream = torch.cuda.ExternalStream(stream, device=self.device)
+        if isinstance(stream, int):  # (a handle of 0 is the default stream; ExternalStream(0) would be a new one)
+            stream = torch.cuda.ExternalStream(stream, device=self.device) if stream else torch.cuda.default_stream(self.device)
         with torch.cuda.stream(stream):
             return torch.empty(shape, dtype=dtype, device=self.device)
 

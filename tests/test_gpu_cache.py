@@ -811,6 +811,23 @@ def test_outputs_belong_to_the_stream_that_writes_them():
     c.poll()
 
 
+def test_handle_zero_is_the_default_stream():
+    """Outputs that a call allocates for stream=0, with another stream current, come from the default stream's memory."""
+    both = Both("e4m3", 2, pages=40, max_seqs=1, max_pages=40)
+    both.grow([0], [5000], 613)
+    ids, q = i32([0]), tokens(5000, 8, 614).to(DEV)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        outs = [both.gpu.attention(q, ids, stream=0), both.gpu.compact(stream=0)]
+    torch.cuda.synchronize()
+    for out in outs:
+        at = out.data_ptr()
+        home = [x["stream"] for x in torch.cuda.memory_snapshot() if x["address"] <= at < x["address"] + x["total_size"]]
+        assert home == [torch.cuda.default_stream().cuda_stream] == [0]
+    both.gpu.poll(stream=0)
+
+
 def test_the_binding_s_calls_are_the_object_s():
     """The functions of binding.py on a descriptor do what the methods do."""
     a, b = (Both("int8", 2, pages=16, max_seqs=4, max_pages=4, garbage=False) for _ in range(2))
