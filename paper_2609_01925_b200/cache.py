@@ -27,7 +27,9 @@ class CrispCache:
     `stream` (a torch stream or its handle; default: the current stream of the cache's device) and may be captured into a
     CUDA graph; mistakes that only the device can see (no free page, a sequence listed twice, ...) are raised by poll().
     Calls of one object must not overlap in time (they share its workspaces): use one stream, or order the streams with
-    events.  Objects over the same tensors may read them (attention) at the same time.
+    events, also behind the object's creation, which initialises its tensors on the current stream.  Objects over the same
+    tensors may read them (attention) at the same time.  Tensors given to a call may be dropped right behind it, whatever its
+    stream; the cache itself is kept until its calls have run.
     """
 
     def __init__(self, k_codes, v_codes, k_scale, v_scale, page_table, seq_lens, page_refs, *, fmt: str = "e4m3"):
@@ -119,22 +121,26 @@ class CrispCache:
         a refused call stands (until one that lists the sequence succeeds), append leaves the sequence as it is."""
         ids, n = self._list("seq_ids", seq_ids), seq_ids.shape[0]
         self._call("crisp_cache_reserve", stream, ids, self._list("n_new", n_new, n), n, *self._pages_ws)
+        self._used(stream, seq_ids, n_new)
 
     def fork(self, src, dst, n_tokens: Optional[torch.Tensor] = None, share: bool = True, stream=None) -> None:
         """Makes the empty sequence dst[i] the first n_tokens[i] (None: all) tokens of src[i]."""
         n = src.shape[0]
         self._call("crisp_cache_fork", stream, self._list("src", src), self._list("dst", dst, n),
                    self._list("n_tokens", n_tokens, n), n, 1 if share else 0, *self._pages_ws)
+        self._used(stream, src, dst, n_tokens)
 
     def free(self, seq_ids, stream=None) -> None:
         """Empties the listed sequences."""
         self._call("crisp_cache_free", stream, self._list("seq_ids", seq_ids), seq_ids.shape[0], *self._pages_ws)
+        self._used(stream, seq_ids)
 
     def compact(self, n_used: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         """Moves the pages in use to the front of the pool; returns how many there are (int32 [1], on the device)."""
         if n_used is None:
             n_used = self._new((1,), torch.int32, stream)
         self._call("crisp_cache_compact", stream, self._list("n_used", n_used, 1), *self._pages_ws)
+        self._used(stream, n_used)
         return n_used
 
     # ---- contents
@@ -145,6 +151,7 @@ class CrispCache:
         self._call("crisp_cache_append", stream, layer, self._list("seq_ids", seq_ids),
                    self._list("cu_tokens", cu_tokens, batch + 1), batch, n, self._tokens("k", k, n, self.n_kv_heads),
                    self._tokens("v", v, n, self.n_kv_heads), *self._pages_ws)
+        self._used(stream, k, v, seq_ids, cu_tokens)
 
     def attention(self, q, seq_ids, cu_tokens: Optional[torch.Tensor] = None, max_new: Optional[int] = None,
                   layer: int = 0, softmax_scale: float = 0.0, o: Optional[torch.Tensor] = None,
@@ -173,16 +180,31 @@ class CrispCache:
             po = o.data_ptr()
         self._call("crisp_cache_attention", stream, layer, ids, cu, batch, n, max_new, hq, softmax_scale, pq, po, plse,
                    *self._attention_ws)
+        self._used(stream, q, seq_ids, cu_tokens, o, lse)
         return o
+
+    def _torch_stream(self, stream):
+        """The torch stream of a stream or handle.  (0 is the default stream's; ExternalStream(0) would be a new one.)"""
+        if not isinstance(stream, int):
+            return stream
+        return torch.cuda.ExternalStream(stream, device=self.device) if stream else torch.cuda.default_stream(self.device)
+
+    def _used(self, stream, *tensors):
+        """Tells the allocator that a call on a given stream uses these tensors, so that their memory is not handed out
+        again before it has run."""
+        if stream is None:
+            return
+        stream = self._torch_stream(stream)
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
 
     def _new(self, shape, dtype, stream):
         """An output, allocated on the stream that will write it (memory that the current stream freed may still be in
         use there)."""
         if stream is None:
             return torch.empty(shape, dtype=dtype, device=self.device)
-        if isinstance(stream, int):  # (a handle of 0 is the default stream; ExternalStream(0) would be a new one)
-            stream = torch.cuda.ExternalStream(stream, device=self.device) if stream else torch.cuda.default_stream(self.device)
-        with torch.cuda.stream(stream):
+        with torch.cuda.stream(self._torch_stream(stream)):
             return torch.empty(shape, dtype=dtype, device=self.device)
 
     def poll(self, stream=None) -> None:

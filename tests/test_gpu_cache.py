@@ -811,6 +811,37 @@ def test_outputs_belong_to_the_stream_that_writes_them():
     c.poll()
 
 
+@pytest.mark.parametrize("handle", [False, True])
+def test_inputs_may_be_dropped_behind_a_call_on_another_stream(handle):
+    """The side stream is busy when the calls are made; their temporaries' memory is not handed out again before they ran."""
+    both = Both("e4m3", 2, pages=8, max_seqs=2, max_pages=4)
+    both.grow([1], [10], 621)
+    c = both.gpu
+    k, v, q = (tokens(300, h, 623 + j) for j, h in enumerate((2, 2, 8)))
+    both.ref.reserve([0], [300])
+    both.ref.append(k.double().numpy(), v.double().numpy(), [0], [0, 300])
+    side = torch.cuda.Stream()
+    stream = side.cuda_stream if handle else side
+    given = [x.to(DEV) for x in (k, v, q)]
+    lse = torch.full((8, 300), 7.0, device=DEV)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(100_000_000)     # some tens of milliseconds
+    ids, n_new, cu, temporary = i32([0]), i32([300]), i32([0, 300]), [x.clone() for x in given]
+    side.wait_stream(torch.cuda.current_stream())
+    c.reserve(ids, n_new, stream=stream)
+    c.append(*temporary[:2], ids, cu, stream=stream)
+    o = c.attention(temporary[2], ids, lse=lse, stream=stream)
+    del ids, n_new, cu, temporary
+    junk = [torch.full_like(x, float("nan")) for x in given for _ in range(3)] + [i32([1]) for _ in range(20)]
+    junk += [i32([0, 5]) for _ in range(20)]
+    torch.cuda.synchronize()
+    both.check_tables()
+    both.check_contents()
+    check_rows(o, lse, both.ref.attention(q.double().numpy(), [0], [0, 300]), 1200)
+    del junk
+
+
 def test_handle_zero_is_the_default_stream():
     """Outputs that a call allocates for stream=0, with another stream current, come from the default stream's memory."""
     both = Both("e4m3", 2, pages=40, max_seqs=1, max_pages=40)
