@@ -284,8 +284,8 @@ int crisp_forward_host(const crisp_params* p, const void* q_host, const void* k_
  *
  * Lists of sequences (DEVICE int32): seq_ids[i] is the sequence of item i; a negative entry is padding and is
  * skipped; NULL means item i is sequence i.  At most CRISP_CACHE_MAX_BATCH items.  Nothing on the device is trusted:
- * what breaks a rule is not read or written, and sets the status word of the workspace to CRISP_ERR_BAD_CACHE or
- * CRISP_ERR_NO_PAGES.  Unlike the calls above, cache calls do not clear that word: the first error stays until
+ * what breaks a rule is not read or written, and sets the status word of the workspace to CRISP_ERR_BAD_CACHE,
+ * CRISP_ERR_NO_PAGES or CRISP_ERR_UNSUPPORTED.  Unlike the calls above, cache calls do not clear that word: the first error stays until
  * crisp_poll_device_status, so a run of calls needs one poll.  The caller therefore zeroes the first 256 bytes of a
  * workspace once before its first use.  Calls that use one workspace must not overlap in time, and neither must calls
  * that change one cache.  The reserve, append, fork and compact calls of a cache share one workspace of its own: it also holds
@@ -351,6 +351,9 @@ int crisp_cache_append(const crisp_cache* c, int32_t layer, const int32_t* seq_i
  * behind the last item are left as they are.  A sequence may be listed more than once.  n_q_heads / n_kv_heads <= 16.
  * What lies behind a sequence's end, or is hidden from a row, does not reach it, NaN among the codes included; only a
  * NaN among a sequence's own cached V may reach every row of its items.
+ * The work of a call is counted in pages: each item has, for each KV head and each 256 rows (new tokens x query heads of the
+ * head) of it, the pages that those rows see plus 4.  Where the sum over a kernel's items reaches 2^31 - 1, these are left as
+ * they are and the status is CRISP_ERR_UNSUPPORTED.
  * max_new and the rest of the batch change a row's result only through roundings and the order of fp32 sums; the same
  * call gives the same bits.
  */
@@ -406,8 +409,8 @@ int crisp_selftest_bounded_wait(void* ws, size_t ws_bytes, int64_t limit_ns, voi
 
 /*
  * Synchronises `cuda_stream`, reads the status word at the start of `ws`, clears it and returns it
- * (CRISP_OK, CRISP_ERR_CAPACITY, CRISP_ERR_DEVICE_TIMEOUT, CRISP_ERR_BAD_LIST, CRISP_ERR_NO_PAGES or
- * CRISP_ERR_BAD_CACHE), or CRISP_ERR_CUDA if the stream failed.
+ * (CRISP_OK, CRISP_ERR_CAPACITY, CRISP_ERR_DEVICE_TIMEOUT, CRISP_ERR_BAD_LIST, CRISP_ERR_NO_PAGES, CRISP_ERR_BAD_CACHE or
+ * CRISP_ERR_UNSUPPORTED), or CRISP_ERR_CUDA if the stream failed.
  */
 int crisp_poll_device_status(void* ws, void* cuda_stream);
 

@@ -217,7 +217,7 @@ cache_prefill_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
   if (tid == 0) s.start[batch] = static_cast<int>(min(carry, 0x7fffffffLL));
   __syncthreads();
   const bool too_many = carry * heads >= 0x7fffffffLL;  // units are counted in 32 bits
-  if (too_many && tid == 0) cache_fail(a.status, CRISP_ERR_BAD_CACHE);
+  if (too_many && tid == 0) cache_fail(a.status, CRISP_ERR_UNSUPPORTED);
   const Cut cut(too_many ? 0 : static_cast<int>(carry) * heads, gridDim.x);
   const int cta = blockIdx.x;
   if (cta >= cut.ctas) {

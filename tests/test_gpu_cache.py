@@ -577,6 +577,20 @@ def test_attention_skips_what_breaks_its_rules():
         both.gpu.poll()
 
 
+@pytest.mark.parametrize("new,hq", [(1, 8), (4, 64)])
+def test_a_call_with_too_much_work_is_refused_as_such(new, hq):
+    """Sixteen readers of a sequence of the greatest length, 8 KV heads: 2^31 pages of work.  All of its pages are one page."""
+    c = crisp.CrispCache.allocate(1, 8, 1, (1 << 24) - 1)
+    c.page_table.zero_()
+    c.page_refs.fill_(1)
+    c.seq_lens.fill_(((1 << 24) - 1) * 128)
+    q = tokens(16 * new, hq, 99).to(DEV)
+    o = torch.full_like(q, 7.0)
+    c.attention(q, i32([0] * 16), o=o)
+    raises_at_poll(c, B.ERR_UNSUPPORTED)
+    assert (o == 7).all()
+
+
 # ------------------------------------------------------------------------------------------------ as they are used
 @pytest.mark.parametrize("fmt", ["e4m3", "int8"])
 def test_prompt_answer_branch_and_compact(fmt):
