@@ -99,6 +99,11 @@ class CrispCache:
             raise ValueError(f"{name} must be [{tokens}, {heads}, 128]")
         return t.data_ptr()
 
+    def check_tokens(self, k, v, tokens):
+        """Raises what append would unless k and v are [tokens, kv_heads, 128] bf16 tensors that it takes."""
+        if any(self._tokens(name, t, tokens, self.n_kv_heads) % 16 for name, t in (("k", k), ("v", v))):
+            raise B.CrispError(B.ERR_INVALID_ARG, "crisp_cache_append")
+
     def _call(self, name, stream, *args):
         """The C call of that name on (cache, *args, stream), with the cache's device current.  (The answering loop calls
         this once or more per layer and token, so the way to the library is kept short.)"""

@@ -69,9 +69,10 @@ class CrispLayer:
 
     def store(self, k, v, cache, seq_ids, cache_layer: int = 0, stream=None):
         """Keeps the prompt's K and V for the answer: sequence seq_ids[0] of `cache` (a CrispCache) grows by the prompt,
-        once for all layers (at cache_layer 0), and this layer's part of it is written."""
+        once for all layers (at cache_layer 0), and this layer's part of it is written.  k and v hold the whole prompt."""
         if seq_ids.shape != (1,):
             raise ValueError("seq_ids must name one sequence")
+        cache.check_tokens(k, v, self.p.seq_len)   # before the sequence grows
         if cache_layer == 0:
             cache.reserve(seq_ids, self.n_tokens, stream)
         cache.append(k, v, seq_ids, layer=cache_layer, stream=stream)

@@ -507,6 +507,30 @@ def test_a_refused_reserve_stops_only_the_sequences_that_it_lists():
     both.check_contents()
 
 
+def test_a_prompt_that_is_not_the_layer_s_changes_nothing():
+    """k or v of another length, number of heads, type or place, or a layer that is not there: the sequence does not grow."""
+    from workloads import synth
+    both = Both("int8", 1, pages=8, max_seqs=2, max_pages=8, garbage=False)
+    both.grow([1], [30], 725)
+    q, k, v = synth.random_qkv(300, 4, 1, seed=5, device=DEV)
+    layer = crisp.CrispLayer(crisp.make_params(300, 4, 1, sink_tokens=4))
+    odd = torch.empty(300 * 128 + 1, dtype=torch.bfloat16, device=DEV)[1:].view(300, 1, 128)
+    for bad in ((k[:299], v[:299]), (k, v[:299]), (k, q), (k, v.float()), (k, v.cpu()),
+                (k.expand(300, 2, 128).contiguous(), v), (torch.cat([k, k]), torch.cat([v, v]))):
+        with pytest.raises(ValueError):
+            layer.store(*bad, both.gpu, i32([1]))
+    for bad, at in (((k, odd), 0), ((k, v), -1), ((k, v), 1)):
+        with pytest.raises(crisp.CrispError):
+            layer.store(*bad, both.gpu, i32([1]), cache_layer=at)
+    both.check_tables()
+    both.check_contents()
+    layer.store(k, v, both.gpu, i32([1]))
+    both.ref.reserve([1], [300])
+    both.ref.append(k.double().cpu().numpy(), v.double().cpu().numpy(), [1], [0, 300])
+    both.check_tables()
+    both.check_contents()
+
+
 def test_a_prompt_that_does_not_fit_overwrites_nothing():
     """CrispLayer.store onto a sequence that already holds as many tokens as the prompt has."""
     from workloads import synth
