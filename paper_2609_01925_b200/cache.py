@@ -213,11 +213,13 @@ class CrispCache:
             return torch.empty(shape, dtype=dtype, device=self.device)
 
     def poll(self, stream=None) -> None:
-        """Waits for the stream and raises the first error that the device has recorded since the last poll."""
+        """Waits for the stream and raises the first error that the device has recorded since the last poll: that of the
+        pages' calls, or attention's.  With one of each, the message names both."""
         if stream is None:
             stream = torch.cuda.current_stream(self.device)
         with torch.cuda.device(self.device):
-            status = [(name, B.crisp_poll_device_status(ws, stream))
-                      for ws, name in ((self.pages_ws, "pages"), (self.attention_ws, "attention"))]
-        for name, rc in status:
-            B.check(rc, f"cache status ({name})")
+            pages, attention = (B.crisp_poll_device_status(ws, stream) for ws in (self.pages_ws, self.attention_ws))
+        if pages != B.OK and attention != B.OK:
+            raise B.CrispError(pages, f"cache status (attention: {B.status_string(attention)} ({attention}); pages)")
+        B.check(pages, "cache status (pages)")
+        B.check(attention, "cache status (attention)")

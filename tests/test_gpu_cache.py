@@ -601,6 +601,19 @@ def test_attention_skips_what_breaks_its_rules():
         both.gpu.poll()
 
 
+def test_poll_names_the_errors_of_both_workspaces():
+    both = Both("e4m3", heads=1, pages=2, max_seqs=2, max_pages=2)
+    both.grow([0, 1], [128, 5], 741)
+    c = both.gpu
+    c.reserve(i32([0]))                                          # no page
+    c.attention(tokens(1, 4, 743).to(DEV), i32([9]))             # no such sequence
+    with pytest.raises(crisp.CrispError) as e:
+        c.poll()
+    assert e.value.status == B.ERR_NO_PAGES
+    assert B.status_string(B.ERR_NO_PAGES) in str(e.value) and B.status_string(B.ERR_BAD_CACHE) in str(e.value)
+    both.check_tables()
+
+
 @pytest.mark.parametrize("new,hq", [(1, 8), (4, 64)])
 def test_a_call_with_too_much_work_is_refused_as_such(new, hq):
     """Sixteen readers of a sequence of the greatest length, 8 KV heads: 2^31 pages of work.  All of its pages are one page."""
