@@ -597,9 +597,12 @@ cache_free_kernel(const CacheView c, const int32_t* __restrict__ seq_ids, int* s
   }
   if (threadIdx.x == 0) s_len = atomicExch(&c.seq_lens[s], 0);
   __syncthreads();
-  int len = s_len;
+  const int len = s_len;
   if (len < 0 || len > c.max_pages * kPage) {
-    if (threadIdx.x == 0) cache_fail(status, CRISP_ERR_BAD_CACHE);
+    if (threadIdx.x == 0) {
+      c.seq_lens[s] = len;  // what breaks its rule stays
+      cache_fail(status, CRISP_ERR_BAD_CACHE);
+    }
     return;
   }
   int* row = c.page_table + static_cast<size_t>(s) * c.max_pages;

@@ -601,6 +601,22 @@ def test_attention_skips_what_breaks_its_rules():
         both.gpu.poll()
 
 
+@pytest.mark.parametrize("length", [-5, 257, 1 << 30])
+def test_free_leaves_a_length_that_breaks_its_rule(length):
+    both = Both("e4m3", heads=1, pages=4, max_seqs=2, max_pages=2, garbage=False)
+    both.grow([0, 1], [128, 5], 745)
+    c = both.gpu
+    c.seq_lens[0] = length
+    before = [t.clone() for t in tensors(c)[:3]]
+    c.free(i32([0, 0]))
+    raises_at_poll(c, B.ERR_BAD_CACHE)
+    assert all(torch.equal(a, b) for a, b in zip(before, tensors(c)[:3]))       # table, lengths, references
+    c.seq_lens[0] = 128
+    c.free(i32([0, 0]))
+    both.ref.free([0])
+    both.check_tables()
+
+
 def test_poll_names_the_errors_of_both_workspaces():
     both = Both("e4m3", heads=1, pages=2, max_seqs=2, max_pages=2)
     both.grow([0, 1], [128, 5], 741)
