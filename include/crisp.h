@@ -351,6 +351,11 @@ int crisp_cache_append(const crisp_cache* c, int32_t layer, const int32_t* seq_i
  * behind the last item are left as they are.  A sequence may be listed more than once.  n_q_heads / n_kv_heads <= 16.
  * What lies behind a sequence's end, or is hidden from a row, does not reach it, NaN among the codes included; only a
  * NaN among a sequence's own cached V may reach every row of its items.
+ * Roundings: q in fp16 times a power of two per row (exact but for elements 2^-29 below the row's largest); codes exactly;
+ * logits, maxima and sums in fp32; a weight to 11 bits (one or a few tokens; in a unit of 2^-15 of the largest among 32
+ * neighbours, so down to 2^-29 of that) or, like the prompt's, to bf16 (longer pieces).  Weights reach 2^8 (2^40 where
+ * logits come near 2^30), and their products with V are summed before the division: that times V and the number of keys must
+ * stay within fp32.
  * The work of a call is counted in pages: each item has, for each KV head and each 256 rows (new tokens x query heads of the
  * head) of it, the pages that those rows see plus 4.  Where the sum over a kernel's items reaches 2^31 - 1, these are left as
  * they are and the status is CRISP_ERR_UNSUPPORTED.

@@ -837,10 +837,12 @@ int crisp_cache_attention(const crisp_cache* c, int32_t layer, const int32_t* se
   if (rc != CRISP_OK) return rc;
   const size_t decode_off = kWsHeader, prefill_off = cache_decode_ws(nullptr, decode_off);
   // Rows per KV head: an item's new tokens x the query heads of the KV head's group.  Up to 24 are three fragments of the
-  // kernel that reads the cache near HBM speed: a page takes an SM 0.8 to 1.0 us with 8 rows, 1.1 with 16, 1.8 with 24,
-  // where the tensor-core kernel takes 2.5 us for up to 128 rows and 3.3 for 256 (16 sequences of 8192 tokens, 32/8 heads).
+  // kernel that reads the cache near HBM speed: a page takes an SM 1.0 us with 8 rows, 1.2 with 16, 1.9 with 24,
+  // where the tensor-core kernel takes 2.7 us for up to 128 rows and 3.3 for 256 (16 sequences of 8192 tokens, 32/8 heads).
   // A batch of both kinds is split: its items of up to 8 rows (16 with larger groups) go to the first kernel, which costs
-  // about 5 us when there are none.
+  // about 5 us when there are none.  The bound serves answers of one token: the first kernel computes as many rows per item
+  // as its longest may have.  64 users beside a piece of 1024 tokens, up to 8192 cached, 32/8 heads, bound of 8 and of 24 rows:
+  // one or two tokens each 163 and 264 us, three to six tokens 390 and 272.
   const int group = n_q_heads / v.heads;
   const bool few = static_cast<long long>(b.max_new) * group <= kDecodeRows;
   const bool split = !few && b.cu != nullptr && b.batch > 1;

@@ -21,10 +21,12 @@
 //    shared-memory phase always touch eight different 16-byte banks of the 128-byte-swizzled tile.
 //  * Scales are one per page and head: K's multiplies the logits, V's the page's P V product (O is accumulated in
 //    fp32 per page, which also applies the running maximum's correction).
-// Measured: 4 sequences of 65k to 131k tokens, 32/8 heads, int8: 133 us, 6.0 TB/s (150 us once the board has settled at its
-// power cap's clock); 262144 tokens, 28/4 heads, e4m3: 56 us, of which about 10 are the start and the join; 32 sequences of
-// 1 to 8192 tokens: 22 us for 82 MB; 300 tokens, 4/1 heads: 7 us.  With 24 rows (five tokens, groups of four) a page costs
-// three times the products and softmax, and the latency of its chain bounds the kernel: 93 us for 224 MB.
+// Measured: 4 sequences of 65k to 131k tokens, 32/8 heads, int8: 134 us, 5.9 TB/s (151 us, 5.3 TB/s, once the board has settled
+// at its power cap's clock); 262144 tokens, 28/4 heads, e4m3: 57 us, of which about 10 are the start and the join; 32 sequences
+// of 1 to 8192 tokens: 22.5 us for 82 MB (24.7 settled); 300 tokens, 4/1 heads: 7 us.  With 24 rows (five tokens, groups of
+// four) a page costs three times the products and softmax, and the latency of its chain bounds the kernel: 98 us for 224 MB.
+// The weights' units cost 1 to 4 % (one exponential, one directed subtraction and four more instructions per row and page);
+// two exponentials, for both factors, instead of one cost 13 % with 24 rows.
 #include <cuda_fp16.h>
 
 #include "cache_codes.cuh"

@@ -6,7 +6,7 @@
 // counts per warp and step, in ballots).  A plan checks its whole batch before it changes anything.  Page contents
 // are moved by a second kernel over all SMs, which reads the plan's list of moves: a stream of 16 KB tiles (one page, one
 // KV head, K or V), bound by HBM.  Measured: branching 16 sequences four times each, 8 layers of 8 heads, 150 MB: 28 us with
-// the release of the old branches; a compaction that moves 426 MB (read + written): 76 us, 8 of them the plan; releasing 32
+// the release of the old branches; a compaction that moves 426 MB (read + written): 77 us, 8 of them the plan; releasing 32
 // sequences and reserving 32: 8 us.
 #include <cuda_fp8.h>
 

@@ -7,14 +7,19 @@
 //  * TMA brings half a page's codes (64 tokens, 8 KB) into a ring; four converter warps turn them into 16-bit operands
 //    in a second ring, in the 128-byte-swizzled layout the descriptors want.  Conversion is exact: K's codes become fp16 (a single
 //    instruction per pair for e4m3), V's values, code * scale, become bf16, whose exponent range holds every scale.
+//    Two pairs of warps share the halves by the slots of the rings (cache_ring.h).
 //    Rows of V behind the sequence's end become zero (their codes may be anything, NaN among it).
 //  * Q K^T is fp16: Q is brought to fp16 by a power of two per row (exact but for elements 2^-29 below the row's
 //    largest); that power and the page's K scale multiply the logits.  P V is bf16, P rounded to bf16 as in prefill.cu.
 // The work is cut into equal runs of pages, one per CTA, and partial results are joined (cache_split.cuh).
 //
-// What bounds it: 4650 cycles per page of 256 rows (2048 new tokens over 32768, 32/8 heads, e4m3: 1.10 ms, 0.97 PFLOP/s).
-// The softmax warps are busy for 4200 of them; the tensor pipe needs 2880 (its N = 64 products are bound by operand fetch)
-// and the shared memory port about 3100 (256 KB of operands, 96 KB of conversion, 32 KB of codes).  Tried and slower: two
+// P's 8 bits are the prompt kernel's, so that a piece answers like the prompt it continues; V is exact in bf16 in both formats.
+// (The kernel for few rows has 11 bits: fp16 P would want V's codes as fp16 and its scale elsewhere.)
+//
+// What bounds it: 4850 cycles per page of 256 rows (2048 new tokens over 32768, 32/8 heads, e4m3: 1.15 ms, 0.92 PFLOP/s; once
+// the board has settled at its power cap's clock 1.22 ms, 0.88 PFLOP/s).  Of 4650 in an earlier version the softmax warps were
+// busy for 4200; the tensor pipe needs 2880 (its N = 64 products are bound by operand fetch) and the shared memory port about
+// 3100 (256 KB of operands, 96 KB of conversion, 32 KB of codes).  Tried and slower, in that version (1.10 ms): two
 // warpgroups per tile, one for each half of the keys, with a shared running maximum (1180 us); Q K^T of whole pages behind
 // P V, with either (1360 to 1410 us: the chain from S to S is what it lengthens); pacing the two tiles' exponentials or
 // computing part of them on the FMA pipe (1125 to 1195 us).  Code size matters more than any of these: with the converters'
