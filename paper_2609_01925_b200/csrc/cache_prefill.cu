@@ -65,7 +65,7 @@ struct TileArgs {
   Partials w;
   Output out;
   int layer, group, tile_tokens;  // tile_tokens: 256 / group, the new tokens of a group of work
-  float scale_pow2, scale_rest;  // softmax scale x log2(e) = scale_pow2 x scale_rest, a power of two and 1/2 to 1
+  float scale_pow2, scale_rest;  // softmax scale x log2(e) = 2 scale_pow2 x scale_rest, a power of two and 1/2 to 1
   const __nv_bfloat16* q;
   int* status;
 };
@@ -297,7 +297,7 @@ cache_prefill_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_co
           const int ex = static_cast<int>(amax >> 7);        // 255: the row holds an infinity or NaN and stays one
           const int e = ex == 255 ? 0 : min(141 - ex, 126);  // the row's largest element lands in [2^14, 2^15)
           const float f = pow2i(e);
-          row_scale = a.scale_pow2 * pow2i(-e);
+          row_scale = a.scale_pow2 * pow2i(1 - e);
 #pragma unroll
           for (int c = 0; c < 16; ++c) {
             const uint32_t wd[4] = {x[c].x, x[c].y, x[c].z, x[c].w};
@@ -691,7 +691,7 @@ int launch_cache_prefill(const CacheView& v, int layer, const CacheBatch& b, int
   a.tile_tokens = kTileRows / a.group;
   int exponent;
   a.scale_rest = std::frexp(scale * kLog2e, &exponent);
-  a.scale_pow2 = std::ldexp(1.f, exponent);
+  a.scale_pow2 = std::ldexp(1.f, exponent - 1);
   a.q = static_cast<const __nv_bfloat16*>(q);
   a.out = Output{static_cast<__nv_bfloat16*>(o), lse, n_q_heads, a.group, b.n_tokens, 0.f};
   a.status = static_cast<int*>(ws);

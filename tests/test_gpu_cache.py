@@ -356,6 +356,20 @@ def test_layers_and_scale_and_repeats():
     assert (np.abs(o.double().cpu().numpy() - want) <= ref.tolerance(want, slack, 2.0 ** -11, 64)).all()
 
 
+@pytest.mark.parametrize("new", [2, 20])
+@pytest.mark.parametrize("scale,eq", [(1.5e38, -124), (3e-38, 120), (1e-44, 126)])
+def test_extreme_softmax_scales(scale, eq, new):
+    """The largest and the smallest scales, over queries that bring the logits back to ordinary size."""
+    both = Both("e4m3", 2, pages=8, max_seqs=1, max_pages=4)
+    both.grow([0], [300], 75)
+    q = (tokens(new, 4, 76) / 8).clamp(-1, 1) * 2.0 ** eq
+    lse = torch.empty(4, new, device=DEV)
+    o = both.gpu.attention(q.to(DEV), i32([0]), softmax_scale=scale, lse=lse)
+    both.gpu.poll()
+    scale = float(np.float32(scale))
+    check_rows(o, lse, both.ref.attention(q.double().numpy(), [0], [0, new], scale=scale), 2 * new)
+
+
 def test_same_call_same_bits_and_uniform_form():
     both = Both("e4m3", 2, pages=200, max_seqs=4, max_pages=100)
     both.grow([0, 1, 2], [9000, 300, 4000], 81)
