@@ -25,7 +25,7 @@
 // at its power cap's clock); 262144 tokens, 28/4 heads, e4m3: 57 us, of which about 10 are the start and the join; 32 sequences
 // of 1 to 8192 tokens: 22.5 us for 82 MB (24.7 settled); 300 tokens, 4/1 heads: 7 us.  With 24 rows (five tokens, groups of
 // four) a page costs three times the products and softmax, and the latency of its chain bounds the kernel: 98 us for 224 MB.
-// The weights' units cost 1 to 4 % (one exponential, one directed subtraction and four more instructions per row and page);
+// The weights' units cost 1 to 5 % (one exponential, one directed subtraction and four more instructions per row and page);
 // two exponentials, for both factors, instead of one cost 13 % with 24 rows.
 #include <cuda_fp16.h>
 
