@@ -10,7 +10,8 @@
  *   crisp_sparse_prefill exact softmax attention over the listed blocks, causal (Eq. 1)
  *   crisp_dense_prefill  the same kernel over every causal block (the dense baseline)
  * and, for what follows the prompt, a paged K/V cache held in 8 bits (crisp_cache_...; not part of the paper):
- * its pages, the quantising write of new K/V and causal attention over it.
+ * its pages, the quantising write of new K/V and causal attention over it.  Around the attention (not part of the paper either)
+ * crisp_rms_norm, crisp_quantize, crisp_matmul and crisp_rotary lead from hidden states to Q, K, V and from O back.
  *
  * Conventions shared by every entry point
  *   - Tensors are contiguous, row major, bf16: Q and O are [seq_len, n_q_heads, 128]; K and V are
@@ -386,6 +387,89 @@ int crisp_cache_free(const crisp_cache* c, const int32_t* seq_ids, int32_t count
  * *n_used (DEVICE int32) receives U: pages U .. n_pages - 1 are then free.
  */
 int crisp_cache_compact(const crisp_cache* c, int32_t* n_used, void* ws, size_t ws_bytes, void* cuda_stream);
+
+/*
+ * The way into and out of the attention of a layer (not part of the paper): the norm of the hidden states, their products
+ * with the weights in 8 bits, and the rotary positions.  For these calls a size may be 0 (nothing is launched); rows and
+ * columns are at most 2^28.
+ *
+ * Operand of a product: a matrix [n_rows][n_cols], n_cols a multiple of 16, as
+ *   codes  [n_rows][n_cols] e4m3 bytes, and
+ *   scales [n_rows][4 * ceil(n_cols / 512)] bytes: byte b of a row stands for 2^(b - 127) and belongs to its columns
+ *          128 b .. 128 b + 127; bytes behind the last block are 127 and are not used (they make rows of whole 32-bit words).
+ * An element is code * scale.  A scale is the smallest power of two >= 2^-126 that brings its block's largest finite
+ * magnitude within 448, codes are rounded to nearest, ties to even; infinities become the largest code, NaN stays NaN.
+ * All of these arrays are 16-byte aligned.
+ */
+
+/* Rows of bf16 x [n_rows][n_cols] as an operand: weights, once, or the output of attention. */
+int crisp_quantize(const void* x, int32_t n_rows, int32_t n_cols, void* codes, uint8_t* scales, void* cuda_stream);
+
+/*
+ * Root-mean-square norm of rows, with the residual's addition:
+ *   h = x + residual, rounded to bf16 and stored in `sum` (residual and sum both NULL: h = x)
+ *   y = h / sqrt(mean(h^2) + eps) * weight            (weight [n_cols] bf16, NULL: 1), the mean in fp32
+ * written either as bf16 `y` or as an operand, `codes` and `scales` (converted from fp32, not from bf16); the other is NULL.
+ * sum may be x or residual, and y may be x: rows are read before they are written.  n_cols is a multiple of 16, at most 32768.
+ */
+int crisp_rms_norm(const void* x, const void* residual, const void* weight, int32_t n_rows, int32_t n_cols, float eps,
+                   void* sum, void* y, void* codes, uint8_t* scales, void* cuda_stream);
+
+/*
+ * out[m][n] = sum_k A[m][k] W[n][k]: operand A [n_rows][n_cols] times the transpose of operand W [n_out][n_cols], bf16
+ * [n_rows][n_out].  Products and sums run on the tensor cores with fp32 accumulators; where there are few tiles, the columns
+ * are dealt to up to 8 CTAs, whose sums are added in their order, so that the same call gives the same bits.
+ * ws: crisp_matmul_workspace_bytes() bytes; only its status word is used (CRISP_ERR_DEVICE_TIMEOUT), which the calls do not
+ * clear: zero its first 256 bytes once.  Calls may share it, also at the same time.
+ */
+size_t crisp_matmul_workspace_bytes(void);
+int crisp_matmul(const void* codes, const uint8_t* scales, const void* w_codes, const uint8_t* w_scales, int32_t n_rows,
+                 int32_t n_out, int32_t n_cols, void* out, void* ws, size_t ws_bytes, void* cuda_stream);
+
+/*
+ * Rotary positions.  The first rotary_dim elements of a head are rotary_dim / 2 pairs, elements (i, i + rotary_dim / 2)
+ * (CRISP_ROTARY_HALF) or (2 i, 2 i + 1) (CRISP_ROTARY_INTERLEAVED); pair i of a token at position p turns by p f_i:
+ *   (a, b) -> magnitude (a cos - b sin, b cos + a sin);  the rest of the head is copied.
+ * crisp_rotary_init (HOST) fills a plan with f_i = theta^(-2 i / rotary_dim), scaled for lengths beyond the original one:
+ *   CRISP_ROTARY_PLAIN   as it is
+ *   CRISP_ROTARY_LINEAR  f_i / factor
+ *   CRISP_ROTARY_BASE    theta is multiplied by factor^(rotary_dim / (rotary_dim - 2))
+ *   CRISP_ROTARY_RAMP    c f_i + (1 - c) f_i / factor, where c falls linearly in i from 1 at the pair with `high` turns over
+ *                        original_len positions (rounded down) to 0 at the one with `low` turns (rounded up);
+ *                        magnitude 0.1 ln(factor) + 1
+ *   CRISP_ROTARY_BANDS   the same with c = (turns of the pair over original_len - low) / (high - low), within 0 and 1
+ * low and high: 0 for 1 and 32 (RAMP) or 1 and 4 (BANDS).  rotary_dim: a multiple of 16, at most 128; theta > 1, factor >= 1.
+ * turns[i] is f_i in turns per position, as a fraction of 2^64.  Angles are within 2^-24 turns, plus 2^-51 of the whole angle
+ * (f_i is computed in 64 bits): no precision is lost to the size of a position.
+ */
+#define CRISP_ROTARY_HALF 0
+#define CRISP_ROTARY_INTERLEAVED 1
+#define CRISP_ROTARY_PLAIN 0
+#define CRISP_ROTARY_LINEAR 1
+#define CRISP_ROTARY_BASE 2
+#define CRISP_ROTARY_RAMP 3
+#define CRISP_ROTARY_BANDS 4
+typedef struct crisp_rotary_plan {
+  int32_t struct_size;   /* = sizeof(crisp_rotary_plan); ABI guard */
+  int32_t rotary_dim;
+  int32_t layout;
+  float magnitude;       /* factor on what is rotated              */
+  uint64_t turns[64];
+} crisp_rotary_plan;
+int crisp_rotary_init(crisp_rotary_plan* plan, int32_t rotary_dim, int32_t layout, double theta, int32_t scaling,
+                      double factor, int32_t original_len, double low, double high);
+
+/*
+ * Rotates q and k and copies v, from rows of any stride into contiguous tensors as the attention calls take them.
+ *   q [n_tokens][n_q_heads][128], k and v [n_tokens][n_kv_heads][128] bf16; token t of q starts at element t * q_stride (a
+ *   multiple of 8, at least n_q_heads * 128), likewise k and v: the three may be parts of one product's rows.
+ *   Any of them may be NULL, together with its output.  An output may be its input if that is contiguous; other overlaps
+ *   are not allowed.
+ *   positions [n_tokens] int32 (DEVICE; any value); NULL: first_position + t.
+ */
+int crisp_rotary(const crisp_rotary_plan* plan, int32_t n_tokens, const int32_t* positions, int32_t first_position,
+                 int32_t n_q_heads, int32_t n_kv_heads, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                 const void* v, int64_t v_stride, void* q_out, void* k_out, void* v_out, void* cuda_stream);
 
 /*
  * Diagnostic (the paper has no counterpart): per-kernel device times of the stage calls, for benchmarks.

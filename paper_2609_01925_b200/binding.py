@@ -28,6 +28,8 @@ ERR_BAD_CACHE = -9
 PATTERN_PE, PATTERN_VS = 0, 1
 CACHE_E4M3, CACHE_INT8 = 0, 1
 CACHE_MAX_BATCH = 1024
+ROTARY_HALF, ROTARY_INTERLEAVED = 0, 1
+ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_BASE, ROTARY_RAMP, ROTARY_BANDS = range(5)
 
 EXPORTS = (
     "crisp_version", "crisp_status_string", "crisp_last_cuda_error", "crisp_workspace_bytes",
@@ -36,6 +38,7 @@ EXPORTS = (
     "crisp_forward_varlen", "crisp_selftest_bounded_wait", "crisp_profile_enable", "crisp_profile_read",
     "crisp_forward_host", "crisp_forward_host_stage_bytes", "crisp_cache_workspace_bytes", "crisp_cache_reserve",
     "crisp_cache_append", "crisp_cache_attention", "crisp_cache_fork", "crisp_cache_free", "crisp_cache_compact",
+    "crisp_quantize", "crisp_rms_norm", "crisp_matmul_workspace_bytes", "crisp_matmul", "crisp_rotary_init", "crisp_rotary",
 )
 
 
@@ -59,6 +62,14 @@ class CrispCacheDesc(ctypes.Structure):
         ("max_pages", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("k_codes", ctypes.c_void_p),
         ("v_codes", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
         ("page_table", ctypes.c_void_p), ("seq_lens", ctypes.c_void_p), ("page_refs", ctypes.c_void_p),
+    ]
+
+
+class CrispRotaryPlan(ctypes.Structure):
+    """Mirror of `crisp_rotary_plan` (include/crisp.h)."""
+    _fields_ = [
+        ("struct_size", ctypes.c_int32), ("rotary_dim", ctypes.c_int32), ("layout", ctypes.c_int32),
+        ("magnitude", ctypes.c_float), ("turns", ctypes.c_uint64 * 64),
     ]
 
 
@@ -148,6 +159,19 @@ def load() -> ctypes.CDLL:
     lib.crisp_cache_free.argtypes = [C, vp, i32, vp, sz, vp]
     lib.crisp_cache_compact.restype = ctypes.c_int
     lib.crisp_cache_compact.argtypes = [C, vp, vp, sz, vp]
+    lib.crisp_quantize.restype = ctypes.c_int
+    lib.crisp_quantize.argtypes = [vp, i32, i32, vp, vp, vp]
+    lib.crisp_rms_norm.restype = ctypes.c_int
+    lib.crisp_rms_norm.argtypes = [vp, vp, vp, i32, i32, ctypes.c_float, vp, vp, vp, vp, vp]
+    lib.crisp_matmul_workspace_bytes.restype = sz
+    lib.crisp_matmul_workspace_bytes.argtypes = []
+    lib.crisp_matmul.restype = ctypes.c_int
+    lib.crisp_matmul.argtypes = [vp, vp, vp, vp, i32, i32, i32, vp, vp, sz, vp]
+    R, f64 = ctypes.POINTER(CrispRotaryPlan), ctypes.c_double
+    lib.crisp_rotary_init.restype = ctypes.c_int
+    lib.crisp_rotary_init.argtypes = [R, i32, i32, f64, i32, f64, i32, f64, f64]
+    lib.crisp_rotary.restype = ctypes.c_int
+    lib.crisp_rotary.argtypes = [R, i32, vp, i32, i32, i32, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp]
     lib.crisp_poll_device_status.restype = ctypes.c_int
     lib.crisp_poll_device_status.argtypes = [vp, vp]
     _lib = lib
@@ -340,6 +364,43 @@ def crisp_cache_free(c, seq_ids, count, ws, stream=None) -> int:
 
 def crisp_cache_compact(c, n_used, ws, stream=None) -> int:
     return load().crisp_cache_compact(c, _ptr(n_used), _ptr(ws), _nbytes(ws), _stream(stream))
+
+
+def crisp_quantize(x, codes, scales, stream=None) -> int:
+    return load().crisp_quantize(_ptr(x), x.shape[0], x.shape[1], _ptr(codes), _ptr(scales), _stream(stream))
+
+
+def crisp_rms_norm(x, residual, weight, eps, sum_out, y, codes, scales, stream=None) -> int:
+    return load().crisp_rms_norm(_ptr(x), _ptr(residual), _ptr(weight), x.shape[0], x.shape[1], eps, _ptr(sum_out), _ptr(y),
+                                 _ptr(codes), _ptr(scales), _stream(stream))
+
+
+def crisp_matmul_workspace_bytes() -> int:
+    return load().crisp_matmul_workspace_bytes()
+
+
+def crisp_matmul(codes, scales, w_codes, w_scales, out, ws, stream=None) -> int:
+    return load().crisp_matmul(_ptr(codes), _ptr(scales), _ptr(w_codes), _ptr(w_scales), codes.shape[0], w_codes.shape[0],
+                               codes.shape[1], _ptr(out), _ptr(ws), _nbytes(ws), _stream(stream))
+
+
+def crisp_rotary_init(rotary_dim, layout, theta, scaling=ROTARY_PLAIN, factor=1.0, original_len=0, low=0.0,
+                      high=0.0) -> CrispRotaryPlan:
+    plan = CrispRotaryPlan()
+    check(load().crisp_rotary_init(ctypes.byref(plan), rotary_dim, layout, theta, scaling, factor, original_len, low, high),
+          "crisp_rotary_init")
+    return plan
+
+
+def crisp_rotary(plan, positions, first_position, q, k, v, q_out, k_out, v_out, stream=None) -> int:
+    """q, k, v: [tokens, heads, 128] with any stride between tokens, or None together with their outputs."""
+    def part(t):
+        return (None, 0) if t is None else (t.data_ptr(), t.stride(0))
+    some = next(t for t in (q, k, v) if t is not None)
+    heads = [0 if t is None else t.shape[1] for t in (q, k, v)]
+    return load().crisp_rotary(ctypes.byref(plan), some.shape[0], _ptr(positions), first_position, heads[0],
+                               heads[1] or heads[2], *part(q), *part(k), *part(v), _ptr(q_out), _ptr(k_out), _ptr(v_out),
+                               _stream(stream))
 
 
 def crisp_poll_device_status(ws, stream=None) -> int:

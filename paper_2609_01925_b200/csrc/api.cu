@@ -9,6 +9,7 @@
 
 #include "cache.cuh"
 #include "common.cuh"
+#include "operand.cuh"
 
 namespace crisp {
 
@@ -104,15 +105,15 @@ int make_tmap_bf16_nhd(CUtensorMap* out, const void* base, int n, int heads, int
   return CRISP_OK;
 }
 
-int make_tmap_codes(CUtensorMap* out, const void* base, size_t rows, int box_rows) {
+static int make_tmap_bytes(CUtensorMap* out, const void* base, size_t rows, size_t cols, int box_rows) {
   EncodeTiledFn enc = encode_fn();
   if (!enc) {
     set_cu_error("cuTensorMapEncodeTiled is not available (no CUDA driver?)");
     return CRISP_ERR_CUDA;
   }
-  const cuuint64_t dims[2] = {static_cast<cuuint64_t>(kHeadDim), static_cast<cuuint64_t>(rows)};
-  const cuuint64_t strides[1] = {static_cast<cuuint64_t>(kHeadDim)};
-  const cuuint32_t box[2] = {static_cast<cuuint32_t>(kHeadDim), static_cast<cuuint32_t>(box_rows)};
+  const cuuint64_t dims[2] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows)};
+  const cuuint64_t strides[1] = {static_cast<cuuint64_t>(cols)};
+  const cuuint32_t box[2] = {128, static_cast<cuuint32_t>(box_rows)};
   const cuuint32_t estr[2] = {1, 1};
   CUresult r = enc(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr,
                    CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
@@ -124,6 +125,14 @@ int make_tmap_codes(CUtensorMap* out, const void* base, size_t rows, int box_row
     return CRISP_ERR_CUDA;
   }
   return CRISP_OK;
+}
+
+int make_tmap_codes(CUtensorMap* out, const void* base, size_t rows, int box_rows) {
+  return make_tmap_bytes(out, base, rows, kHeadDim, box_rows);
+}
+
+int make_tmap_operand(CUtensorMap* out, const void* base, int rows, int cols, int box_rows) {
+  return make_tmap_bytes(out, base, static_cast<size_t>(rows), static_cast<size_t>(cols), box_rows);
 }
 
 // dense_only: the call runs dense attention alone, which is defined for every length >= 1 and reads none of
@@ -893,6 +902,117 @@ int crisp_cache_compact(const crisp_cache* c, int32_t* n_used, void* ws, size_t 
   if (rc == CRISP_OK) rc = check_pages_ws(v, ws, ws_bytes);
   if (rc != CRISP_OK) return rc;
   return launch_cache_compact(v, n_used, ws, static_cast<cudaStream_t>(cuda_stream));
+}
+
+// Sizes of an operand: whole vectors of 16 codes, scales of whole words.
+static int check_operand(int32_t n_rows, int32_t n_cols) {
+  if (n_rows < 0 || n_cols <= 0) return CRISP_ERR_INVALID_ARG;
+  return n_cols % 16 != 0 || n_cols > kMaxOperandSize || n_rows > kMaxOperandSize ? CRISP_ERR_UNSUPPORTED : CRISP_OK;
+}
+
+int crisp_quantize(const void* x, int32_t n_rows, int32_t n_cols, void* codes, uint8_t* scales, void* cuda_stream) {
+  const int rc = check_operand(n_rows, n_cols);
+  if (rc != CRISP_OK || n_rows == 0) return rc;
+  if (!x || !codes || !scales || !aligned16(x) || !aligned16(codes) || !aligned16(scales)) return CRISP_ERR_INVALID_ARG;
+  return launch_quantize(x, n_rows, n_cols, codes, scales, static_cast<cudaStream_t>(cuda_stream));
+}
+
+int crisp_rms_norm(const void* x, const void* residual, const void* weight, int32_t n_rows, int32_t n_cols, float eps,
+                   void* sum, void* y, void* codes, uint8_t* scales, void* cuda_stream) {
+  int rc = check_operand(n_rows, n_cols);
+  if (rc == CRISP_OK && (!(eps >= 0.f) || !std::isfinite(eps))) rc = CRISP_ERR_INVALID_ARG;
+  if (rc == CRISP_OK && n_cols > kMaxNormCols) rc = CRISP_ERR_UNSUPPORTED;
+  if (rc != CRISP_OK || n_rows == 0) return rc;
+  // either 16 bits or codes with their scales; a sum exactly where there is something to add
+  if (!x || (y != nullptr) == (codes != nullptr) || (codes != nullptr) != (scales != nullptr) ||
+      (residual != nullptr) != (sum != nullptr))
+    return CRISP_ERR_INVALID_ARG;
+  for (const void* p : {x, residual, weight, static_cast<const void*>(sum), static_cast<const void*>(y),
+                        static_cast<const void*>(codes), static_cast<const void*>(scales)})
+    if (!aligned16(p)) return CRISP_ERR_INVALID_ARG;
+  return launch_rms_norm(x, residual, weight, n_rows, n_cols, eps, sum, y, codes, scales,
+                         static_cast<cudaStream_t>(cuda_stream));
+}
+
+size_t crisp_matmul_workspace_bytes(void) { return kWsHeader; }
+
+int crisp_matmul(const void* codes, const uint8_t* scales, const void* w_codes, const uint8_t* w_scales, int32_t n_rows,
+                 int32_t n_out, int32_t n_cols, void* out, void* ws, size_t ws_bytes, void* cuda_stream) {
+  int rc = check_operand(n_rows, n_cols);
+  if (rc == CRISP_OK) rc = check_operand(n_out, n_cols);
+  if (rc != CRISP_OK || n_rows == 0 || n_out == 0) return rc;
+  if (!codes || !scales || !w_codes || !w_scales || !out || !ws) return CRISP_ERR_INVALID_ARG;
+  for (const void* p : {codes, static_cast<const void*>(scales), w_codes, static_cast<const void*>(w_scales),
+                        static_cast<const void*>(out)})
+    if (!aligned16(p)) return CRISP_ERR_INVALID_ARG;
+  if (!aligned16(ws) || ws_bytes < kWsHeader) return CRISP_ERR_WORKSPACE;
+  return launch_matmul(codes, scales, w_codes, w_scales, n_rows, n_out, n_cols, out, ws,
+                       static_cast<cudaStream_t>(cuda_stream));
+}
+
+int crisp_rotary_init(crisp_rotary_plan* plan, int32_t rotary_dim, int32_t layout, double theta, int32_t scaling,
+                      double factor, int32_t original_len, double low, double high) {
+  if (!plan || rotary_dim <= 0 || (layout != CRISP_ROTARY_HALF && layout != CRISP_ROTARY_INTERLEAVED))
+    return CRISP_ERR_INVALID_ARG;
+  if (scaling < CRISP_ROTARY_PLAIN || scaling > CRISP_ROTARY_BANDS) return CRISP_ERR_INVALID_ARG;
+  if (!(theta > 1.0) || !std::isfinite(theta) || !(factor >= 1.0) || !std::isfinite(factor)) return CRISP_ERR_INVALID_ARG;
+  const bool by_turns = scaling == CRISP_ROTARY_RAMP || scaling == CRISP_ROTARY_BANDS;
+  if (low == 0.0) low = 1.0;
+  if (high == 0.0) high = scaling == CRISP_ROTARY_RAMP ? 32.0 : 4.0;
+  if (by_turns && (original_len <= 0 || !(low > 0.0) || !(high > low) || !std::isfinite(high))) return CRISP_ERR_INVALID_ARG;
+  if (rotary_dim % 16 != 0 || rotary_dim > kHeadDim) return CRISP_ERR_UNSUPPORTED;
+  constexpr double kTwoPi = 6.283185307179586476925286766559;
+  const int pairs = rotary_dim / 2;
+  const double dim = rotary_dim;
+  plan->struct_size = static_cast<int32_t>(sizeof(crisp_rotary_plan));
+  plan->rotary_dim = rotary_dim;
+  plan->layout = layout;
+  plan->magnitude = scaling == CRISP_ROTARY_RAMP ? static_cast<float>(0.1 * std::log(factor) + 1.0) : 1.f;
+  if (scaling == CRISP_ROTARY_BASE) theta *= std::pow(factor, dim / (dim - 2.0));
+  // the pairs (not rounded to whole ones) that make `high` and `low` turns over the original length
+  const double at_high = dim * std::log(original_len / (kTwoPi * high)) / (2.0 * std::log(theta));
+  const double at_low = dim * std::log(original_len / (kTwoPi * low)) / (2.0 * std::log(theta));
+  const double first = std::fmax(std::floor(at_high), 0.0), last = std::fmin(std::ceil(at_low), dim - 1.0);
+  for (int i = 0; i < kHeadDim / 2; ++i) {
+    double f = i < pairs ? std::pow(theta, -2.0 * i / dim) : 0.0;
+    double keep = 1.0;   // share of the frequency as it was; the rest is divided by the factor
+    if (scaling == CRISP_ROTARY_LINEAR) keep = 0.0;
+    if (scaling == CRISP_ROTARY_RAMP) keep = 1.0 - (i - first) / std::fmax(last - first, 0.001);
+    if (scaling == CRISP_ROTARY_BANDS) keep = (original_len * f / kTwoPi - low) / (high - low);
+    keep = std::fmin(std::fmax(keep, 0.0), 1.0);
+    f = f * keep + f / factor * (1.0 - keep);
+    plan->turns[i] = static_cast<uint64_t>(std::ldexp(f / kTwoPi, 64) + 0.5);   // below 2^62
+  }
+  return CRISP_OK;
+}
+
+int crisp_rotary(const crisp_rotary_plan* plan, int32_t n_tokens, const int32_t* positions, int32_t first_position,
+                 int32_t n_q_heads, int32_t n_kv_heads, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                 const void* v, int64_t v_stride, void* q_out, void* k_out, void* v_out, void* cuda_stream) {
+  if (!plan || plan->struct_size != static_cast<int32_t>(sizeof(crisp_rotary_plan))) return CRISP_ERR_INVALID_ARG;
+  if (plan->rotary_dim <= 0 || (plan->layout != CRISP_ROTARY_HALF && plan->layout != CRISP_ROTARY_INTERLEAVED) ||
+      !std::isfinite(plan->magnitude))
+    return CRISP_ERR_INVALID_ARG;
+  if (plan->rotary_dim % 16 != 0 || plan->rotary_dim > kHeadDim) return CRISP_ERR_UNSUPPORTED;
+  if (n_tokens < 0 || n_q_heads < 0 || n_kv_heads < 0) return CRISP_ERR_INVALID_ARG;
+  if (n_tokens > kMaxOperandSize || n_q_heads > 65535 || n_kv_heads > 65535) return CRISP_ERR_UNSUPPORTED;
+  struct Tensor {
+    const void* in;
+    const void* out;
+    int64_t stride;
+    int32_t heads;
+  };
+  for (const Tensor& t : {Tensor{q, q_out, q_stride, n_q_heads}, Tensor{k, k_out, k_stride, n_kv_heads},
+                          Tensor{v, v_out, v_stride, n_kv_heads}}) {
+    if ((t.in != nullptr) != (t.out != nullptr) || !aligned16(t.in) || !aligned16(t.out)) return CRISP_ERR_INVALID_ARG;
+    if (!t.in) continue;
+    const int64_t row = static_cast<int64_t>(t.heads) * kHeadDim;
+    if (t.heads == 0 || t.stride < row || t.stride % 8 != 0 || t.stride > kMaxOperandSize) return CRISP_ERR_INVALID_ARG;
+    if (t.in == t.out && t.stride != row) return CRISP_ERR_INVALID_ARG;   // in place: the same rows
+  }
+  if (n_tokens == 0 || (!q && !k && !v)) return CRISP_OK;
+  return launch_rotary(*plan, n_tokens, positions, first_position, n_q_heads, n_kv_heads, q, q_stride, k, k_stride, v, v_stride,
+                       q_out, k_out, v_out, static_cast<cudaStream_t>(cuda_stream));
 }
 
 int crisp_poll_device_status(void* ws, void* cuda_stream) {
