@@ -11,8 +11,7 @@
 // the tensor core wants them in all four).
 #include <atomic>
 
-#include "cache.cuh"
-#include "operand.cuh"
+#include "matmul.cuh"
 #include "sm100_ptx.cuh"
 
 namespace crisp {
@@ -26,15 +25,6 @@ constexpr int kMaxStages = 12;
 constexpr int kScaleSlots = 4;         // words of scales (512 columns) in TMEM at a time
 constexpr int kMaxSplit = 8;           // CTAs of a cluster
 constexpr uint32_t kOnes = 0x7f7f7f7fu;  // four scales of one
-
-struct MatmulArgs {
-  const uint8_t *scales, *w_scales;
-  __nv_bfloat16* out;
-  int* status;
-  int n_rows, n_out, n_cols;
-  int tile_tokens;       // a multiple of 16, at most 256
-  int n_feature_tiles, split, stages, tmem_cols;
-};
 
 struct __align__(16) MatmulSmem {
   uint64_t full[kMaxStages], empty[kMaxStages], scale_full[kScaleSlots], scale_empty[kScaleSlots], done;
@@ -221,8 +211,6 @@ __global__ void __launch_bounds__(kMatmulThreads, 1) matmul_kernel(const __grid_
   }
 }
 
-int ceil_div(int a, int b) { return (a + b - 1) / b; }
-
 }  // namespace
 
 int launch_matmul(const void* codes, const uint8_t* scales, const void* w_codes, const uint8_t* w_scales, int n_rows,
@@ -235,11 +223,12 @@ int launch_matmul(const void* codes, const uint8_t* scales, const void* w_codes,
   a.n_rows = n_rows;
   a.n_out = n_out;
   a.n_cols = n_cols;
-  a.tile_tokens = n_rows >= 256 ? 256 : ceil_div(n_rows, 16) * 16;
-  a.n_feature_tiles = ceil_div(n_out, kTileFeatures);
   int n_sm = 0;
   int rc = current_sm_count(&n_sm);
   if (rc != CRISP_OK) return rc;
+  if (n_rows > 256) return launch_matmul_pair(a, codes, w_codes, 224, n_sm, stream);
+  a.tile_tokens = n_rows >= 256 ? 256 : ceil_div(n_rows, 16) * 16;
+  a.n_feature_tiles = ceil_div(n_out, kTileFeatures);
   const long long tiles = static_cast<long long>(a.n_feature_tiles) * ceil_div(n_rows, a.tile_tokens);
   const int blocks = ceil_div(n_cols, kScaleBlock);
   if (tiles > INT32_MAX) return CRISP_ERR_UNSUPPORTED;

@@ -1,0 +1,287 @@
+// The product of 8-bit operands for many rows: tiles of 256 features and up to 224 tokens, each computed by a pair of CTAs
+// (tcgen05, cta_group::2): either CTA holds the codes of 128 features and of half the tokens, so that a byte brought to an SM
+// serves twice as many products as it would for a CTA alone.  matmul.cu says how the scales get to the tensor core.
+//
+// The CTAs are persistent.  Roles: warps 0..3 write finished tiles, 4..7 bring scales to TMEM, 8 loads codes (TMA), 9 issues the
+// products (first CTA of the pair).  TMEM holds two tiles' accumulators, so that one is written while the other is computed.
+#include <atomic>
+
+#include "matmul.cuh"
+#include "sm100_ptx.cuh"
+
+namespace crisp {
+namespace {
+
+using namespace sm100;
+
+constexpr int kRows = 128;              // features of a CTA
+constexpr int kThreads = 320;
+constexpr int kMostTokens = 224;        // two accumulators and the scales fit TMEM's 512 columns
+constexpr int kStages = 6;
+constexpr int kSlots = 4;               // words of scales in TMEM at a time
+constexpr int kSlotCols = 12;           // 4 for the features, 8 for the tokens
+constexpr int kScaleColumn = 512 - kSlots * kSlotCols;
+static_assert(2 * kMostTokens <= kScaleColumn, "TMEM");
+constexpr uint32_t kOnes = 0x7f7f7f7fu;
+
+struct __align__(16) PairSmem {
+  uint64_t full[kStages], empty[kStages], scale_full[kSlots], scale_empty[kSlots], acc_full[2], acc_empty[2];
+  uint32_t words[2][4][3 * kRows];      // scales of four words' 128 features and 256 tokens
+  uint32_t tmem;
+  int abort_flag;
+};
+
+// Four words of a row's scales, those behind the end as ones.
+__device__ __forceinline__ void load_words(const uint8_t* scales, long long row, int rows, int words, int at, uint32_t (&w)[4]) {
+  const uint32_t* p = reinterpret_cast<const uint32_t*>(scales) + row * words + at;
+  if (row < rows && (words & 3) == 0) {
+    const uint4 v = *reinterpret_cast<const uint4*>(p);
+    w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = row < rows && at + i < words ? p[i] : kOnes;
+  }
+}
+
+__global__ void __launch_bounds__(kThreads, 1) matmul_pair_kernel(const __grid_constant__ CUtensorMap tw,
+                                                                  const __grid_constant__ CUtensorMap ta, const MatmulArgs a) {
+  extern __shared__ __align__(1024) uint8_t raw[];
+  __shared__ PairSmem s;
+  uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int rank = static_cast<int>(cluster_rank());
+  const long long pairs = gridDim.x / 2, first = blockIdx.x / 2;
+  const int blocks = (a.n_cols + kScaleBlock - 1) / kScaleBlock, words = (a.n_cols + kScaleWord - 1) / kScaleWord;
+  const int stage_bytes = (kRows + a.tile_tokens / 2) * kScaleBlock;
+  pdl_enter();
+  if (tid == 0) {
+    for (int i = 0; i < kStages; ++i) {
+      mbar_init(&s.full[i], 1);
+      mbar_init(&s.empty[i], 1);
+    }
+    for (int i = 0; i < kSlots; ++i) {
+      mbar_init(&s.scale_full[i], 8);
+      mbar_init(&s.scale_empty[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&s.acc_full[i], 1);
+      mbar_init(&s.acc_empty[i], 8);
+    }
+    s.abort_flag = 0;
+    fence_mbar_init();
+  }
+  if (warp == 9) {
+    tmem_alloc_pair(&s.tmem, 512);
+    tmem_relinquish_pair();
+    tc_fence_before_sync();
+  }
+  cluster_sync();   // both CTAs' barriers are ready
+  tc_fence_after_sync();
+  const uint32_t tm = s.tmem;
+  volatile int* abort_flag = &s.abort_flag;
+  auto place = [&](long long tile, int& f0, int& t0) {   // this CTA's first feature, the pair's first token
+    f0 = static_cast<int>(tile % a.n_feature_tiles) * (2 * kRows) + rank * kRows;
+    t0 = static_cast<int>(tile / a.n_feature_tiles) * a.tile_tokens;
+  };
+
+  if (warp == 8) {
+    if (lane == 0) {
+      prefetch_tmap(&tw);
+      prefetch_tmap(&ta);
+      int stage = 0;
+      uint32_t phase = 0;
+      bool ok = true, round0 = true;
+      for (long long tile = first; tile < a.n_tiles && ok; tile += pairs) {
+        int f0, t0;
+        place(tile, f0, t0);
+        t0 += rank * (a.tile_tokens / 2);
+        for (int kb = 0; kb < blocks; ++kb) {
+          if (!round0 && !(ok = mbar_wait(&s.empty[stage], phase ^ 1u, abort_flag))) break;
+          uint8_t* slot = ring + stage * stage_bytes;
+          const uint32_t bar = cluster_map(smem_u32(&s.full[stage]), 0);
+          // the first CTA's barrier counts both CTAs' bytes (the other's may land before it expects them: the phase cannot
+          // end without its arrival)
+          if (rank == 0) mbar_arrive_expect_tx(&s.full[stage], 2 * stage_bytes);
+          tma_load_2d_pair(slot, &tw, bar, kb * kScaleBlock, f0);
+          tma_load_2d_pair(slot + kRows * kScaleBlock, &ta, bar, kb * kScaleBlock, t0);
+          if (++stage == kStages) {
+            stage = 0;
+            phase ^= 1u;
+            round0 = false;
+          }
+        }
+      }
+    }
+    __syncwarp();
+  } else if (warp == 9) {
+    if (rank == 0 && lane == 0) {
+      int stage = 0, slot = 0, turn = 0;
+      uint32_t phase = 0, slot_phase = 0;
+      bool ok = true;
+      for (long long tile = first; tile < a.n_tiles && ok; tile += pairs, ++turn) {
+        const int buf = turn & 1;
+        if (turn >= 2) ok = mbar_wait_cluster(&s.acc_empty[buf], ((turn >> 1) - 1) & 1, abort_flag);
+        const uint32_t acc = tm + buf * kMostTokens;
+        for (int kb = 0; kb < blocks && ok; ++kb) {
+          if ((kb & 3) == 0) ok = ok && mbar_wait_cluster(&s.scale_full[slot], slot_phase, abort_flag);
+          ok = ok && mbar_wait_cluster(&s.full[stage], phase, abort_flag);
+          if (!ok) break;
+          tc_fence_after_sync();
+          const uint32_t at = smem_u32(ring + stage * stage_bytes);
+          const uint64_t wd = umma_desc_sw128(at, 0, 1024), ad = umma_desc_sw128(at + kRows * kScaleBlock, 0, 1024);
+          const uint32_t idesc = umma_idesc_mx_e4m3(2 * kRows, a.tile_tokens, kb & 3);
+          const uint32_t sc = tm + kScaleColumn + slot * kSlotCols;
+#pragma unroll
+          for (int i = 0; i < 4; ++i)   // 32 columns each
+            umma_mx_ss_pair(acc, wd + 2 * i, ad + 2 * i, idesc, sc, sc + 4, kb > 0 || i > 0);
+          umma_commit_pair(&s.empty[stage]);
+          if (++stage == kStages) {
+            stage = 0;
+            phase ^= 1u;
+          }
+          if ((kb & 3) == 3 || kb == blocks - 1) {
+            umma_commit_pair(&s.scale_empty[slot]);
+            if (++slot == kSlots) {
+              slot = 0;
+              slot_phase ^= 1u;
+            }
+          }
+        }
+        if (ok) umma_commit_pair(&s.acc_full[buf]);
+      }
+    }
+    __syncwarp();
+  } else if (warp >= 4) {
+    const int row = tid - 128;   // of the features, and of both halves of 256 tokens
+    const uint32_t quarter = tm + kScaleColumn + (static_cast<uint32_t>((warp & 3) * 32) << 16);
+    uint32_t next[3][4];
+    auto fetch = [&](long long tile, int word) {
+      int f0, t0;
+      place(tile, f0, t0);
+      load_words(a.w_scales, static_cast<long long>(f0) + row, a.n_out, words, word, next[0]);
+      load_words(a.scales, static_cast<long long>(t0) + row, a.n_rows, words, word, next[1]);
+      if (kRows + row < a.tile_tokens) load_words(a.scales, static_cast<long long>(t0) + kRows + row, a.n_rows, words, word, next[2]);
+    };
+    bool ok = true, round0 = true;
+    int slot = 0, side = 0;
+    uint32_t phase = 0;
+    if (first < a.n_tiles) fetch(first, 0);
+    // (after a wait that gave up the loops go on without their work, so that all four warps meet at every barrier)
+    for (long long tile = first; tile < a.n_tiles; tile += pairs) {
+      for (int word = 0; word < words; ++word) {
+        if ((word & 3) == 0) {
+          // each warp needs all rows' words: through shared memory (a side is free once everybody has come here again)
+          side ^= 1;
+#pragma unroll
+          for (int c = 0; c < 3; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s.words[side][i][c * kRows + row] = next[c][i];
+          named_bar_sync(1, 128);
+          if (word + 4 < words) {
+            fetch(tile, word + 4);
+          } else if (tile + pairs < a.n_tiles) {
+            fetch(tile + pairs, 0);
+          }
+        }
+        if (!round0) ok = ok && mbar_wait_warp(&s.scale_empty[slot], phase ^ 1u, abort_flag);
+        if (ok) {
+          tc_fence_after_sync();
+          uint32_t w[12];
+#pragma unroll
+          for (int c = 0; c < 12; ++c) w[c] = s.words[side][word & 3][32 * c + lane];
+          const uint32_t at = quarter + slot * kSlotCols;
+          tmem_st_x4(at, w);
+          tmem_st_x4(at + 4, w + 4);
+          tmem_st_x4(at + 8, w + 8);
+          tmem_st_wait();
+          tc_fence_before_sync();
+          __syncwarp();
+          if (lane == 0) cluster_arrive(cluster_map(smem_u32(&s.scale_full[slot]), 0));
+        }
+        if (++slot == kSlots) {
+          slot = 0;
+          phase ^= 1u;
+          round0 = false;
+        }
+      }
+    }
+  } else {
+    bool ok = true;
+    int turn = 0;
+    const uint32_t quarter = tm + (static_cast<uint32_t>(warp * 32) << 16);
+    const bool pairs_ok = (a.n_out & 1) == 0;   // two neighbouring features in one store
+    for (long long tile = first; tile < a.n_tiles && ok; tile += pairs, ++turn) {
+      int f0, t0;
+      place(tile, f0, t0);
+      const int buf = turn & 1, feature = f0 + warp * 32 + lane;
+      ok = mbar_wait_warp(&s.acc_full[buf], (turn >> 1) & 1, abort_flag);
+      if (!ok) break;
+      tc_fence_after_sync();
+      const int n_tokens = min(a.tile_tokens, a.n_rows - t0);
+      for (int c = 0; c < a.tile_tokens; c += 32) {
+        uint32_t v[32];
+        tmem_ld_x32(quarter + buf * kMostTokens + c, v);
+        tmem_ld_wait();
+        if (c + 32 >= a.tile_tokens) {
+          tc_fence_before_sync();
+          __syncwarp();
+          if (lane == 0) cluster_arrive(cluster_map(smem_u32(&s.acc_empty[buf]), 0));
+        }
+        if (pairs_ok) {
+          // even lanes write the even tokens' pair of features, odd lanes the odd tokens'
+          const bool odd = lane & 1;
+          __nv_bfloat16* out = a.out + static_cast<size_t>(t0 + c + odd) * a.n_out + (feature & ~1);
+#pragma unroll
+          for (int i = 0; i < 32; i += 2) {
+            const float mine = __uint_as_float(odd ? v[i + 1] : v[i]);
+            const float other = __shfl_xor_sync(0xffffffffu, __uint_as_float(odd ? v[i] : v[i + 1]), 1);
+            if (c + i + odd < n_tokens && feature < a.n_out)
+              *reinterpret_cast<uint32_t*>(out + static_cast<size_t>(i) * a.n_out) = odd ? pack_bf16(other, mine) : pack_bf16(mine, other);
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 32; ++i)
+            if (c + i < n_tokens && feature < a.n_out)
+              a.out[static_cast<size_t>(t0 + c + i) * a.n_out + feature] = __float2bfloat16_rn(__uint_as_float(v[i]));
+        }
+      }
+    }
+  }
+  tc_fence_before_sync();
+  __syncthreads();
+  if (tid == 0 && s.abort_flag) {
+    // given up: copies in flight still write to this CTA's shared memory, so give them time to land (bounded)
+    const unsigned long long from = global_timer_ns();
+    while (global_timer_ns() - from < kWaitLimitNs / 4) {
+    }
+    cache_fail(a.status, CRISP_ERR_DEVICE_TIMEOUT);
+  }
+  cluster_sync();   // nobody leaves while the other CTA's products read its shared memory or arrive on its barriers
+  if (warp == 9) {
+    tc_fence_after_sync();
+    tmem_dealloc_pair(tm, 512);
+  }
+}
+
+}  // namespace
+
+int launch_matmul_pair(MatmulArgs a, const void* codes, const void* w_codes, int tile_tokens, int n_sm, cudaStream_t stream) {
+  a.tile_tokens = tile_tokens;
+  a.n_feature_tiles = ceil_div(a.n_out, 2 * kRows);
+  a.n_tiles = static_cast<long long>(a.n_feature_tiles) * ceil_div(a.n_rows, tile_tokens);
+  constexpr size_t kSmem = kStages * (kRows + kMostTokens / 2) * kScaleBlock + 1024;
+  static_assert(kSmem + sizeof(PairSmem) + 1024 <= 228 * 1024, "shared memory of an SM");
+  CUtensorMap tw, ta;
+  int rc = make_tmap_operand(&tw, w_codes, a.n_out, a.n_cols, kRows);
+  if (rc == CRISP_OK) rc = make_tmap_operand(&ta, codes, a.n_rows, a.n_cols, tile_tokens / 2);
+  static std::atomic<unsigned long long> done{0};
+  if (rc == CRISP_OK) rc = allow_smem(reinterpret_cast<const void*>(&matmul_pair_kernel), kSmem, &done);
+  if (rc != CRISP_OK) return rc;
+  const long long pairs = a.n_tiles < n_sm / 2 ? a.n_tiles : n_sm / 2;
+  CRISP_KERNEL("matmul_pair", stream, launch_pdl_cluster(matmul_pair_kernel, dim3(static_cast<unsigned>(2 * pairs)), dim3(kThreads),
+                                                         kSmem, 2, stream, tw, ta, a));
+  CRISP_CUDA_TRY(cudaGetLastError(), "matmul: launch");
+  return CRISP_OK;
+}
+
+}  // namespace crisp
