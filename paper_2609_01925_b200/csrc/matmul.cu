@@ -20,11 +20,10 @@ namespace {
 using namespace sm100;
 
 constexpr int kTileFeatures = 128;
-constexpr int kMatmulThreads = 192;    // warps 0..3: scales, then the epilogue; 4: TMA; 5: MMA
+constexpr int kMatmulThreads = 224;    // warps 0..3: scales, then the epilogue; 4 and 5: TMA; 6: MMA
 constexpr int kMaxStages = 12;
 constexpr int kScaleSlots = 4;         // words of scales (512 columns) in TMEM at a time
 constexpr int kMaxSplit = 8;           // CTAs of a cluster
-constexpr uint32_t kOnes = 0x7f7f7f7fu;  // four scales of one
 
 struct __align__(16) MatmulSmem {
   uint64_t full[kMaxStages], empty[kMaxStages], scale_full[kScaleSlots], scale_empty[kScaleSlots], done;
@@ -32,26 +31,27 @@ struct __align__(16) MatmulSmem {
   int abort_flag;
 };
 
-__device__ __forceinline__ uint32_t scale_word(const uint8_t* scales, long long row, int rows, int words, int word) {
-  return row < rows ? *reinterpret_cast<const uint32_t*>(scales + (row * words + word) * 4) : kOnes;
-}
-
 __global__ void __launch_bounds__(kMatmulThreads, 1) matmul_kernel(const __grid_constant__ CUtensorMap tw,
                                                                    const __grid_constant__ CUtensorMap ta, const MatmulArgs a) {
   extern __shared__ __align__(1024) uint8_t raw[];
   __shared__ MatmulSmem s;
   uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~static_cast<uintptr_t>(1023));
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const int rank = a.split > 1 ? static_cast<int>(cluster_rank()) : 0;
   const int tile = blockIdx.x / a.split;
   const int f0 = (tile % a.n_feature_tiles) * kTileFeatures;
   const int t0 = (tile / a.n_feature_tiles) * a.tile_tokens;
   const int blocks = (a.n_cols + kScaleBlock - 1) / kScaleBlock, words = (a.n_cols + kScaleWord - 1) / kScaleWord;
-  const int k0 = static_cast<int>(static_cast<long long>(rank) * blocks / a.split);
-  const int k1 = static_cast<int>(static_cast<long long>(rank + 1) * blocks / a.split);
+  const int pairs = (blocks + 1) / 2;   // blocks are dealt in pairs
+  const int k0 = static_cast<int>(static_cast<long long>(rank) * pairs / a.split) * 2;
+  const int k1 = min(static_cast<int>(static_cast<long long>(rank + 1) * pairs / a.split) * 2, blocks);
   const int stage_bytes = (kTileFeatures + a.tile_tokens) * kScaleBlock;
   const int token_cells = (a.tile_tokens + 31) / 32;            // TMEM columns of the tokens' scales
   const int slot_cols = token_cells > 4 ? 12 : 8;
+  if (warp == 4 && elect_one()) {
+    // the weights set out for L2 while the kernel before this one ends
+    for (int kb = k0; kb < k1; ++kb) tma_prefetch_2d(&tw, kb * kScaleBlock, f0);
+  }
   pdl_enter();
   if (tid == 0) {
     for (int i = 0; i < a.stages; ++i) {
@@ -66,7 +66,7 @@ __global__ void __launch_bounds__(kMatmulThreads, 1) matmul_kernel(const __grid_
     s.abort_flag = 0;
     fence_mbar_init();
   }
-  if (warp == 5) {
+  if (warp == 6) {
     tmem_alloc(&s.tmem, a.tmem_cols);
     tmem_relinquish();
     tc_fence_before_sync();
@@ -76,82 +76,97 @@ __global__ void __launch_bounds__(kMatmulThreads, 1) matmul_kernel(const __grid_
   const uint32_t tm = s.tmem;
   volatile int* abort_flag = &s.abort_flag;
 
-  if (warp == 4) {
-    if (lane == 0) {
-      prefetch_tmap(&tw);
-      prefetch_tmap(&ta);
-      int stage = 0;
-      uint32_t phase = 0;
-      for (int kb = k0; kb < k1; ++kb) {
-        if (kb - k0 >= a.stages && !mbar_wait(&s.empty[stage], phase ^ 1u, abort_flag)) break;
+  // (Loads and products are issued by one elected lane of a warp that stays together, and two blocks at a time: see
+  // matmul_pair.cu.)
+  if (warp == 4 || warp == 5) {
+    int stage = warp - 4;
+    uint32_t phase = 0;
+    for (int kb = k0 + warp - 4; kb < k1; kb += 2) {
+      if (kb - k0 >= a.stages && !mbar_wait_warp(&s.empty[stage], phase ^ 1u, abort_flag)) break;
+      if (elect_one()) {
         uint8_t* slot = ring + stage * stage_bytes;
         mbar_arrive_expect_tx(&s.full[stage], stage_bytes);
         tma_load_2d(slot, &tw, &s.full[stage], kb * kScaleBlock, f0);
         tma_load_2d(slot + kTileFeatures * kScaleBlock, &ta, &s.full[stage], kb * kScaleBlock, t0);
-        if (++stage == a.stages) {
-          stage = 0;
-          phase ^= 1u;
-        }
+      }
+      if ((stage += 2) >= a.stages) {
+        stage -= a.stages;
+        phase ^= 1u;
       }
     }
-    __syncwarp();
-  } else if (warp == 5) {
-    if (lane == 0) {
-      int stage = 0, slot = 0;
-      uint32_t phase = 0, slot_phase = 0;
-      bool ok = true;
-      for (int kb = k0; kb < k1 && ok; ++kb) {
-        if (kb == k0 || (kb & 3) == 0) ok = mbar_wait(&s.scale_full[slot], slot_phase, abort_flag);
-        ok = ok && mbar_wait(&s.full[stage], phase, abort_flag);
-        if (!ok) break;
-        tc_fence_after_sync();
-        const uint32_t at = smem_u32(ring + stage * stage_bytes);
-        const uint64_t wd = umma_desc_sw128(at, 0, 1024), ad = umma_desc_sw128(at + kTileFeatures * kScaleBlock, 0, 1024);
-        const uint32_t idesc = umma_idesc_mx_e4m3(kTileFeatures, a.tile_tokens, kb & 3);
-        const uint32_t sc = tm + static_cast<uint32_t>(a.tile_tokens + 31) / 32 * 32 + slot * slot_cols;
+  } else if (warp == 6) {
+    int stage = 0, slot = 0;
+    uint32_t phase = 0, slot_phase = 0;
+    const uint32_t scale_base = tm + static_cast<uint32_t>(a.tile_tokens + 31) / 32 * 32;
+    for (int kb = k0; kb < k1; kb += 2) {
+      const bool two = kb + 1 < k1, word = kb == k0 || (kb & 3) == 0;   // k0 is even
+      const int stage1 = stage + 1 == a.stages ? 0 : stage + 1;
+      const uint32_t phase1 = phase ^ (stage1 == 0 ? 1u : 0u);
+      const bool ready = mbar_try_wait(&s.full[stage], phase) & (!two || mbar_try_wait(&s.full[stage1], phase1)) &
+                         (!word || mbar_try_wait(&s.scale_full[slot], slot_phase));
+      if (!__all_sync(0xffffffffu, ready)) {
+        if (!mbar_wait_warp(&s.full[stage], phase, abort_flag) || (two && !mbar_wait_warp(&s.full[stage1], phase1, abort_flag)) ||
+            (word && !mbar_wait_warp(&s.scale_full[slot], slot_phase, abort_flag)))
+          break;
+      }
+      tc_fence_after_sync();
+      const uint32_t at = smem_u32(ring + stage * stage_bytes), at1 = smem_u32(ring + stage1 * stage_bytes);
+      const uint64_t wd = umma_desc_sw128(at, 0, 1024), wd1 = umma_desc_sw128(at1, 0, 1024);
+      constexpr int kTokens = kTileFeatures * kScaleBlock >> 4;   // from a stage's weights to its tokens, in a descriptor
+      const uint32_t idesc = umma_idesc_mx_e4m3(kTileFeatures, a.tile_tokens, kb & 3);
+      const uint32_t idesc1 = umma_idesc_mx_e4m3(kTileFeatures, a.tile_tokens, (kb & 3) + 1);
+      const uint32_t sc = scale_base + slot * slot_cols;
+      const bool last = (kb & 2) != 0;   // of a word of scales
+      if (elect_one()) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)   // 32 columns each
-          umma_mx_ss(tm, wd + 2 * i, ad + 2 * i, idesc, sc, sc + 4, kb > k0 || i > 0);
+          umma_mx_ss(tm, wd + 2 * i, wd + kTokens + 2 * i, idesc, sc, sc + 4, kb > k0 || i > 0);
         umma_commit(&s.empty[stage]);
-        if (++stage == a.stages) {
-          stage = 0;
-          phase ^= 1u;
+        if (two) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) umma_mx_ss(tm, wd1 + 2 * i, wd1 + kTokens + 2 * i, idesc1, sc, sc + 4, 1);
+          umma_commit(&s.empty[stage1]);
         }
-        if ((kb & 3) == 3) {
-          umma_commit(&s.scale_empty[slot]);
-          if (++slot == kScaleSlots) {
-            slot = 0;
-            slot_phase ^= 1u;
-          }
-        }
+        if (last) umma_commit(&s.scale_empty[slot]);
+        if (kb + 2 >= k1) umma_commit(&s.done);
       }
-      if (ok) umma_commit(&s.done);
+      if ((stage += 2) >= a.stages) {
+        stage -= a.stages;
+        phase ^= 1u;
+      }
+      if (last && ++slot == kScaleSlots) {
+        slot = 0;
+        slot_phase ^= 1u;
+      }
     }
-    __syncwarp();
   } else {
     const uint32_t quarter = tm + (static_cast<uint32_t>(warp * 32) << 16);
     const uint32_t scale_base = quarter + (a.tile_tokens + 31) / 32 * 32;
-    uint32_t next[12];
-    auto fetch = [&](int word) {
-#pragma unroll
-      for (int c = 0; c < 4; ++c) next[c] = scale_word(a.w_scales, static_cast<long long>(f0) + 32 * c + lane, a.n_out, words, word);
-#pragma unroll
-      for (int c = 0; c < 8; ++c)
-        next[4 + c] = c < token_cells ? scale_word(a.scales, static_cast<long long>(t0) + 32 * c + lane, a.n_rows, words, word) : kOnes;
-    };
     const int w0 = k0 >> 2, w1 = (k1 + 3) >> 2;
+    uint32_t next[12][4];   // four words at a time: a fetch takes longer than four words' products
     bool ok = true;
-    fetch(w0);
     for (int word = w0; word < w1; ++word) {
       const int i = word - w0, slot = i % kScaleSlots;
+      if ((i & 3) == 0) {
+#pragma unroll
+        for (int c = 0; c < 12; ++c) {
+          if (c < 4) {
+            load_words(a.w_scales, static_cast<long long>(f0) + 32 * c + lane, a.n_out, words, word, next[c]);
+          } else if (c - 4 < token_cells) {
+            load_words(a.scales, static_cast<long long>(t0) + 32 * (c - 4) + lane, a.n_rows, words, word, next[c]);
+          }
+        }
+      }
       if (i >= kScaleSlots) ok = mbar_wait_warp(&s.scale_empty[slot], (i / kScaleSlots - 1) & 1, abort_flag);
       if (!ok) break;
       if (i >= kScaleSlots) tc_fence_after_sync();
       const uint32_t at = scale_base + slot * slot_cols;
-      tmem_st_x4(at, next);
-      tmem_st_x4(at + 4, next + 4);
-      if (slot_cols > 8) tmem_st_x4(at + 8, next + 8);
-      if (word + 1 < w1) fetch(word + 1);
+      uint32_t w[12];
+#pragma unroll
+      for (int c = 0; c < 12; ++c) w[c] = (i & 2) ? ((i & 1) ? next[c][3] : next[c][2]) : ((i & 1) ? next[c][1] : next[c][0]);
+      tmem_st_x4(at, w);
+      tmem_st_x4(at + 4, w + 4);
+      if (slot_cols > 8) tmem_st_x4(at + 8, w + 8);
       tmem_st_wait();
       tc_fence_before_sync();
       __syncwarp();
@@ -183,14 +198,37 @@ __global__ void __launch_bounds__(kMatmulThreads, 1) matmul_kernel(const __grid_
   }
   if (a.split > 1) {
     cluster_sync();   // every CTA's partial sums are in its shared memory
-    if (tid < kTileFeatures && f0 + tid < a.n_out) {
-      // the tokens are dealt to the CTAs; each sums its own in the order of the columns
-      const int n = min(a.tile_tokens, a.n_rows - t0);
-      const uint32_t mine = smem_u32(ring) + tid * 4;
-      for (int t = rank * n / a.split; t < (rank + 1) * n / a.split; ++t) {
-        float sum = 0.f;
-        for (int p = 0; p < a.split; ++p) sum += cluster_load(cluster_map(mine + t * (kTileFeatures * 4), p));
-        a.out[static_cast<size_t>(t0 + t) * a.n_out + f0 + tid] = __float2bfloat16_rn(sum);
+    // the tokens are dealt to the cluster's warps, a lane has four features; sums are taken in the order of the columns
+    constexpr int kWarps = kMatmulThreads / 32;
+    const int n = min(a.tile_tokens, a.n_rows - t0), step = kWarps * a.split;
+    const int feature = f0 + 4 * lane;
+    const uint32_t mine = smem_u32(ring) + lane * 16;
+    for (int t = warp * a.split + rank; t < n; t += 2 * step) {   // two at a time
+      float4 v[2][kMaxSplit];
+#pragma unroll
+      for (int p = 0; p < kMaxSplit; ++p)
+        if (p < a.split) {
+          const uint32_t from = cluster_map(mine, p);
+          v[0][p] = cluster_load4(from + t * (kTileFeatures * 4));
+          if (t + step < n) v[1][p] = cluster_load4(from + (t + step) * (kTileFeatures * 4));
+        }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int at = t + i * step;
+        if (at >= n) break;
+        float4 sum = v[i][0];
+#pragma unroll
+        for (int p = 1; p < kMaxSplit; ++p)
+          if (p < a.split) sum.x += v[i][p].x, sum.y += v[i][p].y, sum.z += v[i][p].z, sum.w += v[i][p].w;
+        __nv_bfloat16* out = a.out + static_cast<size_t>(t0 + at) * a.n_out + feature;
+        if ((a.n_out & 3) == 0) {
+          if (feature < a.n_out) *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16(sum.x, sum.y), pack_bf16(sum.z, sum.w));
+        } else {
+          const float f[4] = {sum.x, sum.y, sum.z, sum.w};
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (feature + j < a.n_out) out[j] = __float2bfloat16_rn(f[j]);
+        }
       }
     }
     cluster_sync();   // nobody leaves while its sums are read
@@ -205,9 +243,48 @@ __global__ void __launch_bounds__(kMatmulThreads, 1) matmul_kernel(const __grid_
     cache_fail(a.status, CRISP_ERR_DEVICE_TIMEOUT);
   }
   __syncthreads();
-  if (warp == 5) {
+  if (warp == 6) {
     tc_fence_after_sync();
     tmem_dealloc(tm, a.tmem_cols);
+  }
+}
+
+}  // namespace
+
+namespace {
+
+// How a product is cut, by estimates in ns of what was measured on one B200 (12 to 32 blocks of columns, 1 to 2048 rows).
+struct Plan {
+  int tile_tokens = 0, split = 0;   // split 0: the kernel for pairs of CTAs
+  long long ns = INT64_MAX;
+};
+
+bool is_wide(int tile_tokens) { return tile_tokens > 208; }   // wants all of an SM's TMEM
+
+// Tiles of 128 features, each block of columns in one of `split` CTAs.  A launch and an exchange take 3 and 0.8 us; a block takes
+// a CTA 185 ns with 16 tokens, 290 with 64, 520 with 128 and more (its loads' latency over the few stages of its ring); more
+// CTAs than SMs get in each other's way; the sums of a token are read across the cluster in 12 ns.
+void plan_split(int n_rows, int n_out, int blocks, int n_sm, int tile_tokens, Plan* best) {
+  const long long tiles = static_cast<long long>(ceil_div(n_out, kTileFeatures)) * ceil_div(n_rows, tile_tokens);
+  const long long block_ns = tile_tokens < 128 ? 150 + 11 * tile_tokens / 5 : 520;
+  for (int split = 1; split <= kMaxSplit && split <= (blocks + 1) / 2; split *= 2) {
+    // clusters do not span the SMs of two GPCs: up to 16 CTAs of four, or 32 of eight, find no place
+    const long long ctas = tiles * split, room = (is_wide(tile_tokens) ? 1 : 2) * n_sm - (split > 2 ? 4 * split : 0);
+    if (ctas > room && split > 1) break;
+    const long long rounds = (ctas + room - 1) / room;
+    const long long crowd = ctas > n_sm && rounds == 1 ? 100 * ctas / n_sm * ctas / n_sm : 100;
+    const long long ns = 3000 + (split > 1 ? 800 + 12 * tile_tokens : 0) + rounds * ceil_div(blocks, split) * block_ns * crowd / 100;
+    if (ns < best->ns) *best = Plan{tile_tokens, split, ns};
+  }
+}
+
+// Tiles of 256 features and up to 224 tokens, each in a pair of CTAs: 5 us, and 95 + 0.9 tokens ns for a block of a round.
+void plan_pairs(int n_rows, int n_out, int blocks, int n_sm, Plan* best) {
+  for (int tokens = 64; tokens <= kPairTokens; tokens += 16) {
+    const long long tiles = static_cast<long long>(ceil_div(n_out, 2 * kTileFeatures)) * ceil_div(n_rows, tokens);
+    const long long rounds = (tiles + n_sm / 2 - 1) / (n_sm / 2), ns = 5000 + rounds * blocks * (95 + 9 * tokens / 10);
+    if (ns < best->ns) *best = Plan{tokens, 0, ns};
+    if (n_rows <= tokens) break;
   }
 }
 
@@ -226,22 +303,31 @@ int launch_matmul(const void* codes, const uint8_t* scales, const void* w_codes,
   int n_sm = 0;
   int rc = current_sm_count(&n_sm);
   if (rc != CRISP_OK) return rc;
-  if (n_rows > 256) return launch_matmul_pair(a, codes, w_codes, 224, n_sm, stream);
-  a.tile_tokens = n_rows >= 256 ? 256 : ceil_div(n_rows, 16) * 16;
-  a.n_feature_tiles = ceil_div(n_out, kTileFeatures);
-  const long long tiles = static_cast<long long>(a.n_feature_tiles) * ceil_div(n_rows, a.tile_tokens);
   const int blocks = ceil_div(n_cols, kScaleBlock);
-  if (tiles > INT32_MAX) return CRISP_ERR_UNSUPPORTED;
-  int split = static_cast<int>(tiles >= n_sm ? 1 : n_sm / tiles);
-  if (split > kMaxSplit) split = kMaxSplit;
-  if (split > blocks) split = blocks;
-  a.split = split;
+  Plan plan;
+  if (n_rows > 64) plan_pairs(n_rows, n_out, blocks, n_sm, &plan);
+  if (n_rows <= 256) {
+    plan_split(n_rows, n_out, blocks, n_sm, ceil_div(n_rows, 16) * 16, &plan);
+  } else {
+    plan_split(n_rows, n_out, blocks, n_sm, 128, &plan);
+    plan_split(n_rows, n_out, blocks, n_sm, 256, &plan);
+  }
+  if (plan.split == 0) return launch_matmul_pair(a, codes, w_codes, plan.tile_tokens, n_sm, stream);
+  a.tile_tokens = plan.tile_tokens;
+  a.split = plan.split;
+  a.n_feature_tiles = ceil_div(n_out, kTileFeatures);
+  a.n_tiles = static_cast<long long>(a.n_feature_tiles) * ceil_div(n_rows, a.tile_tokens);
+  if (a.n_tiles > INT32_MAX / kMaxSplit) return CRISP_ERR_UNSUPPORTED;
   // accumulators, then the slots of scales; an SM holds one CTA of the wide tiles and two of the others, so that the CTAs of
-  // an SM never want more than its 512 columns
+  // an SM never want more than its 512 columns.  A CTA that has an SM to itself and much to read gets a longer ring (33 rows,
+  // 8192 x 8192 weights: 20.9 -> 16.9 us); with less to read room for the next call's CTAs is worth more (1 row, 6144 x 4096
+  // weights: 7.9 us with the long ring, 7.2 without).
   const int used = ceil_div(a.tile_tokens, 32) * 32 + kScaleSlots * (a.tile_tokens > 128 ? 12 : 8);
   a.tmem_cols = 32;
   while (a.tmem_cols < used) a.tmem_cols *= 2;
-  const int budget = (a.tmem_cols > 256 ? 200 : 104) * 1024, stage_bytes = (kTileFeatures + a.tile_tokens) * kScaleBlock;
+  const bool alone = a.n_tiles * a.split <= n_sm - (a.split > 2 ? 4 * a.split : 0);
+  const bool deep = is_wide(a.tile_tokens) || (alone && ceil_div(blocks, a.split) >= 24);
+  const int budget = (deep ? 200 : 104) * 1024, stage_bytes = (kTileFeatures + a.tile_tokens) * kScaleBlock;
   a.stages = budget / stage_bytes < kMaxStages ? budget / stage_bytes : kMaxStages;
   const size_t smem = budget + 1024;
   CUtensorMap tw, ta;
@@ -250,8 +336,8 @@ int launch_matmul(const void* codes, const uint8_t* scales, const void* w_codes,
   static std::atomic<unsigned long long> done{0};
   if (rc == CRISP_OK) rc = allow_smem(reinterpret_cast<const void*>(&matmul_kernel), 200 * 1024 + 1024, &done);
   if (rc != CRISP_OK) return rc;
-  CRISP_KERNEL("matmul", stream, launch_pdl_cluster(matmul_kernel, dim3(static_cast<unsigned>(tiles * split)),
-                                                    dim3(kMatmulThreads), smem, split, stream, tw, ta, a));
+  CRISP_KERNEL("matmul", stream, launch_pdl_cluster(matmul_kernel, dim3(static_cast<unsigned>(a.n_tiles * a.split)),
+                                                    dim3(kMatmulThreads), smem, a.split, stream, tw, ta, a));
   CRISP_CUDA_TRY(cudaGetLastError(), "matmul: launch");
   return CRISP_OK;
 }

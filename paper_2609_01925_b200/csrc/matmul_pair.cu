@@ -2,8 +2,8 @@
 // (tcgen05, cta_group::2): either CTA holds the codes of 128 features and of half the tokens, so that a byte brought to an SM
 // serves twice as many products as it would for a CTA alone.  matmul.cu says how the scales get to the tensor core.
 //
-// The CTAs are persistent.  Roles: warps 0..3 write finished tiles, 4..7 bring scales to TMEM, 8 loads codes (TMA), 9 issues the
-// products (first CTA of the pair).  TMEM holds two tiles' accumulators, so that one is written while the other is computed.
+// The CTAs are persistent.  Roles: warps 0..3 write finished tiles, 4..7 bring scales to TMEM, 8 and 9 load codes (TMA), 10
+// issues the products (first CTA of the pair).  TMEM holds two tiles' accumulators, so that one is written while the other is computed.
 #include <atomic>
 
 #include "matmul.cuh"
@@ -15,14 +15,12 @@ namespace {
 using namespace sm100;
 
 constexpr int kRows = 128;              // features of a CTA
-constexpr int kThreads = 320;
-constexpr int kMostTokens = 224;        // two accumulators and the scales fit TMEM's 512 columns
+constexpr int kThreads = 352;
 constexpr int kStages = 6;
 constexpr int kSlots = 4;               // words of scales in TMEM at a time
 constexpr int kSlotCols = 12;           // 4 for the features, 8 for the tokens
 constexpr int kScaleColumn = 512 - kSlots * kSlotCols;
-static_assert(2 * kMostTokens <= kScaleColumn, "TMEM");
-constexpr uint32_t kOnes = 0x7f7f7f7fu;
+static_assert(2 * kPairTokens <= kScaleColumn, "TMEM");
 
 struct __align__(16) PairSmem {
   uint64_t full[kStages], empty[kStages], scale_full[kSlots], scale_empty[kSlots], acc_full[2], acc_empty[2];
@@ -31,24 +29,12 @@ struct __align__(16) PairSmem {
   int abort_flag;
 };
 
-// Four words of a row's scales, those behind the end as ones.
-__device__ __forceinline__ void load_words(const uint8_t* scales, long long row, int rows, int words, int at, uint32_t (&w)[4]) {
-  const uint32_t* p = reinterpret_cast<const uint32_t*>(scales) + row * words + at;
-  if (row < rows && (words & 3) == 0) {
-    const uint4 v = *reinterpret_cast<const uint4*>(p);
-    w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = row < rows && at + i < words ? p[i] : kOnes;
-  }
-}
-
 __global__ void __launch_bounds__(kThreads, 1) matmul_pair_kernel(const __grid_constant__ CUtensorMap tw,
                                                                   const __grid_constant__ CUtensorMap ta, const MatmulArgs a) {
   extern __shared__ __align__(1024) uint8_t raw[];
   __shared__ PairSmem s;
   uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~static_cast<uintptr_t>(1023));
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const int rank = static_cast<int>(cluster_rank());
   const long long pairs = gridDim.x / 2, first = blockIdx.x / 2;
   const int blocks = (a.n_cols + kScaleBlock - 1) / kScaleBlock, words = (a.n_cols + kScaleWord - 1) / kScaleWord;
@@ -70,7 +56,7 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_pair_kernel(const __grid_c
     s.abort_flag = 0;
     fence_mbar_init();
   }
-  if (warp == 9) {
+  if (warp == 10) {
     tmem_alloc_pair(&s.tmem, 512);
     tmem_relinquish_pair();
     tc_fence_before_sync();
@@ -84,73 +70,93 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_pair_kernel(const __grid_c
     t0 = static_cast<int>(tile / a.n_feature_tiles) * a.tile_tokens;
   };
 
-  if (warp == 8) {
-    if (lane == 0) {
-      prefetch_tmap(&tw);
-      prefetch_tmap(&ta);
-      int stage = 0;
-      uint32_t phase = 0;
-      bool ok = true, round0 = true;
-      for (long long tile = first; tile < a.n_tiles && ok; tile += pairs) {
-        int f0, t0;
-        place(tile, f0, t0);
-        t0 += rank * (a.tile_tokens / 2);
-        for (int kb = 0; kb < blocks; ++kb) {
-          if (!round0 && !(ok = mbar_wait(&s.empty[stage], phase ^ 1u, abort_flag))) break;
+  // Loads and products are issued by one elected lane of a warp that stays together, so that descriptors and coordinates are
+  // known to be the warp's: from a branch of one thread a product takes 100 to 190 cycles to issue, and 39 to 128 to compute.
+  if (warp == 8 || warp == 9) {
+    // Two loading warps take turns: the copies of one follow one another, 16 KB in 200 ns, those of two run side by side.
+    int stage = warp - 8;
+    uint32_t phase = 0;
+    long long step = warp - 8;   // blocks of all tiles, counted through
+    bool ok = true;
+    long long base = 0;          // step at which the tile began
+    for (long long tile = first; tile < a.n_tiles && ok; tile += pairs, base += blocks) {
+      int f0, t0;
+      place(tile, f0, t0);
+      t0 += rank * (a.tile_tokens / 2);
+      for (; step < base + blocks; step += 2) {
+        if (step >= kStages && !(ok = mbar_wait_warp(&s.empty[stage], phase ^ 1u, abort_flag))) break;
+        const int column = static_cast<int>(step - base) * kScaleBlock;
+        if (elect_one()) {
           uint8_t* slot = ring + stage * stage_bytes;
           const uint32_t bar = cluster_map(smem_u32(&s.full[stage]), 0);
           // the first CTA's barrier counts both CTAs' bytes (the other's may land before it expects them: the phase cannot
           // end without its arrival)
           if (rank == 0) mbar_arrive_expect_tx(&s.full[stage], 2 * stage_bytes);
-          tma_load_2d_pair(slot, &tw, bar, kb * kScaleBlock, f0);
-          tma_load_2d_pair(slot + kRows * kScaleBlock, &ta, bar, kb * kScaleBlock, t0);
-          if (++stage == kStages) {
-            stage = 0;
-            phase ^= 1u;
-            round0 = false;
-          }
+          tma_load_2d_pair(slot, &tw, bar, column, f0);
+          tma_load_2d_pair(slot + kRows * kScaleBlock, &ta, bar, column, t0);
+        }
+        if ((stage += 2) >= kStages) {
+          stage -= kStages;
+          phase ^= 1u;
         }
       }
     }
-    __syncwarp();
-  } else if (warp == 9) {
-    if (rank == 0 && lane == 0) {
+  } else if (warp == 10) {
+    if (rank == 0) {
+      // Two blocks at a time: a wait, a fence and a commit take about 50 cycles each between products.
       int stage = 0, slot = 0, turn = 0;
       uint32_t phase = 0, slot_phase = 0;
       bool ok = true;
       for (long long tile = first; tile < a.n_tiles && ok; tile += pairs, ++turn) {
         const int buf = turn & 1;
-        if (turn >= 2) ok = mbar_wait_cluster(&s.acc_empty[buf], ((turn >> 1) - 1) & 1, abort_flag);
-        const uint32_t acc = tm + buf * kMostTokens;
-        for (int kb = 0; kb < blocks && ok; ++kb) {
-          if ((kb & 3) == 0) ok = ok && mbar_wait_cluster(&s.scale_full[slot], slot_phase, abort_flag);
-          ok = ok && mbar_wait_cluster(&s.full[stage], phase, abort_flag);
-          if (!ok) break;
+        if (turn >= 2) ok = mbar_wait_warp(&s.acc_empty[buf], ((turn >> 1) - 1) & 1, abort_flag);
+        const uint32_t acc = tm + buf * kPairTokens;
+        for (int kb = 0; kb < blocks && ok; kb += 2) {
+          const bool two = kb + 1 < blocks, word = (kb & 3) == 0;
+          const int stage1 = stage + 1 == kStages ? 0 : stage + 1;
+          const uint32_t phase1 = phase ^ (stage1 == 0 ? 1u : 0u);
+          const bool ready = mbar_try_wait(&s.full[stage], phase) & (!two || mbar_try_wait(&s.full[stage1], phase1)) &
+                             (!word || mbar_try_wait(&s.scale_full[slot], slot_phase));
+          if (!__all_sync(0xffffffffu, ready)) {
+            ok = mbar_wait_warp(&s.full[stage], phase, abort_flag) &&
+                 (!two || mbar_wait_warp(&s.full[stage1], phase1, abort_flag)) &&
+                 (!word || mbar_wait_warp(&s.scale_full[slot], slot_phase, abort_flag));
+            if (!ok) break;
+          }
           tc_fence_after_sync();
-          const uint32_t at = smem_u32(ring + stage * stage_bytes);
-          const uint64_t wd = umma_desc_sw128(at, 0, 1024), ad = umma_desc_sw128(at + kRows * kScaleBlock, 0, 1024);
+          const uint32_t at = smem_u32(ring + stage * stage_bytes), at1 = smem_u32(ring + stage1 * stage_bytes);
+          const uint64_t wd = umma_desc_sw128(at, 0, 1024), wd1 = umma_desc_sw128(at1, 0, 1024);
+          constexpr int kTokens = kRows * kScaleBlock >> 4;   // from a stage's weights to its tokens, in a descriptor
           const uint32_t idesc = umma_idesc_mx_e4m3(2 * kRows, a.tile_tokens, kb & 3);
+          const uint32_t idesc1 = umma_idesc_mx_e4m3(2 * kRows, a.tile_tokens, (kb & 3) + 1);
           const uint32_t sc = tm + kScaleColumn + slot * kSlotCols;
+          const bool end = kb + 2 >= blocks, last = (kb & 2) != 0 || end;   // of a word of scales
+          if (elect_one()) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i)   // 32 columns each
-            umma_mx_ss_pair(acc, wd + 2 * i, ad + 2 * i, idesc, sc, sc + 4, kb > 0 || i > 0);
-          umma_commit_pair(&s.empty[stage]);
-          if (++stage == kStages) {
+            for (int i = 0; i < 4; ++i)   // 32 columns each
+              umma_mx_ss_pair(acc, wd + 2 * i, wd + kTokens + 2 * i, idesc, sc, sc + 4, kb > 0 || i > 0);
+            umma_commit_pair(&s.empty[stage]);
+            if (two) {
+#pragma unroll
+              for (int i = 0; i < 4; ++i) umma_mx_ss_pair(acc, wd1 + 2 * i, wd1 + kTokens + 2 * i, idesc1, sc, sc + 4, 1);
+              umma_commit_pair(&s.empty[stage1]);
+            }
+            if (last) umma_commit_pair(&s.scale_empty[slot]);
+            if (end) umma_commit_pair(&s.acc_full[buf]);
+          }
+          stage = stage1;
+          phase = phase1;
+          if (two && ++stage == kStages) {
             stage = 0;
             phase ^= 1u;
           }
-          if ((kb & 3) == 3 || kb == blocks - 1) {
-            umma_commit_pair(&s.scale_empty[slot]);
-            if (++slot == kSlots) {
-              slot = 0;
-              slot_phase ^= 1u;
-            }
+          if (last && ++slot == kSlots) {
+            slot = 0;
+            slot_phase ^= 1u;
           }
         }
-        if (ok) umma_commit_pair(&s.acc_full[buf]);
       }
     }
-    __syncwarp();
   } else if (warp >= 4) {
     const int row = tid - 128;   // of the features, and of both halves of 256 tokens
     const uint32_t quarter = tm + kScaleColumn + (static_cast<uint32_t>((warp & 3) * 32) << 16);
@@ -220,7 +226,7 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_pair_kernel(const __grid_c
       const int n_tokens = min(a.tile_tokens, a.n_rows - t0);
       for (int c = 0; c < a.tile_tokens; c += 32) {
         uint32_t v[32];
-        tmem_ld_x32(quarter + buf * kMostTokens + c, v);
+        tmem_ld_x32(quarter + buf * kPairTokens + c, v);
         tmem_ld_wait();
         if (c + 32 >= a.tile_tokens) {
           tc_fence_before_sync();
@@ -257,7 +263,7 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_pair_kernel(const __grid_c
     cache_fail(a.status, CRISP_ERR_DEVICE_TIMEOUT);
   }
   cluster_sync();   // nobody leaves while the other CTA's products read its shared memory or arrive on its barriers
-  if (warp == 9) {
+  if (warp == 10) {
     tc_fence_after_sync();
     tmem_dealloc_pair(tm, 512);
   }
@@ -269,7 +275,7 @@ int launch_matmul_pair(MatmulArgs a, const void* codes, const void* w_codes, int
   a.tile_tokens = tile_tokens;
   a.n_feature_tiles = ceil_div(a.n_out, 2 * kRows);
   a.n_tiles = static_cast<long long>(a.n_feature_tiles) * ceil_div(a.n_rows, tile_tokens);
-  constexpr size_t kSmem = kStages * (kRows + kMostTokens / 2) * kScaleBlock + 1024;
+  constexpr size_t kSmem = kStages * (kRows + kPairTokens / 2) * kScaleBlock + 1024;
   static_assert(kSmem + sizeof(PairSmem) + 1024 <= 228 * 1024, "shared memory of an SM");
   CUtensorMap tw, ta;
   int rc = make_tmap_operand(&tw, w_codes, a.n_out, a.n_cols, kRows);

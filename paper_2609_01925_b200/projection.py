@@ -25,7 +25,10 @@ _SCALINGS = {"none": B.ROTARY_PLAIN, "linear": B.ROTARY_LINEAR, "base": B.ROTARY
              "bands": B.ROTARY_BANDS}
 
 
-# ---- what the calls below share
+# ---- what the calls below share (an answer calls them several times per layer and token: the way to the library is short)
+_BF16 = torch.bfloat16
+
+
 def _check(name, t, dtype, device, shape=None):
     """Pointer of a contiguous tensor of that type, place and shape."""
     if t.dtype is not dtype or t.device != device or not t.is_contiguous():
@@ -36,12 +39,13 @@ def _check(name, t, dtype, device, shape=None):
 
 
 def _rows(name, t, dtype):
-    """Device and shape of a matrix of that type."""
-    if t.device.type != "cuda":
+    """Shape of a matrix of that type."""
+    if not t.is_cuda:
         raise RuntimeError(f"{name} must be a CUDA tensor (no CPU fallback)")
-    if t.dim() != 2 or t.dtype is not dtype or not t.is_contiguous():
+    shape = t.shape
+    if len(shape) != 2 or t.dtype is not dtype or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {dtype} matrix")
-    return t.device, t.shape[0], t.shape[1]
+    return shape
 
 
 def _scale_cols(cols):
@@ -55,24 +59,22 @@ def _torch_stream(stream, device):
     return torch.cuda.ExternalStream(stream, device=device) if stream else torch.cuda.default_stream(device)
 
 
-def _new(shape, dtype, device, stream):
-    """An output, allocated on the stream that will write it."""
+def _new(like, shape, dtype, stream):
+    """An output beside `like`, allocated on the stream that will write it."""
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    with torch.cuda.stream(_torch_stream(stream, device)):
-        return torch.empty(shape, dtype=dtype, device=device)
+        return like.new_empty(shape, dtype=dtype)
+    with torch.cuda.stream(_torch_stream(stream, like.device)):
+        return like.new_empty(shape, dtype=dtype)
 
 
 def _call(name, device, stream, args, tensors):
     """The C call of that name on (*args, stream), with the tensors' device current."""
-    index = device.index
-    raw = stream
+    function, index = getattr(B.load(), name), device.index
     if stream is None:
         raw = torch._C._cuda_getCurrentRawStream(index)
-    elif not isinstance(stream, int):
-        raw = stream.cuda_stream
-    function = getattr(B.load(), name)
-    if torch.cuda.current_device() == index:
+    else:
+        raw = stream if isinstance(stream, int) else stream.cuda_stream
+    if torch._C._cuda_getDevice() == index:
         rc = function(*args, raw)
     else:
         with torch.cuda.device(index):
@@ -89,47 +91,49 @@ def _call(name, device, stream, args, tensors):
 # ---- rows
 def quantize(x, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """bf16 [rows, columns] as an operand (codes, scales): weights, once, or the output of attention."""
-    device, rows, cols = _rows("x", x, torch.bfloat16)
-    codes = _new((rows, cols), CODES, device, stream)
-    scales = _new((rows, _scale_cols(cols)), SCALES, device, stream)
-    _call("crisp_quantize", device, stream, (x.data_ptr(), rows, cols, codes.data_ptr(), scales.data_ptr()), (x, codes, scales))
+    rows, cols = _rows("x", x, _BF16)
+    codes = _new(x, (rows, cols), CODES, stream)
+    scales = _new(x, (rows, _scale_cols(cols)), SCALES, stream)
+    _call("crisp_quantize", x.device, stream, (x.data_ptr(), rows, cols, codes.data_ptr(), scales.data_ptr()), (x, codes, scales))
     return codes, scales
 
 
-def _norm(x, weight, residual, eps, sum_out, stream, quantized):
-    device, rows, cols = _rows("x", x, torch.bfloat16)
-    w = r = total = y = codes = scales = None
-    if weight is not None:
-        w = _check("weight", weight, torch.bfloat16, device, (cols,))
-    if residual is not None:
-        r = _check("residual", residual, torch.bfloat16, device, x.shape)
-        if sum_out is None:
-            sum_out = _new(x.shape, torch.bfloat16, device, stream)
-        total = _check("sum_out", sum_out, torch.bfloat16, device, x.shape)
-    elif sum_out is not None:
-        raise ValueError("sum_out belongs to a residual")
-    if quantized:
-        codes = _new((rows, cols), CODES, device, stream)
-        scales = _new((rows, _scale_cols(cols)), SCALES, device, stream)
-        out = (None, codes.data_ptr(), scales.data_ptr())
-    else:
-        y = _new((rows, cols), torch.bfloat16, device, stream)
-        out = (y.data_ptr(), None, None)
-    _call("crisp_rms_norm", device, stream, (x.data_ptr(), r, w, rows, cols, eps, total, *out),
-          (x, weight, residual, sum_out, y, codes, scales))
-    return (codes, scales, sum_out) if quantized else (y, sum_out)
+def _norm_inputs(x, weight, residual, sum_out, stream):
+    """(rows, columns, pointers of residual, weight and sum, sum)."""
+    rows, cols = _rows("x", x, _BF16)
+    device = x.device
+    w = None if weight is None else _check("weight", weight, _BF16, device, (cols,))
+    if residual is None:
+        if sum_out is not None:
+            raise ValueError("sum_out belongs to a residual")
+        return rows, cols, None, w, None, None
+    r = _check("residual", residual, _BF16, device, (rows, cols))
+    if sum_out is None:
+        sum_out = _new(x, (rows, cols), _BF16, stream)
+        return rows, cols, r, w, sum_out.data_ptr(), sum_out
+    return rows, cols, r, w, _check("sum_out", sum_out, _BF16, device, (rows, cols)), sum_out
 
 
 def rms_norm(x, weight=None, residual=None, *, eps: float = 1e-5, sum_out: Optional[torch.Tensor] = None, stream=None):
     """Root-mean-square norm of bf16 rows: h = x + residual (rounded to bf16; without one h is x),
     y = h / sqrt(mean(h^2) + eps) * weight.  Returns (y, h), h None without a residual.  sum_out: where h goes; it may be x
     or residual."""
-    return _norm(x, weight, residual, eps, sum_out, stream, False)
+    rows, cols, r, w, total, h = _norm_inputs(x, weight, residual, sum_out, stream)
+    y = _new(x, (rows, cols), _BF16, stream)
+    _call("crisp_rms_norm", x.device, stream, (x.data_ptr(), r, w, rows, cols, eps, total, y.data_ptr(), None, None),
+          (x, weight, residual, h, y))
+    return y, h
 
 
 def rms_norm_quantize(x, weight=None, residual=None, *, eps: float = 1e-5, sum_out: Optional[torch.Tensor] = None, stream=None):
     """rms_norm with y as an operand of a product: returns (codes, scales, h)."""
-    return _norm(x, weight, residual, eps, sum_out, stream, True)
+    rows, cols, r, w, total, h = _norm_inputs(x, weight, residual, sum_out, stream)
+    codes = _new(x, (rows, cols), CODES, stream)
+    scales = _new(x, (rows, _scale_cols(cols)), SCALES, stream)
+    _call("crisp_rms_norm", x.device, stream,
+          (x.data_ptr(), r, w, rows, cols, eps, total, None, codes.data_ptr(), scales.data_ptr()),
+          (x, weight, residual, h, codes, scales))
+    return codes, scales, h
 
 
 # ---- products
@@ -137,7 +141,8 @@ class CrispLinear:
     """Weights [out_features, in_features] as an operand, and products with them."""
 
     def __init__(self, codes, scales):
-        self.device, self.n_out, self.n_in = _rows("codes", codes, CODES)
+        self.n_out, self.n_in = _rows("codes", codes, CODES)
+        self.device, self._cols = codes.device, _scale_cols(self.n_in)
         _check("scales", scales, SCALES, self.device, (self.n_out, _scale_cols(self.n_in)))
         self.codes, self.scales = codes, scales
         self.ws = torch.zeros(B.crisp_matmul_workspace_bytes(), dtype=torch.uint8, device=self.device)
@@ -150,13 +155,16 @@ class CrispLinear:
 
     def __call__(self, codes, scales, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         """bf16 [rows, out_features]: the operand's rows times the transposed weights."""
-        device, rows, cols = _rows("codes", codes, CODES)
-        if device != self.device or cols != self.n_in:
-            raise ValueError(f"codes must have {self.n_in} columns and be on {self.device}")
-        ps = _check("scales", scales, SCALES, device, (rows, _scale_cols(cols)))
+        rows, cols = _rows("codes", codes, CODES)
+        device = self.device
+        if cols != self.n_in or codes.device != device:
+            raise ValueError(f"codes must have {self.n_in} columns and be on {device}")
+        ps = _check("scales", scales, SCALES, device, (rows, self._cols))
         if out is None:
-            out = _new((rows, self.n_out), torch.bfloat16, device, stream)
-        po = _check("out", out, torch.bfloat16, device, (rows, self.n_out))
+            out = _new(codes, (rows, self.n_out), _BF16, stream)
+            po = out.data_ptr()
+        else:
+            po = _check("out", out, _BF16, device, (rows, self.n_out))
         _call("crisp_matmul", device, stream, (codes.data_ptr(), ps, *self._w, rows, self.n_out, cols, po, *self._ws),
               (codes, scales, self.codes, self.scales, self.ws, out))
         return out
@@ -192,52 +200,47 @@ class CrispRotary:
             self.plan.magnitude = magnitude
         self._plan = ctypes.byref(self.plan)
 
-    def _run(self, device, n, positions, first, heads, inputs, outputs, stream):
+    def _run(self, device, n, positions, first, heads, inputs, outputs, stream, used):
         pos = None if positions is None else _check("positions", positions, torch.int32, device, (n,))
-        _call("crisp_rotary", device, stream, (self._plan, n, pos, first, *heads, *inputs, *(
-            None if t is None else t.data_ptr() for t in outputs)), (positions, *outputs))
+        _call("crisp_rotary", device, stream, (self._plan, n, pos, first, *heads, *inputs, *outputs), (positions, *used))
 
     def split(self, qkv, n_q_heads: int, n_kv_heads: int, positions: Optional[torch.Tensor] = None, *, first_position: int = 0,
               stream=None):
         """q [tokens, n_q_heads, 128], k and v [tokens, n_kv_heads, 128] from a product's rows
         [tokens, (n_q_heads + 2 n_kv_heads) 128]: q and k rotated, v copied.  positions: int32 [tokens] (None: first_position,
         first_position + 1, ...)."""
-        if qkv.device.type != "cuda":
+        if not qkv.is_cuda:
             raise RuntimeError("qkv must be a CUDA tensor (no CPU fallback)")
         if n_q_heads <= 0 or n_kv_heads <= 0:
             raise ValueError("there must be heads")
-        if (qkv.dim() != 2 or qkv.dtype is not torch.bfloat16 or qkv.shape[1] != (n_q_heads + 2 * n_kv_heads) * HEAD
+        if (qkv.dim() != 2 or qkv.dtype is not _BF16 or qkv.shape[1] != (n_q_heads + 2 * n_kv_heads) * HEAD
                 or qkv.stride(1) != 1):
             raise ValueError(f"qkv must be bf16 [tokens, {(n_q_heads + 2 * n_kv_heads) * HEAD}] with contiguous rows")
         device, n = qkv.device, qkv.shape[0]
         at, row = qkv.data_ptr(), qkv.stride(0) if n > 1 else qkv.shape[1]
-        q = _new((n, n_q_heads, HEAD), torch.bfloat16, device, stream)
-        k, v = (_new((n, n_kv_heads, HEAD), torch.bfloat16, device, stream) for _ in range(2))
-        inputs = (at, row, at + 2 * HEAD * n_q_heads, row, at + 2 * HEAD * (n_q_heads + n_kv_heads), row) if n else (
-            None, 0, None, 0, None, 0)
+        q, k, v = (_new(qkv, (n, h, HEAD), _BF16, stream) for h in (n_q_heads, n_kv_heads, n_kv_heads))
         if n:
-            self._run(device, n, positions, first_position, (n_q_heads, n_kv_heads), inputs, (q, k, v), stream)
-            if stream is not None:
-                qkv.record_stream(_torch_stream(stream, device))
+            inputs = (at, row, at + 2 * HEAD * n_q_heads, row, at + 2 * HEAD * (n_q_heads + n_kv_heads), row)
+            self._run(device, n, positions, first_position, (n_q_heads, n_kv_heads), inputs,
+                      (q.data_ptr(), k.data_ptr(), v.data_ptr()), stream, (qkv, q, k, v))
         return q, k, v
 
     def rotate(self, x, positions: Optional[torch.Tensor] = None, *, first_position: int = 0,
                out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         """bf16 x [tokens, heads, 128], whose tokens may have any stride, rotated.  out: contiguous; it may be x."""
-        if x.device.type != "cuda":
+        if not x.is_cuda:
             raise RuntimeError("x must be a CUDA tensor (no CPU fallback)")
-        if (x.dim() != 3 or x.dtype is not torch.bfloat16 or x.shape[1] == 0 or x.shape[2] != HEAD or x.stride(2) != 1
+        if (x.dim() != 3 or x.dtype is not _BF16 or x.shape[1] == 0 or x.shape[2] != HEAD or x.stride(2) != 1
                 or (x.shape[1] > 1 and x.stride(1) != HEAD)):
             raise ValueError("x must be bf16 [tokens, heads, 128] with contiguous tokens")
         device, n, heads = x.device, x.shape[0], x.shape[1]
         if out is None:
-            out = _new(x.shape, torch.bfloat16, device, stream)
-        _check("out", out, torch.bfloat16, device, x.shape)
+            out = _new(x, x.shape, _BF16, stream)
+        _check("out", out, _BF16, device, x.shape)
         if n:
             self._run(device, n, positions, first_position, (heads, 0),
-                      (x.data_ptr(), x.stride(0) if n > 1 else heads * HEAD, None, 0, None, 0), (out, None, None), stream)
-            if stream is not None:
-                x.record_stream(_torch_stream(stream, device))
+                      (x.data_ptr(), x.stride(0) if n > 1 else heads * HEAD, None, 0, None, 0), (out.data_ptr(), None, None),
+                      stream, (x, out))
         return out
 
 
