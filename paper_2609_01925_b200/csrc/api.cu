@@ -207,6 +207,18 @@ int allow_smem(const void* kernel, size_t bytes, std::atomic<unsigned long long>
   return CRISP_OK;
 }
 
+int resident_ctas(const void* kernel, int threads, std::atomic<int>* known, int* per_sm) {
+  int dev = 0;
+  CRISP_CUDA_TRY(cudaGetDevice(&dev), "device");
+  const bool keep = dev >= 0 && dev < 64;
+  *per_sm = keep ? known[dev].load(std::memory_order_relaxed) : 0;
+  if (*per_sm > 0) return CRISP_OK;
+  CRISP_CUDA_TRY(cudaOccupancyMaxActiveBlocksPerMultiprocessor(per_sm, kernel, threads, 0), "occupancy");
+  if (*per_sm < 1) *per_sm = 1;
+  if (keep) known[dev].store(*per_sm, std::memory_order_relaxed);
+  return CRISP_OK;
+}
+
 // ---- the 8-bit cache: host-side checks (what lives on the device is checked by the kernels)
 int check_cache(const crisp_cache* c, CacheView* v) {
   if (!c || c->struct_size != static_cast<int32_t>(sizeof(crisp_cache))) return CRISP_ERR_INVALID_ARG;

@@ -36,6 +36,10 @@ int current_sm_count(int* n_sm);
 // cudaFuncSetAttribute of a kernel's dynamic shared memory, once per device (`done`: a bit per device, the kernel's own).
 int allow_smem(const void* kernel, size_t bytes, std::atomic<unsigned long long>* done);
 
+// CTAs of a kernel without dynamic shared memory that an SM holds at a time, asked once per device (`known`: 64 numbers, the
+// kernel's own).
+int resident_ctas(const void* kernel, int threads, std::atomic<int>* known, int* per_sm);
+
 int check_cache(const crisp_cache* c, CacheView* v);
 int check_batch(const int32_t* seq_ids, const int32_t* cu, int32_t batch, int32_t n_tokens,
                 int32_t max_new, CacheBatch* b);

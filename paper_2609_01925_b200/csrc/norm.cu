@@ -14,6 +14,10 @@ namespace {
 __device__ __forceinline__ uint4 load16(const void* base, size_t offset) {
   return *reinterpret_cast<const uint4*>(static_cast<const char*>(base) + offset);
 }
+// The same for what is read once and should leave L2 to what is written.
+__device__ __forceinline__ uint4 load16_once(const void* base, size_t offset) {
+  return __ldcs(reinterpret_cast<const uint4*>(static_cast<const char*>(base) + offset));
+}
 __device__ __forceinline__ uint32_t add_bf16x2(uint32_t a, uint32_t b) {
   const float lo = __uint_as_float(a << 16) + __uint_as_float(b << 16);
   const float hi = __uint_as_float(a & 0xffff0000u) + __uint_as_float(b & 0xffff0000u);
@@ -29,13 +33,22 @@ struct NormArgs {
   float eps;
 };
 
-// kThreads threads hold kVecs vectors of 8 elements each; 16 neighbouring lanes hold a block of 128 columns.
+// Rows per CTA: four where a warp has a row of its own.
+__host__ __device__ constexpr int norm_rows(int threads) { return threads == 32 ? 4 : 1; }
+
+// CTAs of an SM, which bound a thread's registers: three of 256 threads where a row is two streams (see launch_norm).
+__host__ __device__ constexpr int norm_ctas(int threads, bool residual) {
+  return threads >= 512 ? 1024 / threads : (residual ? 768 : 1024) / (threads * norm_rows(threads));
+}
+
+// kThreads threads of a row hold kVecs vectors of 8 elements each; 16 neighbouring lanes hold a block of 128 columns.
 template <int kThreads, int kVecs, bool kResidual, bool kQuantize>
-__global__ void __launch_bounds__(kThreads) norm_kernel(const NormArgs a) {
-  constexpr int kWarps = kThreads / 32;
+__global__ void __launch_bounds__(kThreads * norm_rows(kThreads), norm_ctas(kThreads, kResidual)) norm_kernel(const NormArgs a) {
+  constexpr int kWarps = kThreads / 32, kRows = norm_rows(kThreads);
   __shared__ float part[2][kWarps < 4 ? 4 : kWarps];
   pdl_enter();
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int tid = threadIdx.x % kThreads, lane = tid & 31, warp = tid >> 5;
+  const long long step = static_cast<long long>(gridDim.x) * kRows;
   const int blocks = (a.n_cols + kScaleBlock - 1) / kScaleBlock;
   const int scale_row = 4 * ((a.n_cols + kScaleWord - 1) / kScaleWord);
   const size_t row_bytes = static_cast<size_t>(a.n_cols) * 2;
@@ -46,7 +59,8 @@ __global__ void __launch_bounds__(kThreads) norm_kernel(const NormArgs a) {
     for (int v = 0; v < kVecs; ++v) {
       if (!mine[v]) continue;
       const size_t at = row * row_bytes + static_cast<size_t>(v * kThreads + tid) * 16;
-      x[v] = load16(a.x, at);
+      // (9001 rows of 3584 to bf16: 22.6 -> 20.0 us; with a second stream, 131072 rows of 4096, it costs 563 -> 578)
+      x[v] = kResidual ? load16(a.x, at) : load16_once(a.x, at);
       if (kResidual) r[v] = load16(a.residual, at);
     }
   };
@@ -56,15 +70,15 @@ __global__ void __launch_bounds__(kThreads) norm_kernel(const NormArgs a) {
     x[v] = r[v] = make_uint4(0, 0, 0, 0);
     w[v] = make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);
   }
-  long long row = blockIdx.x;
+  long long row = static_cast<long long>(blockIdx.x) * kRows + threadIdx.x / kThreads;
   if (row < a.n_rows) fetch(row);
 #pragma unroll
   for (int v = 0; v < kVecs; ++v)
     if (a.weight && mine[v]) w[v] = load16(a.weight, static_cast<size_t>(v * kThreads + tid) * 16);
 
-  for (int turn = 0; row < a.n_rows; row += gridDim.x, turn ^= 1) {
+  for (int turn = 0; row < a.n_rows; row += step, turn ^= 1) {
     uint4 h[kVecs];
-    float ss = 0.f;
+    uint64_t ss2 = 0;   // even and odd columns
 #pragma unroll
     for (int v = 0; v < kVecs; ++v) {
       h[v] = x[v];
@@ -78,10 +92,16 @@ __global__ void __launch_bounds__(kThreads) norm_kernel(const NormArgs a) {
       float f[8];
       unpack_bf16(h[v], f);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) ss = fmaf(f[i], f[i], ss);
+      for (int i = 0; i < 8; i += 2) {
+        const uint64_t p = pack2(f[i], f[i + 1]);
+        ss2 = fma2(p, p, ss2);
+      }
     }
+    float ss, odd;
+    unpack2(ss2, ss, odd);
+    ss += odd;
     // the next row is on its way while this one's sum is joined
-    if (row + gridDim.x < a.n_rows) fetch(row + gridDim.x);
+    if (row + step < a.n_rows) fetch(row + step);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
     if (kWarps > 1) {
@@ -91,14 +111,17 @@ __global__ void __launch_bounds__(kThreads) norm_kernel(const NormArgs a) {
 #pragma unroll
       for (int i = 0; i < kWarps; ++i) ss += part[turn][i];
     }
-    const float s = rsqrtf(ss / static_cast<float>(a.n_cols) + a.eps);
+    const float m = ss / static_cast<float>(a.n_cols) + a.eps, s0 = rsqrtf(m);
+    // one step of Newton: half a rounding instead of two (not where squares have left fp32, and the row becomes 0)
+    const float s = m < INFINITY ? fmaf(0.5f * s0, fmaf(-m * s0, s0, 1.f), s0) : s0;
 #pragma unroll
     for (int v = 0; v < kVecs; ++v) {
       float f[8], g[8];
       unpack_bf16(h[v], f);
       unpack_bf16(w[v], g);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) f[i] = f[i] * s * g[i];
+      for (int i = 0; i < 8; i += 2)
+        unpack2(mul2(mul2(pack2(f[i], f[i + 1]), pack2(s, s)), pack2(g[i], g[i + 1])), f[i], f[i + 1]);
       const size_t vec = static_cast<size_t>(v * kThreads + tid);
       if (kQuantize) {
         float inverse;
@@ -159,8 +182,17 @@ template <int kThreads, int kVecs>
 int launch_norm(const NormArgs& a, int n_sm, cudaStream_t stream) {
   void (*kernel)(NormArgs) = a.residual ? (a.codes ? norm_kernel<kThreads, kVecs, true, true> : norm_kernel<kThreads, kVecs, true, false>)
                                         : (a.codes ? norm_kernel<kThreads, kVecs, false, true> : norm_kernel<kThreads, kVecs, false, false>);
-  const int most = n_sm * (2048 / kThreads < 32 ? 2048 / kThreads : 32);
-  CRISP_KERNEL("rms_norm", stream, launch_pdl(kernel, dim3(a.n_rows < most ? a.n_rows : most), dim3(kThreads), 0, stream, a));
+  // A whole number of rounds of the CTAs that are resident at a time: one (131072 rows of 4096, with addition: 3 per SM 558 us,
+  // 4 per SM 715, 8 per SM 590), or several where a CTA's rows are long or short, so that the CTAs of an SM fall out of step (16384
+  // rows of 8192: 151 us with one round, 142 with four; 30000 rows of 2048: 72 and 68).
+  constexpr int kRounds = kThreads == 512 ? 4 : kThreads == 128 || (kThreads == 1024 && kVecs == 2) ? 2 : 1;
+  static std::atomic<int> known[2][2][64];
+  int per_sm = 0;
+  constexpr int kRows = norm_rows(kThreads);
+  const int rc = resident_ctas(reinterpret_cast<const void*>(kernel), kThreads * kRows, known[a.residual != nullptr][a.codes != nullptr], &per_sm);
+  if (rc != CRISP_OK) return rc;
+  const int most = n_sm * per_sm * kRounds, rows = (a.n_rows + kRows - 1) / kRows;
+  CRISP_KERNEL("rms_norm", stream, launch_pdl(kernel, dim3(rows < most ? rows : most), dim3(kThreads * kRows), 0, stream, a));
   CRISP_CUDA_TRY(cudaGetLastError(), "rms_norm: launch");
   return CRISP_OK;
 }
@@ -174,6 +206,7 @@ int launch_rms_norm(const void* x, const void* residual, const void* weight, int
   const int rc = current_sm_count(&n_sm);
   if (rc != CRISP_OK) return rc;
   if (n_cols <= 256) return launch_norm<32, 1>(a, n_sm, stream);
+  if (n_cols <= 512) return launch_norm<32, 2>(a, n_sm, stream);
   if (n_cols <= 1024) return launch_norm<128, 1>(a, n_sm, stream);
   if (n_cols <= 2048) return launch_norm<128, 2>(a, n_sm, stream);
   if (n_cols <= 4096) return launch_norm<256, 2>(a, n_sm, stream);
@@ -186,7 +219,9 @@ int launch_quantize(const void* x, int n_rows, int n_cols, void* codes, uint8_t*
   int tx_log = 4;
   while (tx_log < 8 && (8 << tx_log) < n_cols) ++tx_log;
   const long long vecs = (static_cast<long long>(n_cols) + 7) / 8, rows = static_cast<long long>(kQuantThreads >> tx_log) * kQuantRows;
-  const dim3 grid(static_cast<unsigned>((n_rows + rows - 1) / rows), static_cast<unsigned>((vecs + (1 << tx_log) - 1) >> tx_log));
+  const long long across = (vecs + (1 << tx_log) - 1) >> tx_log;
+  if (across > 65535) return CRISP_ERR_UNSUPPORTED;   // from 2^27 columns on
+  const dim3 grid(static_cast<unsigned>((n_rows + rows - 1) / rows), static_cast<unsigned>(across));
   CRISP_KERNEL("quantize", stream, launch_pdl(quantize_kernel, grid, dim3(kQuantThreads), 0, stream, x, n_rows, n_cols, tx_log,
                                               codes, scales));
   CRISP_CUDA_TRY(cudaGetLastError(), "quantize: launch");

@@ -4,6 +4,7 @@
 #pragma once
 #include <cstdint>
 #include "common.cuh"
+#include "softmax_rows.cuh"
 
 namespace crisp {
 
@@ -34,7 +35,7 @@ __device__ __forceinline__ uint32_t pack_e4m3(float lo, float hi) {
 __device__ __forceinline__ float block_amax(const float (&y)[8]) {
   float m = 0.f;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(y[i]));
+  for (int i = 0; i < 8; i += 2) m = max3(m, fabsf(y[i]), fabsf(y[i + 1]));
 #pragma unroll
   for (int o = 1; o < 16; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
   if (__any_sync(0xffffffffu, m == INFINITY)) {   // rare: once more without the infinities
@@ -47,10 +48,10 @@ __device__ __forceinline__ float block_amax(const float (&y)[8]) {
   return m;
 }
 __device__ __forceinline__ uint2 pack_codes(const float (&y)[8], float inverse) {
-  uint2 c;
-  c.x = pack_e4m3(y[0] * inverse, y[1] * inverse) | pack_e4m3(y[2] * inverse, y[3] * inverse) << 16;
-  c.y = pack_e4m3(y[4] * inverse, y[5] * inverse) | pack_e4m3(y[6] * inverse, y[7] * inverse) << 16;
-  return c;
+  float z[8];
+#pragma unroll
+  for (int i = 0; i < 8; i += 2) unpack2(mul2(pack2(y[i], y[i + 1]), pack2(inverse, inverse)), z[i], z[i + 1]);
+  return make_uint2(pack_e4m3(z[0], z[1]) | pack_e4m3(z[2], z[3]) << 16, pack_e4m3(z[4], z[5]) | pack_e4m3(z[6], z[7]) << 16);
 }
 __device__ __forceinline__ void unpack_bf16(const uint4& w, float (&f)[8]) {
   const uint32_t u[4] = {w.x, w.y, w.z, w.w};
