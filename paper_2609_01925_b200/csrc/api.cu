@@ -105,18 +105,19 @@ int make_tmap_bf16_nhd(CUtensorMap* out, const void* base, int n, int heads, int
   return CRISP_OK;
 }
 
-static int make_tmap_bytes(CUtensorMap* out, const void* base, size_t rows, size_t cols, int box_rows) {
+static int make_tmap_matrix(CUtensorMap* out, const void* base, CUtensorMapDataType type, int element, size_t rows, size_t cols,
+                            int box_rows, CUtensorMapSwizzle swizzle) {
   EncodeTiledFn enc = encode_fn();
   if (!enc) {
     set_cu_error("cuTensorMapEncodeTiled is not available (no CUDA driver?)");
     return CRISP_ERR_CUDA;
   }
   const cuuint64_t dims[2] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows)};
-  const cuuint64_t strides[1] = {static_cast<cuuint64_t>(cols)};
+  const cuuint64_t strides[1] = {static_cast<cuuint64_t>(cols) * element};
   const cuuint32_t box[2] = {128, static_cast<cuuint32_t>(box_rows)};
   const cuuint32_t estr[2] = {1, 1};
-  CUresult r = enc(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr,
-                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+  CUresult r = enc(out, type, 2, const_cast<void*>(base), dims, strides, box, estr,
+                   CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (r != CUDA_SUCCESS) {
     char msg[96];
@@ -128,11 +129,17 @@ static int make_tmap_bytes(CUtensorMap* out, const void* base, size_t rows, size
 }
 
 int make_tmap_codes(CUtensorMap* out, const void* base, size_t rows, int box_rows) {
-  return make_tmap_bytes(out, base, rows, kHeadDim, box_rows);
+  return make_tmap_matrix(out, base, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, rows, kHeadDim, box_rows, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
 int make_tmap_operand(CUtensorMap* out, const void* base, int rows, int cols, int box_rows) {
-  return make_tmap_bytes(out, base, static_cast<size_t>(rows), static_cast<size_t>(cols), box_rows);
+  return make_tmap_matrix(out, base, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, static_cast<size_t>(rows), static_cast<size_t>(cols),
+                          box_rows, CU_TENSOR_MAP_SWIZZLE_128B);
+}
+
+int make_tmap_product(CUtensorMap* out, void* base, int rows, int cols, int box_rows) {
+  return make_tmap_matrix(out, base, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, static_cast<size_t>(rows), static_cast<size_t>(cols),
+                          box_rows, CU_TENSOR_MAP_SWIZZLE_NONE);
 }
 
 // dense_only: the call runs dense attention alone, which is defined for every length >= 1 and reads none of

@@ -256,7 +256,7 @@ namespace {
 // How a product is cut, by estimates in ns of what was measured on one B200 (12 to 32 blocks of columns, 1 to 2048 rows).
 struct Plan {
   int tile_tokens = 0, split = 0;   // split 0: the kernel for pairs of CTAs
-  long long ns = INT64_MAX;
+  long long rounds = 0, ns = INT64_MAX;
 };
 
 bool is_wide(int tile_tokens) { return tile_tokens > 208; }   // wants all of an SM's TMEM
@@ -274,16 +274,18 @@ void plan_split(int n_rows, int n_out, int blocks, int n_sm, int tile_tokens, Pl
     const long long rounds = (ctas + room - 1) / room;
     const long long crowd = ctas > n_sm && rounds == 1 ? 100 * ctas / n_sm * ctas / n_sm : 100;
     const long long ns = 3000 + (split > 1 ? 800 + 12 * tile_tokens : 0) + rounds * ceil_div(blocks, split) * block_ns * crowd / 100;
-    if (ns < best->ns) *best = Plan{tile_tokens, split, ns};
+    if (ns < best->ns) *best = Plan{tile_tokens, split, rounds, ns};
   }
 }
 
-// Tiles of 256 features and up to 224 tokens, each in a pair of CTAs: 5 us, and 95 + 0.9 tokens ns for a block of a round.
+// Tiles of 256 features and up to 224 tokens, each in a pair of CTAs: 5 us, and 95 + 0.9 tokens ns for a block of a round, or
+// 10 ns for a token that is written where there are few blocks.
 void plan_pairs(int n_rows, int n_out, int blocks, int n_sm, Plan* best) {
   for (int tokens = 64; tokens <= kPairTokens; tokens += 16) {
     const long long tiles = static_cast<long long>(ceil_div(n_out, 2 * kTileFeatures)) * ceil_div(n_rows, tokens);
-    const long long rounds = (tiles + n_sm / 2 - 1) / (n_sm / 2), ns = 5000 + rounds * blocks * (95 + 9 * tokens / 10);
-    if (ns < best->ns) *best = Plan{tokens, 0, ns};
+    const long long rounds = (tiles + n_sm / 2 - 1) / (n_sm / 2), products = blocks * (95 + 9 * tokens / 10);
+    const long long ns = 5000 + rounds * (products > 10 * tokens ? products : 10 * tokens);
+    if (ns < best->ns) *best = Plan{tokens, 0, rounds, ns};
     if (n_rows <= tokens) break;
   }
 }
@@ -308,7 +310,7 @@ int launch_matmul(const void* codes, const uint8_t* scales, const void* w_codes,
   if (n_rows > 64) plan_pairs(n_rows, n_out, blocks, n_sm, &plan);
   if (n_rows <= 256) {
     plan_split(n_rows, n_out, blocks, n_sm, ceil_div(n_rows, 16) * 16, &plan);
-  } else {
+  } else if (plan.rounds == 1 || n_out <= kTileFeatures) {   // few tiles, which more CTAs may share, or half a pair's features
     plan_split(n_rows, n_out, blocks, n_sm, 128, &plan);
     plan_split(n_rows, n_out, blocks, n_sm, 256, &plan);
   }

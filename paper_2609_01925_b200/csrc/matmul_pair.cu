@@ -2,8 +2,8 @@
 // (tcgen05, cta_group::2): either CTA holds the codes of 128 features and of half the tokens, so that a byte brought to an SM
 // serves twice as many products as it would for a CTA alone.  matmul.cu says how the scales get to the tensor core.
 //
-// The CTAs are persistent.  Roles: warps 0..3 write finished tiles, 4..7 bring scales to TMEM, 8 and 9 load codes (TMA), 10
-// issues the products (first CTA of the pair).  TMEM holds two tiles' accumulators, so that one is written while the other is computed.
+// The CTAs are persistent.  Roles: warps 0..3 and 11..14 write finished tiles, 4..7 bring scales to TMEM, 8 and 9 load codes (TMA),
+// 10 issues the products (first CTA of the pair).  TMEM holds two tiles' accumulators, so that one is written while the other is computed.
 #include <atomic>
 
 #include "matmul.cuh"
@@ -15,22 +15,25 @@ namespace {
 using namespace sm100;
 
 constexpr int kRows = 128;              // features of a CTA
-constexpr int kThreads = 352;
+constexpr int kThreads = 480;
 constexpr int kStages = 6;
+constexpr int kChunk = 32;              // tokens that are written at a time
 constexpr int kSlots = 4;               // words of scales in TMEM at a time
 constexpr int kSlotCols = 12;           // 4 for the features, 8 for the tokens
 constexpr int kScaleColumn = 512 - kSlots * kSlotCols;
 static_assert(2 * kPairTokens <= kScaleColumn, "TMEM");
 
-struct __align__(16) PairSmem {
+struct __align__(128) PairSmem {
   uint64_t full[kStages], empty[kStages], scale_full[kSlots], scale_empty[kSlots], acc_full[2], acc_empty[2];
+  __align__(128) uint16_t out[2][kChunk][kRows];   // bf16, [token][feature]
   uint32_t words[2][4][3 * kRows];      // scales of four words' 128 features and 256 tokens
   uint32_t tmem;
   int abort_flag;
 };
 
 __global__ void __launch_bounds__(kThreads, 1) matmul_pair_kernel(const __grid_constant__ CUtensorMap tw,
-                                                                  const __grid_constant__ CUtensorMap ta, const MatmulArgs a) {
+                                                                  const __grid_constant__ CUtensorMap ta,
+                                                                  const __grid_constant__ CUtensorMap to, const MatmulArgs a) {
   extern __shared__ __align__(1024) uint8_t raw[];
   __shared__ PairSmem s;
   uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~static_cast<uintptr_t>(1023));
@@ -51,7 +54,7 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_pair_kernel(const __grid_c
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&s.acc_full[i], 1);
-      mbar_init(&s.acc_empty[i], 8);
+      mbar_init(&s.acc_empty[i], 16);
     }
     s.abort_flag = 0;
     fence_mbar_init();
@@ -157,7 +160,7 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_pair_kernel(const __grid_c
         }
       }
     }
-  } else if (warp >= 4) {
+  } else if (warp >= 4 && warp < 8) {
     const int row = tid - 128;   // of the features, and of both halves of 256 tokens
     const uint32_t quarter = tm + kScaleColumn + (static_cast<uint32_t>((warp & 3) * 32) << 16);
     uint32_t next[3][4];
@@ -212,45 +215,95 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_pair_kernel(const __grid_c
       }
     }
   } else {
+    // Two groups of four warps take turns with chunks of 32 tokens.  A chunk goes through shared memory, where a thread's feature (a
+    // lane of TMEM) becomes a place in a token's row of 256 bytes.  (Straight from registers, 64 bytes of a token at a time, 32768 rows of
+    // 8192 features left at 1.8 TB/s.)
     bool ok = true;
     int turn = 0;
-    const uint32_t quarter = tm + (static_cast<uint32_t>(warp * 32) << 16);
-    const bool pairs_ok = (a.n_out & 1) == 0;   // two neighbouring features in one store
-    for (long long tile = first; tile < a.n_tiles && ok; tile += pairs, ++turn) {
+    const int group = warp > 10, part = warp & 3, member = group ? warp - 11 : warp;   // part: of TMEM's lanes
+    const uint32_t quarter = tm + (static_cast<uint32_t>(part * 32) << 16);
+    const bool by_tma = (a.n_out & 7) == 0;
+    for (long long tile = first; tile < a.n_tiles; tile += pairs, ++turn) {   // (all four warps meet at every barrier: see above)
       int f0, t0;
       place(tile, f0, t0);
-      const int buf = turn & 1, feature = f0 + warp * 32 + lane;
-      ok = mbar_wait_warp(&s.acc_full[buf], (turn >> 1) & 1, abort_flag);
-      if (!ok) break;
+      const int buf = turn & 1;
+      ok = ok && mbar_wait_warp(&s.acc_full[buf], (turn >> 1) & 1, abort_flag);
       tc_fence_after_sync();
       const int n_tokens = min(a.tile_tokens, a.n_rows - t0);
-      for (int c = 0; c < a.tile_tokens; c += 32) {
+      for (int c = group * kChunk; c < a.tile_tokens; c += 2 * kChunk) {
         uint32_t v[32];
-        tmem_ld_x32(quarter + buf * kPairTokens + c, v);
-        tmem_ld_wait();
-        if (c + 32 >= a.tile_tokens) {
-          tc_fence_before_sync();
-          __syncwarp();
-          if (lane == 0) cluster_arrive(cluster_map(smem_u32(&s.acc_empty[buf]), 0));
+        if (ok) {
+          tmem_ld_x32(quarter + buf * kPairTokens + c, v);
+          tmem_ld_wait();
+          if (c + 2 * kChunk >= a.tile_tokens) {
+            tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) cluster_arrive(cluster_map(smem_u32(&s.acc_empty[buf]), 0));
+          }
         }
-        if (pairs_ok) {
-          // even lanes write the even tokens' pair of features, odd lanes the odd tokens'
-          const bool odd = lane & 1;
-          __nv_bfloat16* out = a.out + static_cast<size_t>(t0 + c + odd) * a.n_out + (feature & ~1);
+        if (by_tma && member == 0) {
+          if (elect_one()) tma_store_wait_read0();   // the group's last chunk has been read
+          __syncwarp();
+        }
+        named_bar_sync(2 + group, 128);
+        if (ok) {
 #pragma unroll
           for (int i = 0; i < 32; i += 2) {
-            const float mine = __uint_as_float(odd ? v[i + 1] : v[i]);
-            const float other = __shfl_xor_sync(0xffffffffu, __uint_as_float(odd ? v[i] : v[i + 1]), 1);
-            if (c + i + odd < n_tokens && feature < a.n_out)
-              *reinterpret_cast<uint32_t*>(out + static_cast<size_t>(i) * a.n_out) = odd ? pack_bf16(other, mine) : pack_bf16(mine, other);
+            const uint32_t two = pack_bf16(__uint_as_float(v[i]), __uint_as_float(v[i + 1]));
+            s.out[group][i][part * 32 + lane] = static_cast<uint16_t>(two);
+            s.out[group][i + 1][part * 32 + lane] = static_cast<uint16_t>(two >> 16);
           }
-        } else {
+        }
+        if (by_tma) fence_proxy_async_smem();
+        named_bar_sync(2 + group, 128);
+        if (!ok) continue;
+        if (by_tma) {
+          if (member == 0 && elect_one()) {
+            // in halves, since a tile may end within a chunk; what is behind the last row or feature is left out
+            const bool here = f0 < a.n_out;
+            if (here && c < n_tokens) tma_store_2d(&to, s.out[group][0], f0, t0 + c);
+            if (here && c + kChunk / 2 < n_tokens) tma_store_2d(&to, s.out[group][kChunk / 2], f0, t0 + c + kChunk / 2);
+            tma_store_commit();
+          }
+          continue;
+        }
+        // Rows that TMA cannot write: a warp writes every fourth, a lane two pairs of neighbouring features; where a row begins at an
+        // odd place, pairs are taken from its second feature on and the first is written alone.
+        const int token = t0 + c + member, left = n_tokens - c - member, n_features = a.n_out - f0;
+        const int odd = a.n_out & token & 1;
+        __nv_bfloat16* out = a.out + static_cast<size_t>(token) * a.n_out + f0 + 2 * lane + odd;
+        const int have = n_features - 2 * lane - odd;
+        uint32_t w[kChunk / 4][2];
 #pragma unroll
-          for (int i = 0; i < 32; ++i)
-            if (c + i < n_tokens && feature < a.n_out)
-              a.out[static_cast<size_t>(t0 + c + i) * a.n_out + feature] = __float2bfloat16_rn(__uint_as_float(v[i]));
+        for (int i = 0; i < kChunk / 4; ++i) {
+          const uint32_t* row = reinterpret_cast<const uint32_t*>(s.out[group][member + 4 * i]) + lane;
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            w[i][j] = row[32 * j];
+            if (odd) w[i][j] = __funnelshift_r(w[i][j], 32 * j + lane < 63 ? row[32 * j + 1] : 0, 16);
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < kChunk / 4; ++i) {
+          if (4 * i >= left) break;
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            __nv_bfloat16* at = out + static_cast<size_t>(4 * i) * a.n_out + 64 * j;
+            const bool last = odd && j == 1 && lane == 31;   // its second feature is the next tile's first
+            if (have - 64 * j >= 2 && !last) {
+              *reinterpret_cast<uint32_t*>(at) = w[i][j];
+            } else if (have - 64 * j >= 1) {
+              *reinterpret_cast<uint16_t*>(at) = static_cast<uint16_t>(w[i][j]);
+            }
+          }
+          if (odd && lane == 0 && n_features > 0)
+            *reinterpret_cast<uint16_t*>(out - 1 + static_cast<size_t>(4 * i) * a.n_out) = s.out[group][member + 4 * i][0];
         }
       }
+    }
+    if (by_tma && member == 0) {
+      if (elect_one()) tma_store_wait0();
+      __syncwarp();
     }
   }
   tc_fence_before_sync();
@@ -277,15 +330,17 @@ int launch_matmul_pair(MatmulArgs a, const void* codes, const void* w_codes, int
   a.n_tiles = static_cast<long long>(a.n_feature_tiles) * ceil_div(a.n_rows, tile_tokens);
   constexpr size_t kSmem = kStages * (kRows + kPairTokens / 2) * kScaleBlock + 1024;
   static_assert(kSmem + sizeof(PairSmem) + 1024 <= 228 * 1024, "shared memory of an SM");
-  CUtensorMap tw, ta;
+  CUtensorMap tw, ta, to;
   int rc = make_tmap_operand(&tw, w_codes, a.n_out, a.n_cols, kRows);
   if (rc == CRISP_OK) rc = make_tmap_operand(&ta, codes, a.n_rows, a.n_cols, tile_tokens / 2);
+  to = ta;   // (unused where rows are not whole vectors of 16 bytes)
+  if (rc == CRISP_OK && a.n_out % 8 == 0) rc = make_tmap_product(&to, a.out, a.n_rows, a.n_out, kChunk / 2);
   static std::atomic<unsigned long long> done{0};
   if (rc == CRISP_OK) rc = allow_smem(reinterpret_cast<const void*>(&matmul_pair_kernel), kSmem, &done);
   if (rc != CRISP_OK) return rc;
   const long long pairs = a.n_tiles < n_sm / 2 ? a.n_tiles : n_sm / 2;
   CRISP_KERNEL("matmul_pair", stream, launch_pdl_cluster(matmul_pair_kernel, dim3(static_cast<unsigned>(2 * pairs)), dim3(kThreads),
-                                                         kSmem, 2, stream, tw, ta, a));
+                                                         kSmem, 2, stream, tw, ta, to, a));
   CRISP_CUDA_TRY(cudaGetLastError(), "matmul: launch");
   return CRISP_OK;
 }

@@ -77,5 +77,7 @@ constexpr int kMaxOperandSize = 1 << 28;  // rows and columns of an operand
 
 // Tensor map of codes [rows][cols] with a {128, box_rows} box and 128-byte swizzle; what lies outside reads as zero.
 int make_tmap_operand(CUtensorMap* out, const void* base, int rows, int cols, int box_rows);
+// Tensor map of bf16 [rows][cols], cols a multiple of 8, with a {128, box_rows} box.
+int make_tmap_product(CUtensorMap* out, void* base, int rows, int cols, int box_rows);
 
 }  // namespace crisp
