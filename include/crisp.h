@@ -399,7 +399,7 @@ int crisp_cache_compact(const crisp_cache* c, int32_t* n_used, void* ws, size_t 
  *          128 b .. 128 b + 127; bytes behind the last block are 127 and are not used (they make rows of whole 32-bit words).
  * An element is code * scale.  A scale is the smallest power of two >= 2^-126 that brings its block's largest finite
  * magnitude within 448, codes are rounded to nearest, ties to even; infinities become the largest code, NaN stays NaN.
- * All of these arrays are 16-byte aligned.
+ * Arrays are 16-byte aligned, scales 4-byte aligned: any rows of an operand are an operand.
  */
 
 /* Rows of bf16 x [n_rows][n_cols] as an operand: weights, once, or the output of attention. */
@@ -409,6 +409,7 @@ int crisp_quantize(const void* x, int32_t n_rows, int32_t n_cols, void* codes, u
  * Root-mean-square norm of rows, with the residual's addition:
  *   h = x + residual, rounded to bf16 and stored in `sum` (residual and sum both NULL: h = x)
  *   y = h / sqrt(mean(h^2) + eps) * weight            (weight [n_cols] bf16, NULL: 1), the mean in fp32
+ * (a row whose squares leave fp32 becomes 0),
  * written either as bf16 `y` or as an operand, `codes` and `scales` (converted from fp32, not from bf16); the other is NULL.
  * sum may be x or residual, and y may be x: rows are read before they are written.  n_cols is a multiple of 16, at most 32768.
  */

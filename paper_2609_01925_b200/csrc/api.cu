@@ -190,6 +190,7 @@ int validate(const crisp_params* p, Dims* d, bool dense_only) {
 }
 
 static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+static bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
 int current_sm_count(int* n_sm) {
   static std::atomic<int> known[64];
@@ -932,7 +933,7 @@ static int check_operand(int32_t n_rows, int32_t n_cols) {
 int crisp_quantize(const void* x, int32_t n_rows, int32_t n_cols, void* codes, uint8_t* scales, void* cuda_stream) {
   const int rc = check_operand(n_rows, n_cols);
   if (rc != CRISP_OK || n_rows == 0) return rc;
-  if (!x || !codes || !scales || !aligned16(x) || !aligned16(codes) || !aligned16(scales)) return CRISP_ERR_INVALID_ARG;
+  if (!x || !codes || !scales || !aligned16(x) || !aligned16(codes) || !aligned4(scales)) return CRISP_ERR_INVALID_ARG;
   return launch_quantize(x, n_rows, n_cols, codes, scales, static_cast<cudaStream_t>(cuda_stream));
 }
 
@@ -947,8 +948,9 @@ int crisp_rms_norm(const void* x, const void* residual, const void* weight, int3
       (residual != nullptr) != (sum != nullptr))
     return CRISP_ERR_INVALID_ARG;
   for (const void* p : {x, residual, weight, static_cast<const void*>(sum), static_cast<const void*>(y),
-                        static_cast<const void*>(codes), static_cast<const void*>(scales)})
+                        static_cast<const void*>(codes)})
     if (!aligned16(p)) return CRISP_ERR_INVALID_ARG;
+  if (!aligned4(scales)) return CRISP_ERR_INVALID_ARG;
   return launch_rms_norm(x, residual, weight, n_rows, n_cols, eps, sum, y, codes, scales,
                          static_cast<cudaStream_t>(cuda_stream));
 }
@@ -961,9 +963,8 @@ int crisp_matmul(const void* codes, const uint8_t* scales, const void* w_codes, 
   if (rc == CRISP_OK) rc = check_operand(n_out, n_cols);
   if (rc != CRISP_OK || n_rows == 0 || n_out == 0) return rc;
   if (!codes || !scales || !w_codes || !w_scales || !out || !ws) return CRISP_ERR_INVALID_ARG;
-  for (const void* p : {codes, static_cast<const void*>(scales), w_codes, static_cast<const void*>(w_scales),
-                        static_cast<const void*>(out)})
-    if (!aligned16(p)) return CRISP_ERR_INVALID_ARG;
+  if (!aligned16(codes) || !aligned16(w_codes) || !aligned16(out) || !aligned4(scales) || !aligned4(w_scales))
+    return CRISP_ERR_INVALID_ARG;
   if (!aligned16(ws) || ws_bytes < kWsHeader) return CRISP_ERR_WORKSPACE;
   return launch_matmul(codes, scales, w_codes, w_scales, n_rows, n_out, n_cols, out, ws,
                        static_cast<cudaStream_t>(cuda_stream));

@@ -23,7 +23,7 @@ inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
 // Four words of a row's scales, from word `at`; ones behind the end.
 __device__ __forceinline__ void load_words(const uint8_t* scales, long long row, int rows, int words, int at, uint32_t (&w)[4]) {
   const uint32_t* p = reinterpret_cast<const uint32_t*>(scales) + row * words + at;
-  if (row < rows && ((words | at) & 3) == 0) {
+  if (row < rows && ((words | at) & 3) == 0 && (reinterpret_cast<uintptr_t>(scales) & 15) == 0) {
     const uint4 v = *reinterpret_cast<const uint4*>(p);
     w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
   } else {

@@ -189,6 +189,37 @@ def test_captured_step_replays():
     block.poll()
 
 
+def test_first_calls_of_a_process_may_be_captured():
+    """Nothing that a call does for the first time gets in the way of a capture."""
+    import subprocess
+    import sys
+    code = """
+import torch, paper_2609_01925_b200 as crisp
+x = torch.randn(400, 512, device="cuda").bfloat16(); w = torch.randn(1024, 512, device="cuda").bfloat16()
+rot = crisp.CrispRotary(1e4); torch.cuda.synchronize()
+s = torch.cuda.Stream()
+ws = torch.zeros(256, dtype=torch.uint8, device="cuda")
+g = torch.cuda.CUDAGraph()
+lin = crisp.CrispLinear(torch.empty(1024, 512, device="cuda").to(torch.float8_e4m3fn), torch.empty(1024, 4, dtype=torch.uint8, device="cuda").view(torch.float8_e8m0fnu))
+torch.cuda.synchronize()
+def step(x):
+    c, sc, _ = crisp.rms_norm_quantize(x)
+    wc, ws = crisp.quantize(w)
+    lin.codes.copy_(wc.view(torch.uint8).view(torch.float8_e4m3fn)); lin.scales.view(torch.uint8).copy_(ws.view(torch.uint8))
+    return rot.split(lin(c, sc), 4, 2), rot.split(lin(c[:5].contiguous(), sc[:5].contiguous()), 4, 2)
+with torch.cuda.graph(g):
+    out = step(x)
+g.replay(); torch.cuda.synchronize()
+want = step(x); torch.cuda.synchronize(); lin.poll()
+assert all(torch.equal(a, b) for p, q in zip(out, want) for a, b in zip(p, q))
+print("ok")
+"""
+    import os
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    done = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300, cwd=root)
+    assert done.returncode == 0 and "ok" in done.stdout, done.stderr[-2000:]
+
+
 def test_two_graphs_share_a_linear():
     """Two captured products of one CrispLinear, replayed at the same time on two streams."""
     w = weights(1024, 2048, 60)

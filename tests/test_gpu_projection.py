@@ -138,6 +138,31 @@ def raw_t(t):
     return t.view(torch.uint8)
 
 
+def test_norm_output_in_place():
+    x, w = normal(700, 2048, seed=12).to(DEV), normal(2048, seed=13).to(DEV)
+    want, _ = crisp.rms_norm(x, w)
+    from paper_2609_01925_b200 import binding as B
+    B.check(B.crisp_rms_norm(x, None, w, 1e-5, None, x, None, None), "crisp_rms_norm")
+    assert torch.equal(x, want)
+
+
+def test_norm_of_a_row_and_itself():
+    """x as its own residual, stored over itself."""
+    x = normal(300, 512, seed=14).to(DEV)
+    want, h = crisp.rms_norm(x, None, x.clone())
+    y, h2 = crisp.rms_norm(x, None, x, sum_out=x)
+    assert torch.equal(y, want) and torch.equal(h2, h) and h2 is x
+
+
+def test_norm_beyond_fp32():
+    """Squares that leave fp32 make the row 0; the rows beside it are as they are."""
+    x = normal(3, 1024, seed=15)
+    x[1] = 2.0 ** 100
+    y = f64(crisp.rms_norm(x.to(DEV))[0])
+    assert (y[1] == 0).all()
+    check_norm(x[::2].contiguous(), None, None, 1e-5, False)
+
+
 def test_norm_of_a_stored_sum_is_the_same():
     x, r, w = normal(50, 4096, seed=9).to(DEV), normal(50, 4096, seed=10).to(DEV), normal(4096, seed=11).to(DEV)
     y, h = crisp.rms_norm(x, w, r)
@@ -204,6 +229,32 @@ def test_product_of_whole_numbers_is_exact(rows, n, cols):
     lin.poll()
     want = torch.from_numpy(ref.values(*a)).to(DEV) @ torch.from_numpy(ref.values(*w)).to(DEV).t()
     assert torch.equal(out, want.bfloat16())      # |sums| < 2^24 / 16: exact in fp32, one rounding to bf16
+
+
+@pytest.mark.parametrize("rows,n,cols", [(9000, 2056, 656), (9000, 2051, 656), (9000, 2050, 112), (2500, 4097, 1280), (20000, 45, 256),
+                                         (3987, 20, 1120), (129, 6144, 2064), (1000, 1024, 8192), (48, 128, 20000)])
+def test_product_over_many_tiles_is_exact(rows, n, cols):
+    """Several tiles one after the other in a CTA, rows of every alignment, few features, many columns: made on the GPU, otherwise
+    as above."""
+    g = torch.Generator(device=DEV).manual_seed(rows + n + cols)
+    grid = torch.tensor([0x00, 0x38, 0x40, 0xb8, 0xc0], dtype=torch.uint8, device=DEV)
+    number = torch.tensor([0.0, 1.0, 2.0, -1.0, -2.0], dtype=torch.float64, device=DEV)
+
+    def make(r):
+        pick = torch.randint(0, 5, (r, cols), generator=g, device=DEV)
+        e = torch.randint(125, 130, (r, -(-cols // 128)), generator=g, device=DEV)
+        scales = torch.full((r, ref.scale_cols(cols)), 127, dtype=torch.uint8, device=DEV)
+        scales[:, :e.shape[1]] = e.to(torch.uint8)
+        value = number[pick] * torch.exp2(e.double() - 127).repeat_interleave(128, 1)[:, :cols]
+        return (grid[pick].view(torch.float8_e4m3fn), scales.view(torch.float8_e8m0fnu)), value
+
+    (a, av), (w, wv) = make(rows), make(n)
+    lin = crisp.CrispLinear(*w)
+    buffer = torch.full((rows + 3, n), 7.0, dtype=torch.bfloat16, device=DEV)
+    lin(*a, out=buffer[:rows])
+    lin.poll()
+    assert torch.equal(buffer[:rows], (av @ wv.t()).bfloat16())
+    assert bool((buffer[rows:] == 7.0).all())
 
 
 def test_product_extreme_scales_and_nan():
@@ -308,6 +359,41 @@ def test_rotary_turns_back():
     # two roundings to bf16, the first of which the way back spreads over the pair
     size = (x.float()[..., :64] ** 2 + x.float()[..., 64:] ** 2).sqrt().repeat(1, 1, 2)
     assert bool(((back.float() - x.float()).abs() <= size * (2.5 * HALF_BF16)).all())
+
+
+# ------------------------------------------------------------------------------------------------ large tensors
+def test_offsets_beyond_32_bits():
+    """Tensors of more than 2^31 elements: their last rows, and those around element 2^31, are what the same rows give alone."""
+    rows, cols = 530000, 4096
+    g = torch.Generator(device=DEV).manual_seed(1)
+    x = torch.empty(rows, cols, dtype=torch.bfloat16, device=DEV)
+    base = torch.randn(1000, cols, generator=g, device=DEV).bfloat16()
+    for at in range(0, rows, 1000):
+        x[at:at + 1000] = base.roll(at // 1000, 0)
+    parts = [slice(0, 3), slice(2 ** 31 // cols - 2, 2 ** 31 // cols + 3), slice(rows - 5, rows)]
+    residual = x.flip(0)
+    codes, scales, h = crisp.rms_norm_quantize(x, None, residual)
+    qc, qs = crisp.quantize(x)
+    for p in parts:
+        a = crisp.rms_norm_quantize(x[p].contiguous(), None, residual[p].contiguous())
+        assert torch.equal(raw_t(codes[p]), raw_t(a[0])) and torch.equal(raw_t(scales[p]), raw_t(a[1])) and torch.equal(h[p], a[2])
+        b = crisp.quantize(x[p].contiguous())
+        assert torch.equal(raw_t(qc[p]), raw_t(b[0])) and torch.equal(raw_t(qs[p]), raw_t(b[1]))
+    del residual, codes, scales, h, qc, qs, x
+    rows, n = 360000, 6144
+    a = crisp.quantize(torch.randn(rows, 128, generator=g, device=DEV).bfloat16())
+    lin = crisp.CrispLinear.from_weight(torch.randn(n, 128, generator=g, device=DEV).bfloat16())
+    out = lin(*a)
+    rot = crisp.CrispRotary(1e4)
+    q, k, v = rot.split(out, 32, 8)
+    parts = [slice(0, 300), slice(2 ** 31 // n - 150, 2 ** 31 // n + 150), slice(rows - 300, rows)]
+    for p in parts:
+        want = lin(*(t[p].contiguous() for t in a))
+        # (another cut of the product: sums of 128 columns in one order, so the same bits)
+        assert torch.equal(out[p], want)
+        again = rot.split(want, 32, 8, torch.arange(p.start, p.stop, dtype=torch.int32, device=DEV))
+        assert all(torch.equal(s[p], t) for s, t in zip((q, k, v), again))
+    lin.poll()
 
 
 # ------------------------------------------------------------------------------------------------ sizes of zero, refusals

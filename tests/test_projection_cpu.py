@@ -14,7 +14,7 @@ from paper_2609_01925_b200 import binding as B
 from tests import projection_reference as ref
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
-FAKE, ODD = 0x1000, 0x1008      # never dereferenced: validation comes first
+FAKE, ODD, WORD = 0x1000, 0x100a, 0x1004      # never dereferenced: validation comes first
 NAN, INF = float("nan"), float("inf")
 
 
@@ -54,6 +54,7 @@ def test_matmul_refusals():
         return lib.crisp_matmul(codes, scales, w, ws_, rows, n, cols, out, ws, ws_bytes, None)
 
     for kw in (dict(codes=None), dict(scales=None), dict(w=None), dict(ws_=None), dict(out=None), dict(ws=None), dict(codes=ODD),
+               dict(codes=WORD), dict(w=WORD), dict(out=WORD),
                dict(scales=ODD), dict(w=ODD), dict(ws_=ODD), dict(out=ODD), dict(rows=-1), dict(n=-1), dict(cols=0)):
         assert call(**kw) == B.ERR_INVALID_ARG, kw
     assert call(cols=8) == call(cols=1 << 29) == call(rows=1 << 29) == call(n=1 << 29) == B.ERR_UNSUPPORTED
