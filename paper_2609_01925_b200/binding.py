@@ -7,6 +7,8 @@ if the library cannot be loaded the import fails loudly: there is no CPU or PyTo
 from __future__ import annotations
 
 import ctypes
+import importlib.machinery
+import importlib.util
 import os
 from typing import Optional, Tuple
 
@@ -176,6 +178,29 @@ def load() -> ctypes.CDLL:
     lib.crisp_poll_device_status.argtypes = [vp, vp]
     _lib = lib
     return lib
+
+
+CALLS_PATH = os.path.join(_HERE, "_calls.so")
+_calls = None
+
+
+def calls():
+    """The compiled checks, outputs and streams of the calls around the attention (csrc/calls.cpp), bound to libcrisp.so.
+    Raises if either is missing."""
+    global _calls
+    if _calls is None:
+        lib = load()
+        if not os.path.exists(CALLS_PATH):
+            raise ImportError(f"{CALLS_PATH} not found: build it with `python -m paper_2609_01925_b200.build` "
+                              "(there is no fallback path)")
+        name = __package__ + "._calls"
+        loader = importlib.machinery.ExtensionFileLoader(name, CALLS_PATH)
+        module = importlib.util.module_from_spec(importlib.util.spec_from_loader(name, loader))
+        loader.exec_module(module)
+        module.bind(CrispError, *(ctypes.cast(f, ctypes.c_void_p).value for f in (
+            lib.crisp_quantize, lib.crisp_rms_norm, lib.crisp_matmul, lib.crisp_rotary)))
+        _calls = module
+    return _calls
 
 
 def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:

@@ -1,13 +1,15 @@
-"""Builds the CUDA library (libcrisp.so) in-tree with nvcc for sm_100a."""
+"""Builds the CUDA library (libcrisp.so) in-tree with nvcc for sm_100a, and the compiled part of the binding (_calls.so)."""
 from __future__ import annotations
 
 import os
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcrisp.so")
+CALLS = os.path.join(HERE, "_calls.so")
 SOURCES = ["api.cu", "route.cu", "select.cu", "prefill.cu", "cache_pages.cu", "cache_attention.cu", "cache_prefill.cu",
            "cache_join.cu", "norm.cu", "matmul.cu", "matmul_pair.cu", "rotary.cu", "selftest.cu"]
 HEADERS = ["common.cuh", "cache.cuh", "cache_split.cuh", "cache_codes.cuh", "cache_ring.h", "operand.cuh", "matmul.cuh", "softmax_rows.cuh",
@@ -20,10 +22,10 @@ def _nvcc() -> str:
 
 
 def needs_build() -> bool:
-    if not os.path.exists(LIB):
+    if not os.path.exists(LIB) or not os.path.exists(CALLS):
         return True
-    t = os.path.getmtime(LIB)
-    deps = [os.path.join(CSRC, f) for f in SOURCES + HEADERS] + [os.path.abspath(__file__)]
+    t = min(os.path.getmtime(LIB), os.path.getmtime(CALLS))
+    deps = [os.path.join(CSRC, f) for f in SOURCES + HEADERS + ["calls.cpp"]] + [os.path.abspath(__file__)]
     return any(os.path.getmtime(p) > t for p in deps)
 
 
@@ -43,7 +45,25 @@ def build(force: bool = False, verbose: bool = False) -> str:
         raise RuntimeError("nvcc failed building libcrisp.so")
     if verbose:
         sys.stderr.write(res.stdout + res.stderr)
+    build_calls()
     return LIB
+
+
+def build_calls() -> str:
+    """Compile calls.cpp against the torch that is installed; returns the module's path."""
+    import torch
+    torch_dir = os.path.dirname(torch.__file__)
+    cuda = os.path.dirname(os.path.dirname(_nvcc())) or "/usr/local/cuda"
+    include = [os.path.join(torch_dir, "include"), os.path.join(torch_dir, "include", "torch", "csrc", "api", "include"),
+               os.path.join(cuda, "include"), sysconfig.get_paths()["include"]]
+    cmd = ["g++", "-O2", "-std=c++17", "-shared", "-fPIC", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           "-o", CALLS, os.path.join(CSRC, "calls.cpp")] + [f"-I{d}" for d in include] + [f"-L{os.path.join(torch_dir, 'lib')}"] + [
+           f"-l{x}" for x in ("torch", "torch_cpu", "torch_cuda", "torch_python", "c10", "c10_cuda")]
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    if res.returncode != 0:
+        sys.stderr.write(res.stdout + res.stderr)
+        raise RuntimeError("g++ failed building _calls.so")
+    return CALLS
 
 
 if __name__ == "__main__":

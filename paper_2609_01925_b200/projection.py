@@ -25,120 +25,27 @@ _SCALINGS = {"none": B.ROTARY_PLAIN, "linear": B.ROTARY_LINEAR, "base": B.ROTARY
              "bands": B.ROTARY_BANDS}
 
 
-# ---- what the calls below share (an answer calls them several times per layer and token, so the way to the library is kept
-# short: places are device indexes, -1 for the CPU, and outputs are made beside a tensor that is there)
-_BF16, _I32 = torch.bfloat16, torch.int32
-
-
-def _check(name, t, dtype, index, shape=None):
-    """Pointer of a contiguous tensor of that type, place and shape."""
-    if t.dtype is not dtype or t.get_device() != index or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous {dtype} tensor on cuda:{index}")
-    if shape is not None and t.shape != shape:
-        raise ValueError(f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}")
-    return t.data_ptr()
-
-
-def _rows(name, t, dtype):
-    """Place and shape of a matrix of that type."""
-    index, shape = t.get_device(), t.shape
-    if index < 0:
-        raise RuntimeError(f"{name} must be a CUDA tensor (no CPU fallback)")
-    if len(shape) != 2 or t.dtype is not dtype or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous {dtype} matrix")
-    return index, shape
-
-
+# (Argument checks, outputs and streams of these calls are in csrc/calls.cpp.)
 def _scale_cols(cols):
     return (cols + 511) // 512 * 4
-
-
-def _torch_stream(stream, index):
-    """The torch stream of a stream or handle.  (0 is the default stream's; ExternalStream(0) would be a new one.)"""
-    if not isinstance(stream, int):
-        return stream
-    return torch.cuda.ExternalStream(stream, device=index) if stream else torch.cuda.default_stream(index)
-
-
-def _new(like, shape, dtype, stream):
-    """An output beside `like`, allocated on the stream that will write it."""
-    if stream is None:
-        return like.new_empty(shape, dtype=dtype)
-    with torch.cuda.stream(_torch_stream(stream, like.get_device())):
-        return like.new_empty(shape, dtype=dtype)
-
-
-def _new_like(like, dtype, stream):
-    """The same with the shape of `like`."""
-    if stream is None:
-        return torch.empty_like(like, dtype=dtype)
-    return _new(like, like.shape, dtype, stream)
-
-
-def _call(name, index, stream, args, tensors):
-    """The C call of that name on (*args, stream), with device `index` current."""
-    function = getattr(B.load(), name)
-    if stream is None:
-        raw = torch._C._cuda_getCurrentRawStream(index)
-    else:
-        raw = stream if isinstance(stream, int) else stream.cuda_stream
-    if torch._C._cuda_getDevice() == index:
-        rc = function(*args, raw)
-    else:
-        with torch.cuda.device(index):
-            rc = function(*args, raw)
-    if rc != B.OK:
-        raise B.CrispError(rc, name)
-    if stream is not None:
-        stream = _torch_stream(stream, index)
-        for t in tensors:
-            if t is not None:
-                t.record_stream(stream)
 
 
 # ---- rows
 def quantize(x, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """bf16 [rows, columns] as an operand (codes, scales): weights, once, or the output of attention."""
-    index, (rows, cols) = _rows("x", x, _BF16)
-    codes, scales = _new_like(x, CODES, stream), _new(x, (rows, _scale_cols(cols)), SCALES, stream)
-    _call("crisp_quantize", index, stream, (x.data_ptr(), rows, cols, codes.data_ptr(), scales.data_ptr()), (x, codes, scales))
-    return codes, scales
-
-
-def _norm_inputs(x, weight, residual, sum_out, stream):
-    """(place, shape, pointers of residual, weight and sum, sum)."""
-    index, shape = _rows("x", x, _BF16)
-    w = None if weight is None else _check("weight", weight, _BF16, index, shape[1:])
-    if residual is None:
-        if sum_out is not None:
-            raise ValueError("sum_out belongs to a residual")
-        return index, shape, None, w, None, None
-    r = _check("residual", residual, _BF16, index, shape)
-    if sum_out is None:
-        sum_out = _new_like(x, _BF16, stream)
-        return index, shape, r, w, sum_out.data_ptr(), sum_out
-    return index, shape, r, w, _check("sum_out", sum_out, _BF16, index, shape), sum_out
+    return B.calls().quantize(x, stream)
 
 
 def rms_norm(x, weight=None, residual=None, *, eps: float = 1e-5, sum_out: Optional[torch.Tensor] = None, stream=None):
     """Root-mean-square norm of bf16 rows: h = x + residual (rounded to bf16; without one h is x),
     y = h / sqrt(mean(h^2) + eps) * weight.  Returns (y, h), h None without a residual.  sum_out: where h goes; it may be x
     or residual."""
-    index, (rows, cols), r, w, total, h = _norm_inputs(x, weight, residual, sum_out, stream)
-    y = _new_like(x, _BF16, stream)
-    _call("crisp_rms_norm", index, stream, (x.data_ptr(), r, w, rows, cols, eps, total, y.data_ptr(), None, None),
-          (x, weight, residual, h, y))
-    return y, h
+    return B.calls().rms_norm(x, weight, residual, eps, sum_out, False, stream)
 
 
 def rms_norm_quantize(x, weight=None, residual=None, *, eps: float = 1e-5, sum_out: Optional[torch.Tensor] = None, stream=None):
     """rms_norm with y as an operand of a product: returns (codes, scales, h)."""
-    index, (rows, cols), r, w, total, h = _norm_inputs(x, weight, residual, sum_out, stream)
-    codes, scales = _new_like(x, CODES, stream), _new(x, (rows, _scale_cols(cols)), SCALES, stream)
-    _call("crisp_rms_norm", index, stream,
-          (x.data_ptr(), r, w, rows, cols, eps, total, None, codes.data_ptr(), scales.data_ptr()),
-          (x, weight, residual, h, codes, scales))
-    return codes, scales, h
+    return B.calls().rms_norm(x, weight, residual, eps, sum_out, True, stream)
 
 
 # ---- products
@@ -146,12 +53,16 @@ class CrispLinear:
     """Weights [out_features, in_features] as an operand, and products with them."""
 
     def __init__(self, codes, scales):
-        self._index, (self.n_out, self.n_in) = _rows("codes", codes, CODES)
-        self._cols = _scale_cols(self.n_in)
-        _check("scales", scales, SCALES, self._index, (self.n_out, self._cols))
+        if not codes.is_cuda:
+            raise RuntimeError("codes must be a CUDA tensor (no CPU fallback)")
+        if codes.dim() != 2 or codes.dtype is not CODES or not codes.is_contiguous():
+            raise ValueError(f"codes must be a contiguous {CODES} matrix")
+        self.n_out, self.n_in = codes.shape
+        shape = (self.n_out, _scale_cols(self.n_in))
+        if scales.dtype is not SCALES or scales.device != codes.device or not scales.is_contiguous() or scales.shape != shape:
+            raise ValueError(f"scales must be a contiguous {SCALES} tensor of shape {shape} beside the codes")
         self.codes, self.scales, self.device = codes, scales, codes.device
         self.ws = torch.zeros(B.crisp_matmul_workspace_bytes(), dtype=torch.uint8, device=self.device)
-        self._w, self._ws = (codes.data_ptr(), scales.data_ptr()), (self.ws.data_ptr(), self.ws.numel())
 
     @classmethod
     def from_weight(cls, weight) -> "CrispLinear":
@@ -160,18 +71,7 @@ class CrispLinear:
 
     def __call__(self, codes, scales, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         """bf16 [rows, out_features]: the operand's rows times the transposed weights."""
-        index, (rows, cols) = _rows("codes", codes, CODES)
-        if cols != self.n_in or index != self._index:
-            raise ValueError(f"codes must have {self.n_in} columns and be on {self.device}")
-        ps = _check("scales", scales, SCALES, index, (rows, self._cols))
-        if out is None:
-            out = _new(codes, (rows, self.n_out), _BF16, stream)
-            po = out.data_ptr()
-        else:
-            po = _check("out", out, _BF16, index, (rows, self.n_out))
-        _call("crisp_matmul", index, stream, (codes.data_ptr(), ps, *self._w, rows, self.n_out, cols, po, *self._ws),
-              (codes, scales, self.codes, self.scales, self.ws, out))
-        return out
+        return B.calls().matmul(codes, scales, self.codes, self.scales, self.ws, out, stream)
 
     def poll(self, stream=None) -> None:
         """Waits for the stream and raises the first error that the device has recorded since the last poll."""
@@ -202,53 +102,19 @@ class CrispRotary:
                                         high or 0.0)
         if magnitude is not None:
             self.plan.magnitude = magnitude
-        self._plan = ctypes.byref(self.plan)
+        self._plan = ctypes.addressof(self.plan)
 
     def split(self, qkv, n_q_heads: int, n_kv_heads: int, positions: Optional[torch.Tensor] = None, *, first_position: int = 0,
               stream=None):
         """q [tokens, n_q_heads, 128], k and v [tokens, n_kv_heads, 128] from a product's rows
         [tokens, (n_q_heads + 2 n_kv_heads) 128]: q and k rotated, v copied.  positions: int32 [tokens] (None: first_position,
         first_position + 1, ...)."""
-        index, shape = qkv.get_device(), qkv.shape
-        if index < 0:
-            raise RuntimeError("qkv must be a CUDA tensor (no CPU fallback)")
-        if n_q_heads <= 0 or n_kv_heads <= 0:
-            raise ValueError("there must be heads")
-        if len(shape) != 2 or shape[1] != (n_q_heads + 2 * n_kv_heads) * HEAD or qkv.dtype is not _BF16 or qkv.stride(1) != 1:
-            raise ValueError(f"qkv must be bf16 [tokens, {(n_q_heads + 2 * n_kv_heads) * HEAD}] with contiguous rows")
-        n, row = shape
-        if n > 1:
-            row = qkv.stride(0)
-        q, k = _new(qkv, (n, n_q_heads, HEAD), _BF16, stream), _new(qkv, (n, n_kv_heads, HEAD), _BF16, stream)
-        v = _new_like(k, _BF16, stream)
-        if n:
-            at = qkv.data_ptr()
-            at_k = at + 2 * HEAD * n_q_heads
-            _call("crisp_rotary", index, stream,
-                  (self._plan, n, None if positions is None else _check("positions", positions, _I32, index, (n,)), first_position,
-                   n_q_heads, n_kv_heads, at, row, at_k, row, at_k + 2 * HEAD * n_kv_heads, row, q.data_ptr(), k.data_ptr(),
-                   v.data_ptr()), (qkv, positions, q, k, v))
-        return q, k, v
+        return B.calls().rotary_split(self._plan, qkv, n_q_heads, n_kv_heads, positions, first_position, stream)
 
     def rotate(self, x, positions: Optional[torch.Tensor] = None, *, first_position: int = 0,
                out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         """bf16 x [tokens, heads, 128], whose tokens may have any stride, rotated.  out: contiguous; it may be x."""
-        index, shape = x.get_device(), x.shape
-        if index < 0:
-            raise RuntimeError("x must be a CUDA tensor (no CPU fallback)")
-        if (len(shape) != 3 or x.dtype is not _BF16 or shape[1] == 0 or shape[2] != HEAD or x.stride(2) != 1
-                or (shape[1] > 1 and x.stride(1) != HEAD)):
-            raise ValueError("x must be bf16 [tokens, heads, 128] with contiguous tokens")
-        n, heads, _ = shape
-        if out is None:
-            out = _new(x, shape, _BF16, stream)
-        po = _check("out", out, _BF16, index, shape)
-        if n:
-            _call("crisp_rotary", index, stream,
-                  (self._plan, n, None if positions is None else _check("positions", positions, _I32, index, (n,)), first_position,
-                   heads, 0, x.data_ptr(), x.stride(0) if n > 1 else heads * HEAD, None, 0, None, 0, po, None, None),
-                  (x, positions, out))
-        return out
+        return B.calls().rotary_rotate(self._plan, x, positions, first_position, out, stream)
 
 
 # ---- a layer's attention, from hidden states to hidden states
