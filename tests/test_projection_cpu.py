@@ -157,3 +157,59 @@ def test_reference_norm_and_rotary():
     # scores depend on distances alone
     a, b = (ref.rotate(x, [p, p + 4, p + 9], freq, "interleaved")[:, 0] for p in (0, 100))
     np.testing.assert_allclose(a @ a.T, b @ b.T)
+
+
+# ------------------------------------------------------------------------------------------------ the product's ring of stages
+def run_ring(stages, loaders, issuers, steps, seed):
+    """The loading and issuing warps of the product over one ring, in a random order: barriers know the parity of their phase
+    only, copies land late, products free their stage late (in order, for one issuer).  Returns what went wrong, or None."""
+    rng = np.random.RandomState(seed)
+    full, empty = [0] * stages, [0] * stages            # phases that have ended
+    holds, freed = [None] * stages, [0] * stages        # step in the stage, uses that have ended
+    load_at, issue_at = list(range(loaders)), list(range(issuers))
+    landing, running = [], [[] for _ in range(issuers)]
+    passed = lambda ended, parity: (ended & 1) != parity  # noqa: E731
+    for _ in range(60 * steps):
+        kind = rng.randint(4)
+        if kind == 0:
+            w = rng.randint(loaders)
+            i = load_at[w]
+            st, use = i % stages, i // stages
+            if i < steps and (i < stages or passed(empty[st], (use - 1) & 1)):
+                if freed[st] != use:
+                    return f"step {i} is loaded over a stage in use"
+                landing.append(i)
+                load_at[w] += loaders
+        elif kind == 1 and landing:
+            i = landing.pop(rng.randint(len(landing)))
+            holds[i % stages] = i
+            full[i % stages] += 1
+        elif kind == 2:
+            w = rng.randint(issuers)
+            i = issue_at[w]
+            if i < steps and passed(full[i % stages], (i // stages) & 1):
+                if holds[i % stages] != i:
+                    return f"step {i} finds step {holds[i % stages]}"
+                running[w].append(i)
+                issue_at[w] += issuers
+        elif kind == 3:
+            w = rng.randint(issuers)
+            if running[w]:
+                i = running[w].pop(0)
+                empty[i % stages] += 1
+                freed[i % stages] += 1
+        if min(load_at) >= steps and min(issue_at) >= steps and not any(running):
+            return None
+    return None if sum(freed) == steps else "no end"
+
+
+@pytest.mark.parametrize("stages", [2, 3, 4, 5, 6, 8, 11, 12])
+def test_ring_of_the_product(stages):
+    """Two loading warps that take turns and one that issues, as in matmul.cu and matmul_pair.cu."""
+    for seed in range(150):
+        assert run_ring(stages, 2, 1, 5 * stages + 3, seed) is None
+
+
+@pytest.mark.parametrize("stages,loaders,issuers", [(3, 4, 1), (4, 3, 2), (5, 4, 2)])
+def test_the_ring_model_sees_loaders_that_come_too_early(stages, loaders, issuers):
+    assert any(run_ring(stages, loaders, issuers, 5 * stages + 3, seed) for seed in range(400))
