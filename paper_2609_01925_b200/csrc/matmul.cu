@@ -79,6 +79,8 @@ __global__ void __launch_bounds__(kMatmulThreads, 1) matmul_kernel(const __grid_
   // (Loads and products are issued by one elected lane of a warp that stays together, and two blocks at a time: see
   // matmul_pair.cu.)
   if (warp == 4 || warp == 5) {
+    // (No more loading warps than stages: one that came to a stage before the use before last had ended would take that use's
+    // phase for the last one's.)
     int stage = warp - 4;
     uint32_t phase = 0;
     for (int kb = k0 + warp - 4; kb < k1; kb += 2) {
@@ -330,7 +332,7 @@ int launch_matmul(const void* codes, const uint8_t* scales, const void* w_codes,
   const bool alone = a.n_tiles * a.split <= n_sm - (a.split > 2 ? 4 * a.split : 0);
   const bool deep = is_wide(a.tile_tokens) || (alone && ceil_div(blocks, a.split) >= 24);
   const int budget = (deep ? 200 : 104) * 1024, stage_bytes = (kTileFeatures + a.tile_tokens) * kScaleBlock;
-  a.stages = budget / stage_bytes < kMaxStages ? budget / stage_bytes : kMaxStages;
+  a.stages = budget / stage_bytes < kMaxStages ? budget / stage_bytes : kMaxStages;   // 2 at least
   const size_t smem = budget + 1024;
   CUtensorMap tw, ta;
   rc = make_tmap_operand(&tw, w_codes, n_out, n_cols, kTileFeatures);
