@@ -51,8 +51,8 @@ __global__ void __launch_bounds__(kMatmulThreads, 1) matmul_kernel(const __grid_
   if (warp == 4 && elect_one()) {
     // the weights set out for L2 while the kernel before this one ends
     for (int kb = k0; kb < k1; ++kb) tma_prefetch_2d(&tw, kb * kScaleBlock, f0);
+    prefetch_tmap(&ta);
   }
-  pdl_enter();
   if (tid == 0) {
     for (int i = 0; i < a.stages; ++i) {
       mbar_init(&s.full[i], 1);
@@ -66,6 +66,7 @@ __global__ void __launch_bounds__(kMatmulThreads, 1) matmul_kernel(const __grid_
     s.abort_flag = 0;
     fence_mbar_init();
   }
+  pdl_enter();
   if (warp == 6) {
     tmem_alloc(&s.tmem, a.tmem_cols);
     tmem_relinquish();

@@ -42,7 +42,11 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_pair_kernel(const __grid_c
   const long long pairs = gridDim.x / 2, first = blockIdx.x / 2;
   const int blocks = (a.n_cols + kScaleBlock - 1) / kScaleBlock, words = (a.n_cols + kScaleWord - 1) / kScaleWord;
   const int stage_bytes = (kRows + a.tile_tokens / 2) * kScaleBlock;
-  pdl_enter();
+  if (warp == 8 && elect_one()) {   // (what does not depend on the kernel before this one comes before the wait for it)
+    prefetch_tmap(&tw);
+    prefetch_tmap(&ta);
+    prefetch_tmap(&to);
+  }
   if (tid == 0) {
     for (int i = 0; i < kStages; ++i) {
       mbar_init(&s.full[i], 1);
@@ -59,6 +63,7 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_pair_kernel(const __grid_c
     s.abort_flag = 0;
     fence_mbar_init();
   }
+  pdl_enter();
   if (warp == 10) {
     tmem_alloc_pair(&s.tmem, 512);
     tmem_relinquish_pair();
