@@ -174,6 +174,7 @@ __global__ void __launch_bounds__(kMatmulThreads, 1) matmul_kernel(const __grid_
       tc_fence_before_sync();
       __syncwarp();
       if (lane == 0) mbar_arrive(&s.scale_full[slot]);
+      __syncwarp();
     }
     ok = ok && mbar_wait_warp(&s.done, 0, abort_flag);
     if (ok) {
@@ -262,7 +263,16 @@ struct Plan {
   long long rounds = 0, ns = INT64_MAX;
 };
 
-bool is_wide(int tile_tokens) { return tile_tokens > 208; }   // wants all of an SM's TMEM
+// TMEM columns of a tile: accumulators and the slots of scales, a power of two.
+constexpr int tmem_columns(int tile_tokens) {
+  const int used = (tile_tokens + 31) / 32 * 32 + kScaleSlots * (tile_tokens > 128 ? 12 : 8);
+  int columns = 32;
+  while (columns < used) columns *= 2;
+  return columns;
+}
+// Tiles that want all of an SM's TMEM get all of its shared memory, so that no second CTA comes to the SM: it would wait for TMEM
+// while its cluster waits for it.  Of the others an SM holds two.
+constexpr bool is_wide(int tile_tokens) { return tmem_columns(tile_tokens) > 256; }
 
 // Tiles of 128 features, each block of columns in one of `split` CTAs.  A launch and an exchange take 3 and 0.8 us; a block takes
 // a CTA 185 ns with 16 tokens, 290 with 64, 520 with 128 and more (its loads' latency over the few stages of its ring); more
@@ -323,15 +333,12 @@ int launch_matmul(const void* codes, const uint8_t* scales, const void* w_codes,
   a.n_feature_tiles = ceil_div(n_out, kTileFeatures);
   a.n_tiles = static_cast<long long>(a.n_feature_tiles) * ceil_div(n_rows, a.tile_tokens);
   if (a.n_tiles > INT32_MAX / kMaxSplit) return CRISP_ERR_UNSUPPORTED;
-  // accumulators, then the slots of scales; an SM holds one CTA of the wide tiles and two of the others, so that the CTAs of
-  // an SM never want more than its 512 columns.  A CTA that has an SM to itself and much to read gets a longer ring (33 rows,
-  // 8192 x 8192 weights: 20.9 -> 16.9 us); with less to read room for the next call's CTAs is worth more (1 row, 6144 x 4096
-  // weights: 7.9 us with the long ring, 7.2 without).
-  const int used = ceil_div(a.tile_tokens, 32) * 32 + kScaleSlots * (a.tile_tokens > 128 ? 12 : 8);
-  a.tmem_cols = 32;
-  while (a.tmem_cols < used) a.tmem_cols *= 2;
+  // A CTA that has an SM to itself and much to read gets a longer ring (33 rows, 8192 x 8192 weights: 20.9 -> 16.9 us); with less
+  // to read room for the next call's CTAs is worth more (1 row, 6144 x 4096 weights: 7.9 us with the long ring, 7.2 without).
+  a.tmem_cols = tmem_columns(a.tile_tokens);
   const bool alone = a.n_tiles * a.split <= n_sm - (a.split > 2 ? 4 * a.split : 0);
   const bool deep = is_wide(a.tile_tokens) || (alone && ceil_div(blocks, a.split) >= 24);
+  static_assert(2 * (104 * 1024 + 1024 + sizeof(MatmulSmem) + 1024) <= 228 * 1024 && 3 * 104 > 228 && 200 + 104 > 228, "CTAs of an SM");
   const int budget = (deep ? 200 : 104) * 1024, stage_bytes = (kTileFeatures + a.tile_tokens) * kScaleBlock;
   a.stages = budget / stage_bytes < kMaxStages ? budget / stage_bytes : kMaxStages;   // 2 at least
   const size_t smem = budget + 1024;

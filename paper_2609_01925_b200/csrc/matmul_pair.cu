@@ -211,6 +211,7 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_pair_kernel(const __grid_c
           tc_fence_before_sync();
           __syncwarp();
           if (lane == 0) cluster_arrive(cluster_map(smem_u32(&s.scale_full[slot]), 0));
+          __syncwarp();
         }
         if (++slot == kSlots) {
           slot = 0;
@@ -244,6 +245,7 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_pair_kernel(const __grid_c
             tc_fence_before_sync();
             __syncwarp();
             if (lane == 0) cluster_arrive(cluster_map(smem_u32(&s.acc_empty[buf]), 0));
+            __syncwarp();
           }
         }
         if (by_tma && member == 0) {

@@ -179,7 +179,7 @@ int launch_rotary(const crisp_rotary_plan& plan, int n_tokens, const int32_t* po
   // whose four took 490).  Where input and output fit L2, two at a time, read once, are ahead (5003 tokens of 28/4 heads: 12.1 us; in
   // that build 14.6, and 15.9 with four, kept), and a few tokens are spread over the SMs.
   const long long bytes = static_cast<long long>(n_tokens) * a.items * 64;
-  if (static_cast<long long>(n_tokens) * a.items <= 4ll * n_sm * 384) {
+  if (n_tokens <= 4 * n_sm) {
     launch_tokens<1, false>(a, stream);
   } else if (bytes <= 120ll << 20) {
     launch_tokens<2, true>(a, stream);

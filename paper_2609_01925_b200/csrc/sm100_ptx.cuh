@@ -305,6 +305,7 @@ __device__ __forceinline__ uint32_t cluster_rank() {
 }
 // Every thread of every CTA of the cluster calls it; what they wrote to shared memory before is visible after it.
 __device__ __forceinline__ void cluster_sync() {
+  __syncwarp();
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 // The address of a peer CTA's copy of a shared-memory variable, and a load from there.
@@ -313,36 +314,10 @@ __device__ __forceinline__ uint32_t cluster_map(uint32_t saddr, uint32_t rank) {
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(saddr), "r"(rank));
   return r;
 }
-// Arrive on a barrier of the cluster (an address of cluster_map), ordering this thread's earlier work before it.
+// Arrive on a barrier of the cluster (an address of cluster_map).  Without `.release.cluster`, a memory barrier that would wait for
+// the thread's stores to global memory: what these arrivals order is tcgen05 work, and tc_fence_before_sync orders that.
 __device__ __forceinline__ void cluster_arrive(uint32_t bar) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-// mbar_wait for a barrier on which threads of other CTAs of the cluster arrive.
-__device__ __forceinline__ bool mbar_try_wait_cluster(uint64_t* bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok)
-      : "r"(smem_u32(bar)), "r"(parity)
-      : "memory");
-  return ok != 0;
-}
-__device__ __forceinline__ bool mbar_wait_cluster(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
-  if (mbar_try_wait_cluster(bar, parity)) return true;
-  const unsigned long long t0 = global_timer_ns();
-  for (;;) {
-    if (mbar_try_wait_cluster(bar, parity)) return true;
-    if (*abort_flag) return false;
-    if (global_timer_ns() - t0 > kWaitLimitNs) break;
-  }
-  *abort_flag = 1;
-  return false;
-}
-__device__ __forceinline__ bool mbar_wait_cluster_warp(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
-  const bool ok = mbar_wait_cluster(bar, parity, abort_flag);
-  return __all_sync(0xffffffffu, ok);
 }
 __device__ __forceinline__ float4 cluster_load4(uint32_t addr) {
   float4 v;

@@ -50,7 +50,11 @@ def rms_norm_quantize(x, weight=None, residual=None, *, eps: float = 1e-5, sum_o
 
 # ---- products
 class CrispLinear:
-    """Weights [out_features, in_features] as an operand, and products with them."""
+    """Weights [out_features, in_features] as an operand, and products with them.
+
+    Products of one object may overlap, on any streams (they share a status word only), behind the object's creation, which
+    zeroes that word on the current stream.
+    """
 
     def __init__(self, codes, scales):
         if not codes.is_cuda:

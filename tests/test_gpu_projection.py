@@ -232,7 +232,8 @@ def test_product_of_whole_numbers_is_exact(rows, n, cols):
 
 
 @pytest.mark.parametrize("rows,n,cols", [(9000, 2056, 656), (9000, 2051, 656), (9000, 2050, 112), (2500, 4097, 1280), (20000, 45, 256),
-                                         (3987, 20, 1120), (129, 6144, 2064), (1000, 1024, 8192), (48, 128, 20000)])
+                                         (3987, 20, 1120), (129, 6144, 2064), (1000, 1024, 8192), (48, 128, 20000), (200, 4224, 1024),
+                                         (208, 2048, 2048), (230, 1000, 4096), (160, 512, 8192), (64, 20000, 512)])
 def test_product_over_many_tiles_is_exact(rows, n, cols):
     """Several tiles one after the other in a CTA, rows of every alignment, few features, many columns: made on the GPU, otherwise
     as above."""
