@@ -411,6 +411,8 @@ int crisp_quantize(const void* x, int32_t n_rows, int32_t n_cols, void* codes, u
  *   y = h / sqrt(mean(h^2) + eps) * weight            (weight [n_cols] bf16, NULL: 1), the mean in fp32
  * (a row whose squares leave fp32 becomes 0),
  * written either as bf16 `y` or as an operand, `codes` and `scales` (converted from fp32, not from bf16); the other is NULL.
+ * (y is fp32 before it is converted: where a block's largest magnitude is within 48 * 2^-24 of the bound of a scale, the scale
+ * may be the one on the other side; codes go with it.)
  * sum may be x or residual, and y may be x: rows are read before they are written.  n_cols is a multiple of 16, at most 32768.
  */
 int crisp_rms_norm(const void* x, const void* residual, const void* weight, int32_t n_rows, int32_t n_cols, float eps,

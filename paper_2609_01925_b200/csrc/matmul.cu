@@ -9,6 +9,8 @@
 // instruction's descriptor says which byte it uses.  So a cell serves 512 columns, and the cells of 128 rows are four TMEM
 // columns: four warps load the words straight from memory and store them to TMEM (each to its own quarter of the lanes, since
 // the tensor core wants them in all four).
+//
+// Bound by latency and L2, not by products.  1 token, 4096 -> 6144: 6.5 us (weights 25 MB); 33 tokens, 4096 -> 4096: 6.2 us.
 #include <atomic>
 
 #include "matmul.cuh"

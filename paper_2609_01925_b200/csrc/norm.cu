@@ -5,6 +5,9 @@
 // between its only read and its only write: 8 bytes of traffic per element (x, residual, h, and one byte of codes makes 7)
 // instead of the 16 and more of separate passes.  What is normalised is h as stored, so that the result does not depend on
 // whether the addition was part of this call.  The sum of squares is held in fp32.
+//
+// Measured: 131072 rows of 4096, addition, 8 bits out: 558 us, 6.7 TB/s; 9001 rows of 3584, 16 bits out: 20 us; one row: 1.9 us.
+// quantize, 32768 rows of 4096: 62.7 us, 6.4 TB/s; 6144 rows: 13.0 us.
 #include "cache.cuh"
 #include "operand.cuh"
 

@@ -116,6 +116,14 @@ def test_norm_extremes():
         check_norm(x[1:], torch.zeros_like(x[1:]), None, 0.0, quantized)
 
 
+@pytest.mark.parametrize("cols", [80, 128, 4096])
+def test_norm_at_the_bound_of_a_scale(cols):
+    """Rows whose largest result is 448 * 2^-8 but for the roundings, and the 16-bit numbers beside it."""
+    x = torch.stack([torch.full((cols,), c) for c in (0.3, 1.0, 7.0, 1e-3, 2.0 ** 30)]).bfloat16()
+    for w in (1.75, 1.75 - 2.0 ** -7, 1.75 + 2.0 ** -7):
+        check_norm(x, x * 0.7, torch.full((cols,), w).bfloat16(), 0.0, True)
+
+
 def test_norm_nan_stays_in_its_row():
     x = normal(3, 4096, seed=6)
     clean = crisp.rms_norm_quantize(x.to(DEV))
