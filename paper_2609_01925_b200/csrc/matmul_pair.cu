@@ -5,8 +5,8 @@
 // The CTAs are persistent.  Roles: warps 0..3 and 11..14 write finished tiles, 4..7 bring scales to TMEM, 8 and 9 load codes (TMA),
 // 10 issues the products (first CTA of the pair).  TMEM holds two tiles' accumulators, so that one is written while the other is computed.
 //
-// 32768 tokens, 4096 -> 6144: 535 to 560 us, 3.0 PFLOP/s, bound by the tensor pipe (91 % active); over seconds the board's
-// power cap leaves 2.65.  700 tokens, 3584 -> 4608: 12.0 us, one round of 72 pairs.
+// 32768 tokens, 4096 -> 6144: 535 to 578 us, 2.9 to 3.1 PFLOP/s, bound by the tensor pipe (91 % active); over seconds the board's
+// power cap leaves 2.4 to 2.65 (687 to 622 us).  700 tokens, 3584 -> 4608: 12.0 us, one round of 72 pairs.
 #include <atomic>
 
 #include "matmul.cuh"
