@@ -106,19 +106,18 @@ class CrispRotary:
                                         high or 0.0)
         if magnitude is not None:
             self.plan.magnitude = magnitude
-        self._plan = ctypes.addressof(self.plan)
 
     def split(self, qkv, n_q_heads: int, n_kv_heads: int, positions: Optional[torch.Tensor] = None, *, first_position: int = 0,
               stream=None):
         """q [tokens, n_q_heads, 128], k and v [tokens, n_kv_heads, 128] from a product's rows
         [tokens, (n_q_heads + 2 n_kv_heads) 128]: q and k rotated, v copied.  positions: int32 [tokens] (None: first_position,
         first_position + 1, ...)."""
-        return B.calls().rotary_split(self._plan, qkv, n_q_heads, n_kv_heads, positions, first_position, stream)
+        return B.calls().rotary_split(ctypes.addressof(self.plan), qkv, n_q_heads, n_kv_heads, positions, first_position, stream)
 
     def rotate(self, x, positions: Optional[torch.Tensor] = None, *, first_position: int = 0,
                out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         """bf16 x [tokens, heads, 128], whose tokens may have any stride, rotated.  out: contiguous; it may be x."""
-        return B.calls().rotary_rotate(self._plan, x, positions, first_position, out, stream)
+        return B.calls().rotary_rotate(ctypes.addressof(self.plan), x, positions, first_position, out, stream)
 
 
 # ---- a layer's attention, from hidden states to hidden states

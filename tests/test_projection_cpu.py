@@ -213,3 +213,31 @@ def test_ring_of_the_product(stages):
 @pytest.mark.parametrize("stages,loaders,issuers", [(3, 4, 1), (4, 3, 2), (5, 4, 2)])
 def test_the_ring_model_sees_loaders_that_come_too_early(stages, loaders, issuers):
     assert any(run_ring(stages, loaders, issuers, 5 * stages + 3, seed) for seed in range(400))
+
+
+@pytest.mark.parametrize("way", ["copy", "deepcopy", "pickle"])
+def test_a_copied_rotary_uses_its_own_plan(way, monkeypatch):
+    """The address that a call is given is that of the plan the object holds, whatever became of the object it was made from."""
+    import copy
+    import ctypes
+    import pickle
+    given = []
+
+    class Calls:
+        def rotary_split(self, plan, *rest):
+            given.append(plan)
+
+        def rotary_rotate(self, plan, *rest):
+            given.append(plan)
+
+    monkeypatch.setattr(crisp.binding, "calls", Calls)
+    first = crisp.CrispRotary(1e4, rotary_dim=64)
+    made = {"copy": copy.copy, "deepcopy": copy.deepcopy, "pickle": lambda r: pickle.loads(pickle.dumps(r))}[way](first)
+    assert bytes(made.plan) == bytes(first.plan)
+    made.split(None, 4, 1)
+    made.rotate(None)
+    made.plan = crisp.CrispRotary(5e5).plan
+    made.split(None, 4, 1)
+    assert given[2] == ctypes.addressof(made.plan) and given[0] == given[1]
+    if way != "copy":
+        assert given[0] != ctypes.addressof(first.plan)
