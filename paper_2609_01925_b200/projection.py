@@ -102,6 +102,8 @@ class CrispRotary:
             raise ValueError(f"layout must be one of {sorted(_LAYOUTS)}, not {layout!r}")
         if scaling not in _SCALINGS:
             raise ValueError(f"scaling must be one of {sorted(_SCALINGS)}, not {scaling!r}")
+        if any(turns is not None and not turns > 0 for turns in (low, high)):
+            raise ValueError("low and high must be positive")   # (zero stands for the usual turns in the C call)
         self.plan = B.crisp_rotary_init(rotary_dim, _LAYOUTS[layout], theta, _SCALINGS[scaling], factor, original, low or 0.0,
                                         high or 0.0)
         if magnitude is not None:

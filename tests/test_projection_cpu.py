@@ -241,3 +241,11 @@ def test_a_copied_rotary_uses_its_own_plan(way, monkeypatch):
     assert given[2] == ctypes.addressof(made.plan) and given[0] == given[1]
     if way != "copy":
         assert given[0] != ctypes.addressof(first.plan)
+
+
+@pytest.mark.parametrize("kw", [dict(low=0.0), dict(high=0.0), dict(low=0), dict(low=float("nan"))])
+@pytest.mark.parametrize("scaling", ["ramp", "bands"])
+def test_turns_of_zero_are_refused(scaling, kw):
+    """None stands for the usual turns; zero is not taken for it."""
+    with pytest.raises((ValueError, RuntimeError)):
+        crisp.CrispRotary(5e5, scaling=scaling, factor=8.0, original=8192, **kw)
