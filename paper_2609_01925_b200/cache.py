@@ -104,6 +104,20 @@ class CrispCache:
         if any(self._tokens(name, t, tokens, self.n_kv_heads) % 16 for name, t in (("k", k), ("v", v))):
             raise B.CrispError(B.ERR_INVALID_ARG, "crisp_cache_append")
 
+    def check_append(self, tokens, n_kv_heads, seq_ids, cu_tokens=None, n_new=None, layer=0):
+        """Raises what reserve and append would on the host for that many tokens of n_kv_heads heads, whose K and V need not be
+        there yet: nothing is enqueued."""
+        if n_kv_heads != self.n_kv_heads:
+            raise ValueError(f"k and v must have {self.n_kv_heads} heads, not {n_kv_heads}")
+        self._list("seq_ids", seq_ids)
+        batch = seq_ids.shape[0]
+        self._list("cu_tokens", cu_tokens, batch + 1)
+        self._list("n_new", n_new, batch)
+        if batch > B.CACHE_MAX_BATCH:
+            raise B.CrispError(B.ERR_UNSUPPORTED, "crisp_cache_append")
+        if not 0 <= layer < self.n_layers or (batch > 0 and cu_tokens is None and tokens % batch != 0):
+            raise B.CrispError(B.ERR_INVALID_ARG, "crisp_cache_append")
+
     def _call(self, name, stream, *args):
         """The C call of that name on (cache, *args, stream), with the cache's device current.  (The answering loop calls
         this once or more per layer and token, so the way to the library is kept short.)"""

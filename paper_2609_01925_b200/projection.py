@@ -153,6 +153,16 @@ class CrispAttention:
                cache_layer: int = 0, dense_below_tokens: int = 0, stream=None):
         """A whole prompt: x [layer.p.seq_len, in_features] through CrispLayer.forward; with a cache its K and V are kept there
         (CrispLayer.store).  Returns (out, h)."""
+        # (the attention is given pointers and takes sizes from layer.p: all of this comes before the first launch)
+        p = layer.p
+        if x.dim() != 2 or x.shape[0] != p.seq_len:
+            raise ValueError(f"x must be [{p.seq_len}, {self.qkv.n_in}], the layer's tokens")
+        if (p.n_q_heads, p.n_kv_heads) != (self.n_q_heads, self.n_kv_heads) or layer.o.device != self.qkv.device:
+            raise ValueError(f"the layer must have {self.n_q_heads} / {self.n_kv_heads} heads and be on {self.qkv.device}")
+        if cache is not None:
+            if seq_ids is None or seq_ids.shape != (1,):
+                raise ValueError("seq_ids must name one sequence")
+            cache.check_append(p.seq_len, self.n_kv_heads, seq_ids, layer=cache_layer)
         q, k, v, h = self.project(x, residual, stream=stream)
         o = layer.forward(q, k, v, stream=stream, dense_below_tokens=dense_below_tokens)
         if cache is not None:

@@ -1,0 +1,130 @@
+"""CrispAttention, CrispLayer and CrispCache without a GPU: what they hand to the library, and what they refuse before the first call.
+The library and the compiled calls are replaced by stand-ins that write down what they are given; nothing is launched."""
+import types
+
+import pytest
+import torch
+
+import paper_2609_01925_b200 as crisp
+from paper_2609_01925_b200 import binding as B
+
+CPU = torch.device("cpu")
+HQ, HKV, HIDDEN = 4, 2, 64
+
+
+class Calls:
+    """Stand-in for the compiled calls: outputs of the right shapes, and a list of what was called."""
+
+    def __init__(self, log):
+        self.log = log
+
+    def rms_norm(self, x, weight, residual, eps, sum_out, quantized, stream):
+        self.log.append("rms_norm")
+        return x, x, None if residual is None else residual
+
+    def matmul(self, codes, scales, w_codes, w_scales, ws, out, stream):
+        self.log.append("matmul")
+        return torch.zeros(codes.shape[0], w_codes.shape[0], dtype=torch.bfloat16)
+
+    def rotary_split(self, plan, qkv, hq, hkv, positions, first, stream):
+        self.log.append("rotary")
+        return tuple(torch.zeros(qkv.shape[0], h, 128, dtype=torch.bfloat16) for h in (hq, hkv, hkv))
+
+    def quantize(self, x, stream):
+        self.log.append("quantize")
+        return x, x
+
+
+class Library:
+    """Stand-in for libcrisp.so's calls of the cache."""
+
+    def __init__(self, log):
+        self.log = log
+
+    def __getattr__(self, name):
+        return lambda *args: self.log.append(name) or B.OK
+
+
+def linear(n_out, n_in):
+    made = object.__new__(crisp.CrispLinear)
+    made.codes, made.scales, made.ws = torch.zeros(n_out, n_in, dtype=torch.uint8), None, None
+    made.n_out, made.n_in, made.device = n_out, n_in, CPU
+    return made
+
+
+def make_cache(log, heads=HKV, layers=2, device=CPU):
+    cache = object.__new__(crisp.CrispCache)
+    cache.device, cache.n_kv_heads, cache.n_layers = device, heads, layers
+    cache._pages_ws = cache._attention_ws = (0, 0)
+    cache._call = lambda name, stream, *args: log.append(name)
+    cache._used = lambda *args: None
+    return cache
+
+
+def make_layer(log, tokens, hq=HQ, hkv=HKV):
+    layer = object.__new__(crisp.CrispLayer)
+    layer.p = crisp.make_params(tokens, hq, hkv)
+    layer.o = torch.zeros(tokens, hq, 128, dtype=torch.bfloat16)
+    layer.n_tokens = torch.full((1,), tokens, dtype=torch.int32)
+    layer.forward = lambda *args, **kw: log.append("forward") or layer.o
+    return layer
+
+
+@pytest.fixture
+def log(monkeypatch):
+    made = []
+    monkeypatch.setattr(B, "calls", lambda: Calls(made))
+    return made
+
+
+@pytest.fixture
+def block():
+    return crisp.CrispAttention(linear((HQ + 2 * HKV) * 128, HIDDEN), linear(HIDDEN, HQ * 128), crisp.CrispRotary(1e4), HQ, HKV)
+
+
+def states(tokens, cols=HIDDEN):
+    return torch.zeros(tokens, cols, dtype=torch.bfloat16)
+
+
+def ids(*which):
+    return torch.tensor(which, dtype=torch.int32)
+
+
+# ------------------------------------------------------------------------------------------------ a prompt
+def test_prompt_calls(log, block):
+    block.prompt(states(300), make_layer(log, 300))
+    assert log == ["rms_norm", "matmul", "rotary", "forward", "quantize", "matmul"]
+    log.clear()
+    block.prompt(states(300), make_layer(log, 300), cache=make_cache(log), seq_ids=ids(1))
+    assert log == ["rms_norm", "matmul", "rotary", "forward", "crisp_cache_reserve", "crisp_cache_append", "quantize", "matmul"]
+    log.clear()
+    block.prompt(states(300), make_layer(log, 300), cache=make_cache(log), seq_ids=ids(1), cache_layer=1)
+    assert log == ["rms_norm", "matmul", "rotary", "forward", "crisp_cache_append", "quantize", "matmul"]
+
+
+@pytest.mark.parametrize("tokens,hq,hkv", [(1024, HQ, HKV), (299, HQ, HKV), (301, HQ, HKV), (300, 32, 8), (300, HQ, 1), (300, 2, 2)])
+def test_prompt_refuses_a_layer_of_another_size(log, block, tokens, hq, hkv):
+    """The attention takes its sizes from the layer, and would read past the ends of shorter tensors."""
+    with pytest.raises(ValueError):
+        block.prompt(states(300), make_layer(log, tokens, hq, hkv))
+    assert log == []
+
+
+def test_prompt_refuses_a_layer_elsewhere(log, block):
+    layer = make_layer(log, 300)
+    layer.o = types.SimpleNamespace(device=torch.device("cuda", 1))
+    with pytest.raises(ValueError):
+        block.prompt(states(300), layer)
+    with pytest.raises(ValueError):
+        block.prompt(states(300)[0], make_layer(log, 300))
+    assert log == []
+
+
+@pytest.mark.parametrize("kw", [dict(seq_ids=None), dict(seq_ids=ids(0, 1)), dict(seq_ids=ids(0).long()), dict(seq_ids=ids(0), heads=1),
+                                dict(seq_ids=ids(0), heads=8), dict(seq_ids=ids(0), cache_layer=2), dict(seq_ids=ids(0), cache_layer=-1),
+                                dict(seq_ids=ids(0), device=torch.device("cuda", 1))])
+def test_prompt_refuses_what_the_cache_would(log, block, kw):
+    cache = make_cache(log, kw.get("heads", HKV), device=kw.get("device", CPU))
+    with pytest.raises((ValueError, crisp.CrispError)):
+        block.prompt(states(300), make_layer(log, 300), cache=cache, seq_ids=kw["seq_ids"], cache_layer=kw.get("cache_layer", 0))
+    assert log == []
