@@ -42,29 +42,35 @@ class CrispLayer:
         self.lse = torch.empty(hq, n, dtype=torch.float32, device=dev) if with_lse else None
         self.n_tokens = torch.full((1,), n, dtype=torch.int32, device=dev)
 
+    # ---- calls: on `stream` (a torch stream or its handle; default: the current stream of the layer's device), with that
+    # device current
+    def _call(self, name, stream, *args):
+        index = self.o.device.index
+        if stream is None:
+            stream = torch._C._cuda_getCurrentRawStream(index)
+        with torch.cuda.device(index):
+            B.check(getattr(B, name)(*args, stream), name)
+
     def route(self, q, k, stream=None):
-        B.check(B.crisp_route(self.p, q, k, self.route_ws, self.c_struct, self.pattern, self.p_v,
-                              self.p_s, stream), "crisp_route")
+        self._call("crisp_route", stream, self.p, q, k, self.route_ws, self.c_struct, self.pattern, self.p_v, self.p_s)
 
     def select(self, q, k, stream=None):
-        B.check(B.crisp_select(self.p, q, k, self.pattern, self.p_v, self.p_s, self.select_ws,
-                               self.row_ptr, self.col_idx, self.capacity, self.nnz, stream),
-                "crisp_select")
+        self._call("crisp_select", stream, self.p, q, k, self.pattern, self.p_v, self.p_s, self.select_ws, self.row_ptr,
+                   self.col_idx, self.capacity, self.nnz)
 
     def sparse_prefill(self, q, k, v, stream=None):
-        B.check(B.crisp_sparse_prefill(self.p, q, k, v, self.row_ptr, self.col_idx, self.prefill_ws,
-                                       self.o, self.lse, stream), "crisp_sparse_prefill")
+        self._call("crisp_sparse_prefill", stream, self.p, q, k, v, self.row_ptr, self.col_idx, self.prefill_ws, self.o,
+                   self.lse)
 
     def dense_prefill(self, q, k, v, stream=None):
-        B.check(B.crisp_dense_prefill(self.p, q, k, v, self.prefill_ws, self.o, self.lse, stream),
-                "crisp_dense_prefill")
+        self._call("crisp_dense_prefill", stream, self.p, q, k, v, self.prefill_ws, self.o, self.lse)
 
     def forward(self, q, k, v, stream=None, dense_below_tokens: int = 0):
         """Algorithm 1 through crisp_forward (one C call: route, select, sparse attention, or the dense
         kernel when seq_len < dense_below_tokens).  Returns O [n, H_q, 128] bf16."""
-        B.check(B.crisp_forward(self.p, q, k, v, self.route_ws, self.select_ws, self.prefill_ws, self.c_struct,
-                                self.pattern, self.p_v, self.p_s, self.row_ptr, self.col_idx, self.capacity,
-                                self.nnz, self.o, self.lse, dense_below_tokens, stream), "crisp_forward")
+        self._call("crisp_forward", stream, self.p, q, k, v, self.route_ws, self.select_ws, self.prefill_ws, self.c_struct,
+                   self.pattern, self.p_v, self.p_s, self.row_ptr, self.col_idx, self.capacity, self.nnz, self.o, self.lse,
+                   dense_below_tokens)
         return self.o
 
     def store(self, k, v, cache, seq_ids, cache_layer: int = 0, stream=None):
@@ -78,5 +84,8 @@ class CrispLayer:
         cache.append(k, v, seq_ids, layer=cache_layer, stream=stream)
 
     def poll(self, stream=None):
-        for ws, name in ((self.route_ws, "route"), (self.select_ws, "select"), (self.prefill_ws, "prefill")):
-            B.check(B.crisp_poll_device_status(ws, stream), f"device status ({name})")
+        if stream is None:
+            stream = torch.cuda.current_stream(self.o.device)
+        with torch.cuda.device(self.o.device):
+            for ws, name in ((self.route_ws, "route"), (self.select_ws, "select"), (self.prefill_ws, "prefill")):
+                B.check(B.crisp_poll_device_status(ws, stream), f"device status ({name})")

@@ -128,3 +128,61 @@ def test_prompt_refuses_what_the_cache_would(log, block, kw):
     with pytest.raises((ValueError, crisp.CrispError)):
         block.prompt(states(300), make_layer(log, 300), cache=cache, seq_ids=kw["seq_ids"], cache_layer=kw.get("cache_layer", 0))
     assert log == []
+
+
+# ------------------------------------------------------------------------------------------------ a layer on another device
+class Cuda:
+    """Two devices, of which device 0 is current; the current streams have the handles 100 and 101."""
+
+    def __init__(self, monkeypatch):
+        self.now = 0
+        cuda = self
+
+        class Guard:
+            def __init__(self, device):
+                self.to = device if isinstance(device, int) else device.index
+
+            def __enter__(self):
+                self.back, cuda.now = cuda.now, self.to
+
+            def __exit__(self, *args):
+                cuda.now = self.back
+
+        def current_stream(device=None):
+            index = cuda.now if device is None else torch.device(device).index
+            return types.SimpleNamespace(cuda_stream=100 + index)
+
+        monkeypatch.setattr(torch.cuda, "device", Guard)
+        monkeypatch.setattr(torch.cuda, "current_stream", current_stream)
+        monkeypatch.setattr(torch.cuda, "current_device", lambda: cuda.now)
+        monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda index: 100 + index, raising=False)
+
+
+@pytest.mark.parametrize("stream,handle", [(None, 101), (7, 7), (types.SimpleNamespace(cuda_stream=9), 9)])
+def test_a_layer_s_calls_run_on_its_device(monkeypatch, stream, handle):
+    """Whatever device is current, a layer's own is during its calls, and their stream is its current one if none is given."""
+    cuda, given = Cuda(monkeypatch), []
+
+    class Lib:
+        def __getattr__(self, name):
+            return lambda *args: given.append((name, cuda.now, args[-1])) or B.OK
+
+    monkeypatch.setattr(B, "load", lambda: Lib())
+    layer = object.__new__(crisp.CrispLayer)
+    layer.p = crisp.make_params(300, HQ, HKV)
+    for name in ("c_struct", "pattern", "p_v", "p_s", "row_ptr", "col_idx", "nnz", "lse"):
+        setattr(layer, name, None)
+    layer.route_ws = layer.select_ws = layer.prefill_ws = torch.zeros(256, dtype=torch.uint8)
+    layer.capacity = 1
+    layer.o = types.SimpleNamespace(device=torch.device("cuda", 1), data_ptr=lambda: 0)
+    q = torch.zeros(1)
+    layer.forward(q, q, q, stream=stream)
+    layer.route(q, q, stream)
+    layer.select(q, q, stream)
+    layer.sparse_prefill(q, q, q, stream)
+    layer.dense_prefill(q, q, q, stream)
+    layer.poll(stream)
+    assert [name for name, _, _ in given] == ["crisp_forward", "crisp_route", "crisp_select", "crisp_sparse_prefill",
+                                              "crisp_dense_prefill"] + 3 * ["crisp_poll_device_status"]
+    assert all(device == 1 and at == handle for _, device, at in given)
+    assert cuda.now == 0
