@@ -30,6 +30,7 @@ ERR_BAD_CACHE = -9
 PATTERN_PE, PATTERN_VS = 0, 1
 CACHE_E4M3, CACHE_INT8 = 0, 1
 CACHE_MAX_BATCH = 1024
+MAX_GROUP = 16             # query heads per K/V head
 ROTARY_HALF, ROTARY_INTERLEAVED = 0, 1
 ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_BASE, ROTARY_RAMP, ROTARY_BANDS = range(5)
 

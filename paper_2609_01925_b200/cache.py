@@ -6,6 +6,7 @@ to libcrisp.so.  Nothing is computed in Python and nothing waits for the device,
 from __future__ import annotations
 
 import ctypes
+import operator
 from typing import Optional
 
 import torch
@@ -104,9 +105,10 @@ class CrispCache:
         if any(self._tokens(name, t, tokens, self.n_kv_heads) % 16 for name, t in (("k", k), ("v", v))):
             raise B.CrispError(B.ERR_INVALID_ARG, "crisp_cache_append")
 
-    def check_append(self, tokens, n_kv_heads, seq_ids, cu_tokens=None, n_new=None, layer=0):
+    def check_append(self, tokens, n_kv_heads, seq_ids, cu_tokens=None, n_new=None, layer=0) -> int:
         """Raises what reserve and append would on the host for that many tokens of n_kv_heads heads, whose K and V need not be
-        there yet: nothing is enqueued."""
+        there yet: nothing is enqueued.  Returns the layer as a number that the calls take."""
+        layer = operator.index(layer)
         if n_kv_heads != self.n_kv_heads:
             raise ValueError(f"k and v must have {self.n_kv_heads} heads, not {n_kv_heads}")
         self._list("seq_ids", seq_ids)
@@ -117,6 +119,23 @@ class CrispCache:
             raise B.CrispError(B.ERR_UNSUPPORTED, "crisp_cache_append")
         if not 0 <= layer < self.n_layers or (batch > 0 and cu_tokens is None and tokens % batch != 0):
             raise B.CrispError(B.ERR_INVALID_ARG, "crisp_cache_append")
+        return layer
+
+    def check_attention(self, tokens, n_q_heads, seq_ids, cu_tokens=None, max_new: Optional[int] = None) -> int:
+        """The same for attention of that many tokens of n_q_heads heads, where check_append has passed.  Returns max_new."""
+        batch = seq_ids.shape[0]
+        max_new = self._max_new(tokens, batch, cu_tokens) if max_new is None else operator.index(max_new)
+        per = tokens // batch if batch > 0 and cu_tokens is None else 0
+        if not per <= max_new < 1 << 31 or n_q_heads <= 0 or n_q_heads % self.n_kv_heads != 0:
+            raise B.CrispError(B.ERR_INVALID_ARG, "crisp_cache_attention")
+        if n_q_heads // self.n_kv_heads > B.MAX_GROUP:
+            raise B.CrispError(B.ERR_UNSUPPORTED, "crisp_cache_attention")
+        return max_new
+
+    @staticmethod
+    def _max_new(tokens, batch, cu_tokens):
+        """The items' largest number of tokens that the shapes allow."""
+        return tokens if cu_tokens is not None or batch == 0 else tokens // batch
 
     def _call(self, name, stream, *args):
         """The C call of that name on (cache, *args, stream), with the cache's device current.  (The answering loop calls
@@ -185,7 +204,7 @@ class CrispCache:
         batch = seq_ids.shape[0]
         pq, ids, cu = self._tokens("q", q, n, hq), self._list("seq_ids", seq_ids), self._list("cu_tokens", cu_tokens, batch + 1)
         if max_new is None:
-            max_new = n if cu_tokens is not None or batch == 0 else n // batch
+            max_new = self._max_new(n, batch, cu_tokens)
         plse = None
         if lse is not None:
             self._check("lse", lse, torch.float32)

@@ -149,6 +149,10 @@ class CrispAttention:
         """The output product of attention's o [tokens, n_q_heads, 128]."""
         return self.out(*quantize(o.view(o.shape[0], self.n_q_heads * HEAD), stream=stream), stream=stream)
 
+    def _same_device(self, cache):
+        if cache.device != self.qkv.device:
+            raise ValueError(f"the cache must be on {self.qkv.device}")
+
     def prompt(self, x, layer: CrispLayer, residual=None, *, cache: Optional[CrispCache] = None, seq_ids=None,
                cache_layer: int = 0, dense_below_tokens: int = 0, stream=None):
         """A whole prompt: x [layer.p.seq_len, in_features] through CrispLayer.forward; with a cache its K and V are kept there
@@ -162,7 +166,8 @@ class CrispAttention:
         if cache is not None:
             if seq_ids is None or seq_ids.shape != (1,):
                 raise ValueError("seq_ids must name one sequence")
-            cache.check_append(p.seq_len, self.n_kv_heads, seq_ids, layer=cache_layer)
+            self._same_device(cache)
+            cache_layer = cache.check_append(p.seq_len, self.n_kv_heads, seq_ids, layer=cache_layer)
         q, k, v, h = self.project(x, residual, stream=stream)
         o = layer.forward(q, k, v, stream=stream, dense_below_tokens=dense_below_tokens)
         if cache is not None:
@@ -173,6 +178,16 @@ class CrispAttention:
                max_new: Optional[int] = None, cache_layer: int = 0, stream=None):
         """New tokens of cached sequences, packed in x as in CrispCache.append, at their positions (int32 [tokens]): appended
         and attended to.  At cache_layer 0 the sequences grow by n_new (None: one token each).  Returns (out, h)."""
+        # (all that append and attention refuse on the host, before the sequences grow: tokens that are counted and not written
+        # would be read as they are)
+        if x.dim() != 2:
+            raise ValueError(f"x must be [tokens, {self.qkv.n_in}]")
+        self._same_device(cache)
+        tokens = x.shape[0]
+        cache_layer = cache.check_append(tokens, self.n_kv_heads, seq_ids, cu_tokens, n_new, cache_layer)
+        max_new = cache.check_attention(tokens, self.n_q_heads, seq_ids, cu_tokens, max_new)
+        if cache_layer == 0 and n_new is None and cu_tokens is None and tokens != seq_ids.shape[0]:
+            raise ValueError("without n_new there must be one token for each sequence")
         q, k, v, h = self.project(x, residual, positions, stream=stream)
         if cache_layer == 0:
             cache.reserve(seq_ids, n_new, stream)

@@ -186,3 +186,52 @@ def test_a_layer_s_calls_run_on_its_device(monkeypatch, stream, handle):
                                               "crisp_dense_prefill"] + 3 * ["crisp_poll_device_status"]
     assert all(device == 1 and at == handle for _, device, at in given)
     assert cuda.now == 0
+
+
+# ------------------------------------------------------------------------------------------------ an answer
+def test_answer_calls(log, block):
+    parts = ["rms_norm", "matmul", "rotary"], ["crisp_cache_append", "crisp_cache_attention", "quantize", "matmul"]
+    first, later = parts[0] + ["crisp_cache_reserve"] + parts[1], parts[0] + parts[1]
+    for kw, tokens, want in ((dict(), 3, first), (dict(cache_layer=1), 3, later), (dict(max_new=1), 3, first),
+                             (dict(n_new=ids(2, 2, 2)), 6, first), (dict(n_new=ids(2, 2, 2), max_new=2), 6, first),
+                             (dict(cu_tokens=ids(0, 1, 5, 5), n_new=ids(1, 4, 0)), 5, first), (dict(cache_layer=1), 6, later)):
+        log.clear()
+        block.answer(states(tokens), None, make_cache(log), ids(0, 4, 2), **kw)
+        assert log == want, kw
+
+
+@pytest.mark.parametrize("tokens,kw", [
+    (3, dict(heads=1)), (3, dict(heads=8)),                                               # another number of K/V heads
+    (3, dict(device=torch.device("cuda", 1))),
+    (3, dict(cu_tokens=ids(0, 1, 2))), (3, dict(cu_tokens=ids(0, 1, 2, 3).long())),       # lists of the wrong length or type
+    (3, dict(cu_tokens=ids(0, 0, 1, 1, 2, 2, 3, 3)[::2])), (3, dict(n_new=ids(1))), (3, dict(n_new=ids(1, 1, 1).float())),
+    (3, dict(seq_ids=ids(0, 1, 2).long())), (3, dict(seq_ids=ids(0, 1, 2)[None])),
+    (4, dict(n_new=ids(2, 1, 1))), (6, dict()), (0, dict()),                              # tokens that the sequences do not share out
+    (6, dict(n_new=ids(2, 2, 2), max_new=1)), (3, dict(max_new=-1)), (3, dict(max_new=1 << 31)), (3, dict(max_new=1.0)),
+    (3, dict(cache_layer=2)), (3, dict(cache_layer=-1)), (3, dict(cache_layer=0.0)),
+    (1025, dict(seq_ids=torch.zeros(1025, dtype=torch.int32)))])
+def test_a_refused_answer_leaves_the_sequences(log, block, tokens, kw):
+    kw = dict(kw)
+    cache = make_cache(log, kw.pop("heads", HKV), device=kw.pop("device", CPU))
+    with pytest.raises((ValueError, TypeError, crisp.CrispError)):
+        block.answer(states(tokens), None, cache, kw.pop("seq_ids", ids(0, 1, 2)), **kw)
+    assert log == []
+
+
+def test_answer_refuses_groups_that_attention_refuses(log):
+    block = crisp.CrispAttention(linear((17 + 2) * 128, HIDDEN), linear(HIDDEN, 17 * 128), crisp.CrispRotary(1e4), 17, 1)
+    with pytest.raises(crisp.CrispError):
+        block.answer(states(1), None, make_cache(log, heads=1), ids(0))
+    block = crisp.CrispAttention(linear((3 + 4) * 128, HIDDEN), linear(HIDDEN, 3 * 128), crisp.CrispRotary(1e4), 3, 2)
+    with pytest.raises(crisp.CrispError):
+        block.answer(states(1), None, make_cache(log, heads=2), ids(0))
+    assert log == []
+
+
+def test_prompt_refuses_a_cache_elsewhere(log, block):
+    cache = make_cache(log)
+    cache.device = torch.device("cuda", 1)
+    cache._check = lambda *args: None      # its lists are there too
+    with pytest.raises(ValueError):
+        block.prompt(states(300), make_layer(log, 300), cache=cache, seq_ids=ids(0))
+    assert log == []
