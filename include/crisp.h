@@ -409,7 +409,7 @@ int crisp_quantize(const void* x, int32_t n_rows, int32_t n_cols, void* codes, u
  * Root-mean-square norm of rows, with the residual's addition:
  *   h = x + residual, rounded to bf16 and stored in `sum` (residual and sum both NULL: h = x)
  *   y = h / sqrt(mean(h^2) + eps) * weight            (weight [n_cols] bf16, NULL: 1), the mean in fp32
- * (a row whose squares leave fp32 becomes 0),
+ * (a row whose squares go beyond fp32 becomes 0; of tiny rows nothing is lost; a row of zeros with eps = 0 is 0 / 0, NaN),
  * written either as bf16 `y` or as an operand, `codes` and `scales` (converted from fp32, not from bf16); the other is NULL.
  * (y is fp32 before it is converted: where a block's largest magnitude is within 48 * 2^-24 of the bound of a scale, the scale
  * may be the one on the other side; codes go with it.)

@@ -4,7 +4,8 @@
 // norm: h = bf16(x + residual) (or x), y = h / sqrt(mean(h^2) + eps) * weight.  A row lives in the registers of one CTA
 // between its only read and its only write: 8 bytes of traffic per element (x, residual, h, and one byte of codes makes 7)
 // instead of the 16 and more of separate passes.  What is normalised is h as stored, so that the result does not depend on
-// whether the addition was part of this call.  The sum of squares is held in fp32.
+// whether the addition was part of this call.  The sum of squares is held in fp32
+// (of tiny rows, of the row times 2^100: see kTiny).
 //
 // Measured: 131072 rows of 4096, addition, 8 bits out: 558 us, 6.7 TB/s; 9001 rows of 3584, 16 bits out: 20 us; one row: 1.9 us.
 // quantize, 32768 rows of 4096: 62.7 us, 6.4 TB/s; 6144 rows: 13.0 us.
@@ -44,8 +45,15 @@ __host__ __device__ constexpr int norm_ctas(int threads, bool residual) {
   return threads >= 512 ? 1024 / threads : (residual ? 768 : 1024) / (threads * norm_rows(threads));
 }
 
+// Below this mean of squares and eps, squares lose bits to fp32's range (down to it 2^-150 each, which is nothing).
+constexpr float kTinyMean = 0x1p-100f;
+
 // kThreads threads of a row hold kVecs vectors of 8 elements each; 16 neighbouring lanes hold a block of 128 columns.
-template <int kThreads, int kVecs, bool kResidual, bool kQuantize>
+//
+// kTiny: eps does not keep the mean above kTinyMean.  Rows below it are taken times 2^100, exact in bf16 and with squares below
+// 2^116, and eps times 2^200; the factor cancels.  Other calls do without the branch, in front of which the compiler moves
+// nothing (32768 rows of 4096 to 8 bits: 80 us without, 97 with; with addition 141 and 142).
+template <int kThreads, int kVecs, bool kResidual, bool kQuantize, bool kTiny>
 __global__ void __launch_bounds__(kThreads * norm_rows(kThreads), norm_ctas(kThreads, kResidual)) norm_kernel(const NormArgs a) {
   constexpr int kWarps = kThreads / 32, kRows = norm_rows(kThreads);
   __shared__ float part[2][kWarps < 4 ? 4 : kWarps];
@@ -114,7 +122,32 @@ __global__ void __launch_bounds__(kThreads * norm_rows(kThreads), norm_ctas(kThr
 #pragma unroll
       for (int i = 0; i < kWarps; ++i) ss += part[turn][i];
     }
-    const float m = ss / static_cast<float>(a.n_cols) + a.eps, s0 = rsqrtf(m);
+    float m = ss / static_cast<float>(a.n_cols) + a.eps;
+    if (kTiny && m < kTinyMean) {   // (the same for all of the row's threads)
+      ss = 0.f;
+#pragma unroll
+      for (int v = 0; v < kVecs; ++v) {
+        uint32_t* u = reinterpret_cast<uint32_t*>(&h[v]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float lo = __uint_as_float(u[i] << 16) * 0x1p100f, hi = __uint_as_float(u[i] & 0xffff0000u) * 0x1p100f;
+          ss = fmaf(lo, lo, fmaf(hi, hi, ss));
+          u[i] = __float_as_uint(hi) | __float_as_uint(lo) >> 16;
+        }
+      }
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+      if (kWarps > 1) {
+        __syncthreads();   // everybody has read this half of `part`
+        if (lane == 0) part[turn][warp] = ss;
+        __syncthreads();
+        ss = 0.f;
+#pragma unroll
+        for (int i = 0; i < kWarps; ++i) ss += part[turn][i];
+      }
+      m = ss / static_cast<float>(a.n_cols) + a.eps * 0x1p100f * 0x1p100f;
+    }
+    const float s0 = rsqrtf(m);
     // one step of Newton: half a rounding instead of two (not where squares have left fp32, and the row becomes 0)
     const float s = m < INFINITY ? fmaf(0.5f * s0, fmaf(-m * s0, s0, 1.f), s0) : s0;
 #pragma unroll
@@ -181,10 +214,11 @@ __global__ void __launch_bounds__(kQuantThreads) quantize_kernel(const void* x, 
   }
 }
 
-template <int kThreads, int kVecs>
+template <int kThreads, int kVecs, bool kTiny>
 int launch_norm(const NormArgs& a, int n_sm, cudaStream_t stream) {
-  void (*kernel)(NormArgs) = a.residual ? (a.codes ? norm_kernel<kThreads, kVecs, true, true> : norm_kernel<kThreads, kVecs, true, false>)
-                                        : (a.codes ? norm_kernel<kThreads, kVecs, false, true> : norm_kernel<kThreads, kVecs, false, false>);
+  void (*kernel)(NormArgs) =
+      a.residual ? (a.codes ? norm_kernel<kThreads, kVecs, true, true, kTiny> : norm_kernel<kThreads, kVecs, true, false, kTiny>)
+                 : (a.codes ? norm_kernel<kThreads, kVecs, false, true, kTiny> : norm_kernel<kThreads, kVecs, false, false, kTiny>);
   // A whole number of rounds of the CTAs that are resident at a time: one (131072 rows of 4096, with addition: 3 per SM 558 us,
   // 4 per SM 715, 8 per SM 590), or several where a CTA's rows are long or short, so that the CTAs of an SM fall out of step (16384
   // rows of 8192: 151 us with one round, 142 with four; 30000 rows of 2048: 72 and 68).
@@ -200,6 +234,18 @@ int launch_norm(const NormArgs& a, int n_sm, cudaStream_t stream) {
   return CRISP_OK;
 }
 
+template <bool kTiny>
+int launch_norm_cols(const NormArgs& a, int n_sm, cudaStream_t stream) {
+  if (a.n_cols <= 256) return launch_norm<32, 1, kTiny>(a, n_sm, stream);
+  if (a.n_cols <= 512) return launch_norm<32, 2, kTiny>(a, n_sm, stream);
+  if (a.n_cols <= 1024) return launch_norm<128, 1, kTiny>(a, n_sm, stream);
+  if (a.n_cols <= 2048) return launch_norm<128, 2, kTiny>(a, n_sm, stream);
+  if (a.n_cols <= 4096) return launch_norm<256, 2, kTiny>(a, n_sm, stream);
+  if (a.n_cols <= 8192) return launch_norm<512, 2, kTiny>(a, n_sm, stream);
+  if (a.n_cols <= 16384) return launch_norm<1024, 2, kTiny>(a, n_sm, stream);
+  return launch_norm<1024, 4, kTiny>(a, n_sm, stream);
+}
+
 }  // namespace
 
 int launch_rms_norm(const void* x, const void* residual, const void* weight, int n_rows, int n_cols, float eps, void* sum,
@@ -208,14 +254,7 @@ int launch_rms_norm(const void* x, const void* residual, const void* weight, int
   int n_sm = 0;
   const int rc = current_sm_count(&n_sm);
   if (rc != CRISP_OK) return rc;
-  if (n_cols <= 256) return launch_norm<32, 1>(a, n_sm, stream);
-  if (n_cols <= 512) return launch_norm<32, 2>(a, n_sm, stream);
-  if (n_cols <= 1024) return launch_norm<128, 1>(a, n_sm, stream);
-  if (n_cols <= 2048) return launch_norm<128, 2>(a, n_sm, stream);
-  if (n_cols <= 4096) return launch_norm<256, 2>(a, n_sm, stream);
-  if (n_cols <= 8192) return launch_norm<512, 2>(a, n_sm, stream);
-  if (n_cols <= 16384) return launch_norm<1024, 2>(a, n_sm, stream);
-  return launch_norm<1024, 4>(a, n_sm, stream);
+  return eps < kTinyMean ? launch_norm_cols<true>(a, n_sm, stream) : launch_norm_cols<false>(a, n_sm, stream);
 }
 
 int launch_quantize(const void* x, int n_rows, int n_cols, void* codes, uint8_t* scales, cudaStream_t stream) {

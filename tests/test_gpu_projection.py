@@ -116,6 +116,41 @@ def test_norm_extremes():
         check_norm(x[1:], torch.zeros_like(x[1:]), None, 0.0, quantized)
 
 
+@pytest.mark.parametrize("cols", [16, 512, 1024, 2048, 4096, 8192, 16384, 32768])
+@pytest.mark.parametrize("eps", [0.0, 1e-40, 1e-30])
+@pytest.mark.parametrize("residual,quantized", [(True, True), (True, False), (False, True), (False, False)])
+def test_norm_of_tiny_rows(cols, eps, residual, quantized):
+    """Rows whose squares are near fp32's smallest number or below it, down to bf16's smallest, beside others."""
+    x = normal(10, cols, seed=cols)
+    for i, e in enumerate((0, -40, -48, -52, -60, -70, -80, -100, -126, -131)):
+        x[i] = x[i] * 2.0 ** e
+    w = (1 + 0.3 * normal(cols, seed=cols + 2).float()).bfloat16()
+    check_norm(x, torch.zeros_like(x) if residual else None, w, eps, quantized)
+
+
+@pytest.mark.parametrize("cols,rows", [(256, 5000), (1024, 3000), (4096, 1500), (16384, 400)])
+def test_norm_of_many_tiny_rows(cols, rows):
+    """More rows than are resident at a time, tiny ones and others in turn; over themselves too."""
+    x = normal(rows, cols, seed=rows)
+    x[::3], x[1::3] = x[::3] * 2.0 ** -120, x[1::3] * 2.0 ** -61
+    check_norm(x, None, None, 0.0, False)
+    check_norm(x, normal(rows, cols, seed=1) * 2.0 ** -75, None, 0.0, True)
+    want, _ = crisp.rms_norm(x.to(DEV), eps=0.0)
+    from paper_2609_01925_b200 import binding as B
+    y = x.to(DEV)
+    B.check(B.crisp_rms_norm(y, None, None, 0.0, None, y, None, None), "crisp_rms_norm")
+    assert torch.equal(y, want)
+
+
+def test_norm_of_zeros_without_eps():
+    """0 / 0 is NaN, in its row alone."""
+    x = normal(5, 512, seed=9)
+    x[2] = 0.0
+    y = f64(crisp.rms_norm(x.to(DEV), eps=0.0)[0])
+    assert np.isnan(y[2]).all() and np.isfinite(np.delete(y, 2, 0)).all()
+    assert (f64(crisp.rms_norm(x.to(DEV), eps=1e-40)[0])[2] == 0).all()
+
+
 @pytest.mark.parametrize("cols", [80, 128, 4096])
 def test_norm_at_the_bound_of_a_scale(cols):
     """Rows whose largest result is 448 * 2^-8 but for the roundings, and the 16-bit numbers beside it."""
