@@ -183,14 +183,17 @@ __global__ void __launch_bounds__(kThreads * norm_rows(kThreads), norm_ctas(kThr
 
 constexpr int kQuantThreads = 256, kQuantRows = 4;
 
-// 2^tx_log threads share a row (16 for each block of 128 columns), every thread has one vector of kQuantRows rows.
+// 2^tx_log threads share a row (16 for each block of 128 columns), every thread has one vector of kQuantRows rows.  kWide: more
+// groups of columns than blockIdx.y counts, from 2^27 columns on (apart: asking costs ordinary calls up to 1 %).
+template <bool kWide>
 __global__ void __launch_bounds__(kQuantThreads) quantize_kernel(const void* x, int n_rows, int n_cols, int tx_log, void* codes,
                                                                  uint8_t* scales) {
   pdl_enter();
   const int tx = threadIdx.x & ((1 << tx_log) - 1), ty = threadIdx.x >> tx_log, step = kQuantThreads >> tx_log;
   const int blocks = (n_cols + kScaleBlock - 1) / kScaleBlock;
   const int scale_row = 4 * ((n_cols + kScaleWord - 1) / kScaleWord);
-  const long long vec = (static_cast<long long>(blockIdx.y) << tx_log) + tx;
+  const long long across = kWide ? static_cast<long long>(blockIdx.z) * gridDim.y + blockIdx.y : blockIdx.y;
+  const long long vec = (across << tx_log) + tx;
   const bool inside = vec * 8 < n_cols;
   const long long row0 = static_cast<long long>(blockIdx.x) * (step * kQuantRows) + ty;
   uint4 v[kQuantRows];
@@ -210,7 +213,7 @@ __global__ void __launch_bounds__(kQuantThreads) quantize_kernel(const void* x, 
       *reinterpret_cast<uint2*>(static_cast<char*>(codes) + static_cast<size_t>(row) * n_cols + vec * 8) = pack_codes(f, inverse);
       if ((tx & 15) == 0) scales[static_cast<size_t>(row) * scale_row + (vec >> 4)] = static_cast<uint8_t>(byte);
     }
-    if (blockIdx.y == 0 && tx < scale_row - blocks) scales[static_cast<size_t>(row) * scale_row + blocks + tx] = kScaleOne;
+    if (across == 0 && tx < scale_row - blocks) scales[static_cast<size_t>(row) * scale_row + blocks + tx] = kScaleOne;
   }
 }
 
@@ -261,11 +264,11 @@ int launch_quantize(const void* x, int n_rows, int n_cols, void* codes, uint8_t*
   int tx_log = 4;
   while (tx_log < 8 && (8 << tx_log) < n_cols) ++tx_log;
   const long long vecs = (static_cast<long long>(n_cols) + 7) / 8, rows = static_cast<long long>(kQuantThreads >> tx_log) * kQuantRows;
-  const long long across = (vecs + (1 << tx_log) - 1) >> tx_log;
-  if (across > 65535) return CRISP_ERR_UNSUPPORTED;   // from 2^27 columns on
-  const dim3 grid(static_cast<unsigned>((n_rows + rows - 1) / rows), static_cast<unsigned>(across));
-  CRISP_KERNEL("quantize", stream, launch_pdl(quantize_kernel, grid, dim3(kQuantThreads), 0, stream, x, n_rows, n_cols, tx_log,
-                                              codes, scales));
+  const long long across = (vecs + (1 << tx_log) - 1) >> tx_log, deep = (across + 65534) / 65535;   // 3 at most
+  const dim3 grid(static_cast<unsigned>((n_rows + rows - 1) / rows), static_cast<unsigned>((across + deep - 1) / deep),
+                  static_cast<unsigned>(deep));
+  CRISP_KERNEL("quantize", stream, launch_pdl(deep > 1 ? quantize_kernel<true> : quantize_kernel<false>, grid, dim3(kQuantThreads), 0,
+                                              stream, x, n_rows, n_cols, tx_log, codes, scales));
   CRISP_CUDA_TRY(cudaGetLastError(), "quantize: launch");
   return CRISP_OK;
 }

@@ -62,6 +62,30 @@ def test_quantize_borders():
     assert ((raw(codes)[nan] & 0x7f) == 0x7f).all()
 
 
+@pytest.mark.parametrize("rows,cols", [(1, (1 << 27) - 512), (5, 1 << 27), (3, (1 << 27) + 16), (1, (1 << 28) - 16), (2, 1 << 28)])
+def test_quantize_widest(rows, cols):
+    """Rows of up to 2^28 columns: each block of 128 is what it is in a row of its own, which the tests above pin."""
+    base = normal(4096, 128, seed=11, spread=40.0).to(DEV)
+    blocks = -(-cols // 128)
+    x = torch.empty(rows, blocks * 128, dtype=torch.bfloat16, device=DEV)
+    want_codes, want_scales = crisp.quantize(base)
+    for r in range(rows):
+        x[r] = base.roll(r, 0).repeat(-(-blocks // 4096), 1)[:blocks].view(-1)
+    x = x[:, :cols].contiguous()
+    codes, scales = crisp.quantize(x)
+    del x
+    for r in range(rows):
+        whole = cols // 128
+        part = lambda t: t.view(torch.uint8).roll(r, 0).repeat(-(-blocks // 4096), 1)[:blocks]  # noqa: E731
+        assert torch.equal(codes[r].view(torch.uint8)[:whole * 128], part(want_codes)[:whole].view(-1))
+        assert torch.equal(scales[r].view(torch.uint8)[:whole], part(want_scales[:, :1])[:whole, 0])
+        if whole < blocks:
+            last, scale = crisp.quantize(base.roll(r, 0)[whole % 4096, :cols % 128].view(1, -1).contiguous())
+            assert torch.equal(codes[r].view(torch.uint8)[whole * 128:], last.view(torch.uint8)[0])
+            assert scales[r].view(torch.uint8)[whole] == scale.view(torch.uint8)[0, 0]
+        assert bool((scales[r].view(torch.uint8)[blocks:] == 127).all())
+
+
 # ------------------------------------------------------------------------------------------------ norm
 NORM_ERROR = 48 * 2.0 ** -24   # of y in fp32, relative: at most 32 + 15 roundings in the sum of squares (halved by the root),
 #                                the division, the root (2 steps) and the two products
