@@ -12,8 +12,8 @@ LIB = os.path.join(HERE, "libcrisp.so")
 CALLS = os.path.join(HERE, "_calls.so")
 SOURCES = ["api.cu", "route.cu", "select.cu", "prefill.cu", "cache_pages.cu", "cache_attention.cu", "cache_prefill.cu",
            "cache_join.cu", "norm.cu", "matmul.cu", "matmul_pair.cu", "rotary.cu", "selftest.cu"]
-HEADERS = ["common.cuh", "cache.cuh", "cache_split.cuh", "cache_codes.cuh", "cache_ring.h", "operand.cuh", "matmul.cuh", "softmax_rows.cuh",
-           "sm100_ptx.cuh", os.path.join("..", "..", "include", "crisp.h")]
+HEADERS = ["common.cuh", "cache.cuh", "cache_split.cuh", "cache_codes.cuh", "cache_ring.h", "operand.cuh", "matmul.cuh", "matmul_wait.h",
+           "softmax_rows.cuh", "sm100_ptx.cuh", os.path.join("..", "..", "include", "crisp.h")]
 
 
 def _nvcc() -> str:

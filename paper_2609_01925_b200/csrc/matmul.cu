@@ -178,7 +178,7 @@ __global__ void __launch_bounds__(kMatmulThreads, 1) matmul_kernel(const __grid_
       if (lane == 0) mbar_arrive(&s.scale_full[slot]);
       __syncwarp();
     }
-    ok = ok && mbar_wait_warp(&s.done, 0, abort_flag);
+    ok = ok && mbar_wait_warp(&s.done, 0, abort_flag, a.wait_ns);
     if (ok) {
       tc_fence_after_sync();
       const int feature = f0 + warp * 32 + lane;
@@ -321,6 +321,7 @@ int launch_matmul(const void* codes, const uint8_t* scales, const void* w_codes,
   int rc = current_sm_count(&n_sm);
   if (rc != CRISP_OK) return rc;
   const int blocks = ceil_div(n_cols, kScaleBlock);
+  a.wait_ns = tile_wait_ns(blocks);
   Plan plan;
   if (n_rows > 64) plan_pairs(n_rows, n_out, blocks, n_sm, &plan);
   if (n_rows <= 256) {

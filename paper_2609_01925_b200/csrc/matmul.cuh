@@ -1,6 +1,7 @@
 // Shared declarations of the two kernels of the product (matmul.cu, matmul_pair.cu).
 #pragma once
 #include "cache.cuh"
+#include "matmul_wait.h"
 #include "operand.cuh"
 
 namespace crisp {
@@ -13,6 +14,7 @@ struct MatmulArgs {
   int tile_tokens;       // tokens of a tile
   int n_feature_tiles, split, stages, tmem_cols;
   long long n_tiles;
+  unsigned long long wait_ns;   // for a whole tile
 };
 
 constexpr int kPairTokens = 224;   // most tokens of a pair's tile: two accumulators and the scales fit TMEM's 512 columns

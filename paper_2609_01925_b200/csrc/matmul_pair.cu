@@ -236,7 +236,7 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_pair_kernel(const __grid_c
       int f0, t0;
       place(tile, f0, t0);
       const int buf = turn & 1;
-      ok = ok && mbar_wait_warp(&s.acc_full[buf], (turn >> 1) & 1, abort_flag);
+      ok = ok && mbar_wait_warp(&s.acc_full[buf], (turn >> 1) & 1, abort_flag, a.wait_ns);
       tc_fence_after_sync();
       const int n_tokens = min(a.tile_tokens, a.n_rows - t0);
       for (int c = group * kChunk; c < a.tile_tokens; c += 2 * kChunk) {

@@ -39,7 +39,8 @@ __device__ __forceinline__ bool mbar_try_wait(uint64_t* bar, uint32_t parity) {
 }
 // Bounded wait.  `abort_flag` (shared memory) lets one role's timeout end every other
 // role's waits quickly.  Gives up after kWaitLimitNs of wall time (every legitimate wait in these
-// kernels lasts microseconds).  Returns false when it gave up.
+// kernels lasts microseconds, but for a whole tile of a product of very many columns: matmul_wait.h).
+// Returns false when it gave up.
 constexpr unsigned long long kWaitLimitNs = 400ull * 1000ull * 1000ull;
 __device__ __forceinline__ unsigned long long global_timer_ns() {
   unsigned long long t;
@@ -64,8 +65,9 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, volati
 
 // Warp-uniform variant: every lane of the warp polls, and the result is agreed on by a vote, so the
 // warp stays converged for the warp-collective instructions that follow a wait.
-__device__ __forceinline__ bool mbar_wait_warp(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
-  const bool ok = mbar_wait(bar, parity, abort_flag);
+__device__ __forceinline__ bool mbar_wait_warp(uint64_t* bar, uint32_t parity, volatile int* abort_flag,
+                                               unsigned long long limit_ns = kWaitLimitNs) {
+  const bool ok = mbar_wait_limit(bar, parity, abort_flag, limit_ns);
   return __all_sync(0xffffffffu, ok);
 }
 

@@ -325,6 +325,30 @@ def test_product_over_many_tiles_is_exact(rows, n, cols):
     assert bool((buffer[rows:] == 7.0).all())
 
 
+@pytest.mark.parametrize("rows,n,cols", [(5, 130, 1 << 24), (300, 260, (1 << 22) + 16), (1, 1, 1 << 28)])
+def test_product_of_very_many_columns(rows, n, cols):
+    """Few elements of a row are not zero, the first and the last block's among them: exact."""
+    g = torch.Generator(device=DEV).manual_seed(cols)
+    at = torch.cat([torch.randint(0, cols, (400,), generator=g, device=DEV), torch.tensor([0, cols - 1, cols - 16], device=DEV)]).unique()
+    grid = torch.tensor([0x38, 0x40, 0xb8], dtype=torch.uint8, device=DEV)         # 1, 2, -1
+    number = torch.tensor([1.0, 2.0, -1.0], dtype=torch.float64, device=DEV)
+
+    def make(r):
+        pick = torch.randint(0, 3, (r, at.numel()), generator=g, device=DEV)
+        codes = torch.zeros(r, cols, dtype=torch.uint8, device=DEV)
+        codes[:, at] = grid[pick]
+        scales = torch.full((r, ref.scale_cols(cols)), 127, dtype=torch.uint8, device=DEV)
+        scales[:, ::3] = 128
+        value = number[pick] * torch.where(at // 128 % 3 == 0, 2.0, 1.0).double()
+        return (codes.view(torch.float8_e4m3fn), scales.view(torch.float8_e8m0fnu)), value
+
+    (a, av), (w, wv) = make(rows), make(n)
+    lin = crisp.CrispLinear(*w)
+    out = lin(*a)
+    lin.poll()
+    assert torch.equal(out, (av @ wv.t()).bfloat16())
+
+
 def test_product_extreme_scales_and_nan():
     """Scales whose products leave fp32 become 0 or infinity; a NaN code reaches its row of A, or its column, alone."""
     a, w = operand(20, 256, 3), operand(130, 256, 4)

@@ -249,3 +249,20 @@ def test_turns_of_zero_are_refused(scaling, kw):
     """None stands for the usual turns; zero is not taken for it."""
     with pytest.raises((ValueError, RuntimeError)):
         crisp.CrispRotary(5e5, scaling=scaling, factor=8.0, original=8192, **kw)
+
+
+def test_a_tile_of_many_columns_is_waited_for(tmp_path):
+    """The warps that write a tile wait for all of its columns: ten times as long as the product's own estimates say that a tile of
+    any documented size takes (pairs: 95 + 0.9 ns per token for a block, 224 tokens; a CTA alone: 520 ns), five times where CTAs
+    crowd an SM (four times as long)."""
+    import subprocess
+    source = tmp_path / "wait.cpp"
+    source.write_text('#include <cstdio>\n#include <cstdlib>\n#include "matmul_wait.h"\n'
+                      'int main(int n, char** a) { for (int i = 1; i < n; ++i) std::printf("%llu ", crisp::tile_wait_ns(std::atoi(a[i]))); }\n')
+    exe = str(tmp_path / "wait")
+    subprocess.run(["g++", "-std=c++17", "-I", os.path.join(ROOT, "paper_2609_01925_b200", "csrc"), "-o", exe, str(source)], check=True)
+    blocks = [1, 64, 16383, 16384, 100000, 1 << 20, 1 << 21]
+    waits = [int(w) for w in subprocess.run([exe, *map(str, blocks)], check=True, capture_output=True, text=True).stdout.split()]
+    for b, w in zip(blocks, waits):
+        assert w >= 10 * b * (95 + 0.9 * 224) and w >= 10 * b * 520 and w >= 5 * b * 520 * 4
+    assert waits[:3] == [400_000_000] * 3
