@@ -945,7 +945,7 @@ int crisp_rms_norm(const void* x, const void* residual, const void* weight, int3
   if (rc != CRISP_OK || n_rows == 0) return rc;
   // either 16 bits or codes with their scales; a sum exactly where there is something to add
   if (!x || (y != nullptr) == (codes != nullptr) || (codes != nullptr) != (scales != nullptr) ||
-      (residual != nullptr) != (sum != nullptr))
+      (residual != nullptr) != (sum != nullptr) || (sum && (sum == y || sum == codes)))
     return CRISP_ERR_INVALID_ARG;
   for (const void* p : {x, residual, weight, static_cast<const void*>(sum), static_cast<const void*>(y),
                         static_cast<const void*>(codes)})

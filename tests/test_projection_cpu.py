@@ -266,3 +266,11 @@ def test_a_tile_of_many_columns_is_waited_for(tmp_path):
     for b, w in zip(blocks, waits):
         assert w >= 10 * b * (95 + 0.9 * 224) and w >= 10 * b * 520 and w >= 5 * b * 520 * 4
     assert waits[:3] == [400_000_000] * 3
+
+
+def test_norm_refuses_one_place_for_two_outputs():
+    """The sum and the result over the same memory would leave one of them."""
+    lib = B.load()
+    for y, codes, scales in ((FAKE, None, None), (None, FAKE, 2 * FAKE)):
+        assert lib.crisp_rms_norm(3 * FAKE, 4 * FAKE, None, 4, 256, 1e-5, FAKE, y, codes, scales, None) == B.ERR_INVALID_ARG
+        assert lib.crisp_rms_norm(FAKE, 4 * FAKE, None, 4, 256, 1e-5, FAKE, y, codes, scales, None) == B.ERR_INVALID_ARG
