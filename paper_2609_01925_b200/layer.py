@@ -48,8 +48,12 @@ class CrispLayer:
         index = self.o.device.index
         if stream is None:
             stream = torch._C._cuda_getCurrentRawStream(index)
-        with torch.cuda.device(index):
-            B.check(getattr(B, name)(*args, stream), name)
+        if torch.cuda.current_device() == index:
+            rc = getattr(B, name)(*args, stream)
+        else:
+            with torch.cuda.device(index):
+                rc = getattr(B, name)(*args, stream)
+        B.check(rc, name)
 
     def route(self, q, k, stream=None):
         self._call("crisp_route", stream, self.p, q, k, self.route_ws, self.c_struct, self.pattern, self.p_v, self.p_s)
