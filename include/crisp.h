@@ -413,7 +413,7 @@ int crisp_quantize(const void* x, int32_t n_rows, int32_t n_cols, void* codes, u
  * written either as bf16 `y` or as an operand, `codes` and `scales` (converted from fp32, not from bf16); the other is NULL.
  * (y is fp32 before it is converted: where a block's largest magnitude is within 48 * 2^-24 of the bound of a scale, the scale
  * may be the one on the other side; codes go with it.)
- * sum may be x or residual, or y may be x: rows are read before they are written.  sum and y are two tensors, and no other
+ * sum may be x or residual, and y may be x: rows are read before they are written.  sum and y are two tensors, and no other
  * overlaps are allowed.  n_cols is a multiple of 16, at most 32768.
  */
 int crisp_rms_norm(const void* x, const void* residual, const void* weight, int32_t n_rows, int32_t n_cols, float eps,

@@ -213,12 +213,14 @@ class CrispCache:
             plse = lse.data_ptr()
         if o is not None:
             po = self._tokens("o", o, n, hq)
+            given = o
         else:
             o = torch.empty_like(q) if stream is None else self._new(q.shape, torch.bfloat16, stream)
             po = o.data_ptr()
+            given = None
         self._call("crisp_cache_attention", stream, layer, ids, cu, batch, n, max_new, hq, softmax_scale, pq, po, plse,
                    *self._attention_ws)
-        self._used(stream, q, seq_ids, cu_tokens, o, lse)
+        self._used(stream, q, seq_ids, cu_tokens, given, lse)
         return o
 
     def _torch_stream(self, stream):
@@ -228,9 +230,10 @@ class CrispCache:
         return torch.cuda.ExternalStream(stream, device=self.device) if stream else torch.cuda.default_stream(self.device)
 
     def _used(self, stream, *tensors):
-        """Tells the allocator that a call on a given stream uses these tensors, so that their memory is not handed out
-        again before it has run."""
-        if stream is None:
+        """Tells the allocator that a call on this stream uses these tensors, so that their memory is not handed out again before
+        it has run."""
+        if stream is None:   # (compiled: an answer comes here three times per layer and token)
+            B.calls().used(self.device.index, *tensors)
             return
         stream = self._torch_stream(stream)
         for t in tensors:

@@ -9,6 +9,7 @@
 #include <optional>
 
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
@@ -80,32 +81,33 @@ int int32(PyObject* o, const char* name) {
 }
 
 // The stream of a call: None is the device's current one, an int a handle (0: the default stream), anything else a
-// torch.cuda.Stream.  Outputs are allocated on it, and tensors that a call on a given stream uses are recorded with it, so
-// that their memory is not handed out again before the call has run.
+// torch.cuda.Stream.  Outputs are allocated on it, and tensors that a call uses are recorded with it (nothing happens where they
+// were allocated on it), so that their memory is not handed out again before the call has run.
 struct Where {
   c10::cuda::OptionalCUDAGuard device;
   c10::cuda::OptionalCUDAStreamGuard guard;
-  std::optional<c10::cuda::CUDAStream> given;
+  std::optional<c10::cuda::CUDAStream> stream;
   cudaStream_t raw;
 
-  Where(PyObject* stream, int index) {
-    if (stream == Py_None) {
+  Where(PyObject* o, int index) {
+    if (o == Py_None) {
       device.set_index(static_cast<c10::DeviceIndex>(index));
-      raw = c10::cuda::getCurrentCUDAStream(static_cast<c10::DeviceIndex>(index)).stream();
+      stream = c10::cuda::getCurrentCUDAStream(static_cast<c10::DeviceIndex>(index));
+      raw = stream->stream();
       return;
     }
-    if (PyLong_Check(stream)) {
-      void* handle = PyLong_AsVoidPtr(stream);
+    if (PyLong_Check(o)) {
+      void* handle = PyLong_AsVoidPtr(o);
       if (!handle && PyErr_Occurred()) throw Raised();
-      given = handle ? c10::cuda::getStreamFromExternal(static_cast<cudaStream_t>(handle), static_cast<c10::DeviceIndex>(index))
-                     : c10::cuda::getDefaultCUDAStream(static_cast<c10::DeviceIndex>(index));
+      stream = handle ? c10::cuda::getStreamFromExternal(static_cast<cudaStream_t>(handle), static_cast<c10::DeviceIndex>(index))
+                      : c10::cuda::getDefaultCUDAStream(static_cast<c10::DeviceIndex>(index));
     } else {
-      const long long id = field(stream, "stream_id"), at = field(stream, "device_index"), type = field(stream, "device_type");
-      given = c10::cuda::CUDAStream::unpack3(id, static_cast<c10::DeviceIndex>(at), static_cast<c10::DeviceType>(type));
+      const long long id = field(o, "stream_id"), at = field(o, "device_index"), type = field(o, "device_type");
+      stream = c10::cuda::CUDAStream::unpack3(id, static_cast<c10::DeviceIndex>(at), static_cast<c10::DeviceType>(type));
     }
-    if (given->device_index() != index) raise(PyExc_ValueError, "the stream must be of the tensors' device");
-    guard.reset_stream(*given);
-    raw = given->stream();
+    if (stream->device_index() != index) raise(PyExc_ValueError, "the stream must be of the tensors' device");
+    guard.reset_stream(*stream);
+    raw = stream->stream();
   }
   static long long field(PyObject* stream, const char* name) {
     PyObject* v = PyObject_GetAttrString(stream, name);
@@ -116,9 +118,11 @@ struct Where {
     return n;
   }
   void used(std::initializer_list<const Tensor*> tensors) const {
-    if (!given) return;
     for (const Tensor* t : tensors)
-      if (t && t->defined()) t->record_stream(given->unwrap());
+      if (t && t->defined()) record(*t, *stream);
+  }
+  static void record(const Tensor& t, c10::cuda::CUDAStream stream) {
+    c10::cuda::CUDACachingAllocator::recordStream(t.storage().data_ptr(), stream);
   }
 };
 
@@ -177,7 +181,7 @@ PyObject* quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const Where where(a[1], index);
     const Tensor codes = fresh({rows, cols}, kCodes, index), scales = fresh({rows, scale_cols(cols)}, kScales, index);
     done(quantize_fn(x.data_ptr(), rows, cols, codes.data_ptr(), static_cast<uint8_t*>(scales.data_ptr()), where.raw), "crisp_quantize");
-    where.used({&x, &codes, &scales});
+    where.used({&x});
     return tuple({&codes, &scales});
   });
 }
@@ -209,7 +213,7 @@ PyObject* rms_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
                      quantized ? nullptr : y.data_ptr(), quantized ? y.data_ptr() : nullptr,
                      quantized ? static_cast<uint8_t*>(scales.data_ptr()) : nullptr, where.raw),
          "crisp_rms_norm");
-    where.used({&x, &weight, &residual, &h, &y, &scales});
+    where.used({&x, &weight, &residual, a[4] != Py_None ? &h : nullptr});
     return quantized ? tuple({&y, &scales, &h}) : tuple({&y, &h});
   });
 }
@@ -234,7 +238,8 @@ PyObject* matmul(PyObject*, PyObject* const* a, Py_ssize_t n) {
     done(matmul_fn(codes.data_ptr(), static_cast<const uint8_t*>(s), w_codes.data_ptr(), static_cast<const uint8_t*>(w_scales.data_ptr()),
                    rows, n_out, cols, out.data_ptr(), ws.data_ptr(), static_cast<size_t>(ws.numel()), where.raw),
          "crisp_matmul");
-    where.used({&codes, &scales, &w_codes, &w_scales, &ws, &out});
+    where.used({&codes, &scales, a[5] != Py_None ? &out : nullptr});
+    if (a[6] != Py_None) where.used({&w_codes, &w_scales, &ws});   // (the weights' object outlives its calls on the current stream)
     return a[5] != Py_None ? Py_NewRef(a[5]) : THPVariable_Wrap(out);
   });
 }
@@ -268,7 +273,7 @@ PyObject* rotary_split(PyObject*, PyObject* const* a, Py_ssize_t n) {
       const char *at_k = at + 2 * kHead * hq, *at_v = at_k + 2 * kHead * hkv;
       done(rotary_fn(plan, rows, pos, first, hq, hkv, at, row, at_k, row, at_v, row, q.data_ptr(), k.data_ptr(), v.data_ptr(), where.raw),
            "crisp_rotary");
-      where.used({&qkv, &positions, &q, &k, &v});
+      where.used({&qkv, &positions});
     }
     return tuple({&q, &k, &v});
   });
@@ -299,9 +304,19 @@ PyObject* rotary_rotate(PyObject*, PyObject* const* a, Py_ssize_t n) {
       done(rotary_fn(plan, rows, pos, first, heads, 0, x.data_ptr(), rows > 1 ? x.stride(0) : heads * kHead, nullptr, 0, nullptr, 0,
                      out.data_ptr(), nullptr, nullptr, where.raw),
            "crisp_rotary");
-      where.used({&x, &positions, &out});
+      where.used({&x, &positions, a[4] != Py_None ? &out : nullptr});
     }
     return a[4] != Py_None ? Py_NewRef(a[4]) : THPVariable_Wrap(out);
+  });
+}
+
+// used(device, tensors...): a call on the device's current stream uses these tensors (or None), as in Where
+PyObject* used(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded<0>(n > 0 ? 0 : -1, [&] {
+    const auto stream = c10::cuda::getCurrentCUDAStream(static_cast<c10::DeviceIndex>(int32(a[0], "device")));
+    for (Py_ssize_t i = 1; i < n; ++i)
+      if (a[i] != Py_None) Where::record(tensor(a[i], "a tensor given to the call"), stream);
+    return Py_NewRef(Py_None);
   });
 }
 
@@ -324,7 +339,8 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 #define CRISP_CALL(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {CRISP_CALL(bind),   CRISP_CALL(quantize),     CRISP_CALL(rms_norm),
-                         CRISP_CALL(matmul), CRISP_CALL(rotary_split), CRISP_CALL(rotary_rotate), {nullptr, nullptr, 0, nullptr}};
+                         CRISP_CALL(matmul), CRISP_CALL(rotary_split), CRISP_CALL(rotary_rotate), CRISP_CALL(used),
+                         {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", "The calls around the attention.", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -53,7 +53,7 @@ class CrispLinear:
     """Weights [out_features, in_features] as an operand, and products with them.
 
     Products of one object may overlap, on any streams (they share a status word only), behind the object's creation, which
-    zeroes that word on the current stream.
+    zeroes that word on the current stream.  The object is kept until its calls have run.
     """
 
     def __init__(self, codes, scales):

@@ -265,6 +265,31 @@ def test_calls_on_a_given_stream(handle):
         assert all(torch.equal(s, t) for s, t in zip(a[:3], b[:3]))
 
 
+@pytest.mark.parametrize("given", [False, True])
+def test_inputs_of_another_stream_may_be_dropped(given):
+    """Tensors of the default stream, used by calls on a side stream (the current one, or given) that run late, and dropped right
+    behind them: their memory is not handed out before."""
+    block, *_ = make_block(170)
+    xs = [hidden(257, 171 + i).to(DEV) for i in range(4)]
+    residual, positions = hidden(257, 180).to(DEV), torch.arange(257, dtype=torch.int32, device=DEV)
+    want = [block.project(x, residual, positions) for x in xs]
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    got = []
+    for x in xs:
+        inputs = [t.clone() for t in (x, residual, positions)]
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(2000000)
+            got.append(block.project(*inputs, stream=side if given else None))
+        del inputs
+        for t in (x, residual, positions):
+            torch.empty_like(t).fill_(7)     # takes memory that was freed too early
+    torch.cuda.synchronize()
+    for a, b in zip(got, want):
+        assert all(torch.equal(s, t) for s, t in zip(a, b))
+
+
 def test_default_stream_as_zero():
     block, *_ = make_block(80)
     x = hidden(33, 81).to(DEV)

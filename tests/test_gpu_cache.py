@@ -992,3 +992,41 @@ def test_arguments_are_checked():
     c.reserve(ids[:0])
     c.free(ids[:0])
     c.poll()
+
+
+@pytest.mark.parametrize("given", [False, True])
+def test_inputs_of_another_stream_may_be_dropped(given):
+    """K, V, Q and lists of the default stream, used by calls on a side stream (the current one, or given) that run late, and
+    dropped right behind them: their memory is not handed out before."""
+    def run(side):
+        cache = crisp.CrispCache.allocate(8, 1, 2, 4)
+        k, v, q = (tokens(n, h, 90 + n).cuda() for n, h in ((130, 1), (130, 1), (130, 4)))
+        lists = [torch.tensor(x, dtype=torch.int32, device="cuda") for x in ([1], [130], [0, 130])]
+        torch.cuda.synchronize()
+        if side is None:
+            cache.reserve(lists[0], lists[1])
+            cache.append(k, v, lists[0], lists[2])
+            return cache, cache.attention(q, lists[0], lists[2])
+        kept = [k, v, q, *lists]
+        inputs = [t.clone() for t in kept]
+        side.wait_stream(torch.cuda.current_stream())
+        stream = side if given else None
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(2000000)
+            cache.reserve(inputs[3], inputs[4], stream)
+            cache.append(inputs[0], inputs[1], inputs[3], inputs[5], stream=stream)
+            o = cache.attention(inputs[2], inputs[3], inputs[5], stream=stream)
+        del inputs
+        for t in kept:
+            torch.empty_like(t).fill_(0)     # takes memory that was freed too early
+        torch.cuda.synchronize()
+        return cache, o
+
+    want, o = run(None)
+    got, o2 = run(torch.cuda.Stream())
+    torch.cuda.synchronize()
+    got.poll()
+    assert int(got.seq_lens[1]) == 130 and torch.equal(o, o2)
+    table = want.page_table[1, :2].long(), got.page_table[1, :2].long()
+    for name in ("k_codes", "v_codes", "k_scale", "v_scale"):
+        assert torch.equal(getattr(want, name)[0, table[0]].flatten()[:128 * 128], getattr(got, name)[0, table[1]].flatten()[:128 * 128])
