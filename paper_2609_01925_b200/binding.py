@@ -181,7 +181,6 @@ def load() -> ctypes.CDLL:
     return lib
 
 
-CALLS_PATH = os.path.join(_HERE, "_calls.so")
 _calls = None
 
 
@@ -190,12 +189,13 @@ def calls():
     Raises if either is missing."""
     global _calls
     if _calls is None:
-        lib = load()
-        if not os.path.exists(CALLS_PATH):
-            raise ImportError(f"{CALLS_PATH} not found: build it with `python -m paper_2609_01925_b200.build` "
+        from .build import calls_path
+        lib, path = load(), calls_path()
+        if not os.path.exists(path):
+            raise ImportError(f"{path} not found: build it with `python -m paper_2609_01925_b200.build` "
                               "(there is no fallback path)")
         name = __package__ + "._calls"
-        loader = importlib.machinery.ExtensionFileLoader(name, CALLS_PATH)
+        loader = importlib.machinery.ExtensionFileLoader(name, path)
         module = importlib.util.module_from_spec(importlib.util.spec_from_loader(name, loader))
         loader.exec_module(module)
         module.bind(CrispError, *(ctypes.cast(f, ctypes.c_void_p).value for f in (

@@ -1,4 +1,4 @@
-"""Builds the CUDA library (libcrisp.so) in-tree with nvcc for sm_100a, and the compiled part of the binding (_calls.so)."""
+"""Builds the CUDA library (libcrisp.so) in-tree with nvcc for sm_100a, and the compiled part of the binding (_calls.*.so)."""
 from __future__ import annotations
 
 import os
@@ -9,7 +9,6 @@ import sysconfig
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcrisp.so")
-CALLS = os.path.join(HERE, "_calls.so")
 SOURCES = ["api.cu", "route.cu", "select.cu", "prefill.cu", "cache_pages.cu", "cache_attention.cu", "cache_prefill.cu",
            "cache_join.cu", "norm.cu", "matmul.cu", "matmul_pair.cu", "rotary.cu", "selftest.cu"]
 HEADERS = ["common.cuh", "cache.cuh", "cache_split.cuh", "cache_codes.cuh", "cache_ring.h", "operand.cuh", "matmul.cuh", "matmul_wait.h",
@@ -21,10 +20,18 @@ def _nvcc() -> str:
     return cand if os.path.exists(cand) else "nvcc"
 
 
+def calls_path() -> str:
+    """The compiled part of the binding uses torch's and Python's C++ and C interfaces, which differ between versions: its name
+    says for which ones it was built, so that others do not load it."""
+    import torch
+    return os.path.join(HERE, f"_calls.{sys.implementation.cache_tag}-torch-{torch.__version__}.so")
+
+
 def needs_build() -> bool:
-    if not os.path.exists(LIB) or not os.path.exists(CALLS):
+    calls = calls_path()
+    if not os.path.exists(LIB) or not os.path.exists(calls):
         return True
-    t = min(os.path.getmtime(LIB), os.path.getmtime(CALLS))
+    t = min(os.path.getmtime(LIB), os.path.getmtime(calls))
     deps = [os.path.join(CSRC, f) for f in SOURCES + HEADERS + ["calls.cpp"]] + [os.path.abspath(__file__)]
     return any(os.path.getmtime(p) > t for p in deps)
 
@@ -52,18 +59,19 @@ def build(force: bool = False, verbose: bool = False) -> str:
 def build_calls() -> str:
     """Compile calls.cpp against the torch that is installed; returns the module's path."""
     import torch
+    path = calls_path()
     torch_dir = os.path.dirname(torch.__file__)
     cuda = os.path.dirname(os.path.dirname(_nvcc())) or "/usr/local/cuda"
     include = [os.path.join(torch_dir, "include"), os.path.join(torch_dir, "include", "torch", "csrc", "api", "include"),
                os.path.join(cuda, "include"), sysconfig.get_paths()["include"]]
     cmd = ["g++", "-O2", "-std=c++17", "-shared", "-fPIC", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
-           "-o", CALLS, os.path.join(CSRC, "calls.cpp")] + [f"-I{d}" for d in include] + [f"-L{os.path.join(torch_dir, 'lib')}"] + [
+           "-o", path, os.path.join(CSRC, "calls.cpp")] + [f"-I{d}" for d in include] + [f"-L{os.path.join(torch_dir, 'lib')}"] + [
            f"-l{x}" for x in ("torch", "torch_cpu", "torch_cuda", "torch_python", "c10", "c10_cuda")]
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
         sys.stderr.write(res.stdout + res.stderr)
-        raise RuntimeError("g++ failed building _calls.so")
-    return CALLS
+        raise RuntimeError("g++ failed building the compiled part of the binding")
+    return path
 
 
 if __name__ == "__main__":

@@ -274,3 +274,24 @@ def test_norm_refuses_one_place_for_two_outputs():
     for y, codes, scales in ((FAKE, None, None), (None, FAKE, 2 * FAKE)):
         assert lib.crisp_rms_norm(3 * FAKE, 4 * FAKE, None, 4, 256, 1e-5, FAKE, y, codes, scales, None) == B.ERR_INVALID_ARG
         assert lib.crisp_rms_norm(FAKE, 4 * FAKE, None, 4, 256, 1e-5, FAKE, y, codes, scales, None) == B.ERR_INVALID_ARG
+
+
+def test_the_compiled_calls_belong_to_their_torch(monkeypatch):
+    """Beside another torch or Python the module that was built for this one is neither loaded nor taken for up to date."""
+    import sys
+    import types
+    from paper_2609_01925_b200 import build
+    here = build.calls_path()
+    assert os.path.exists(here) and B.calls()
+    monkeypatch.setattr(B, "_calls", None)
+    with monkeypatch.context() as m:
+        m.setattr(torch, "__version__", "0.0.1+other")
+        assert build.calls_path() != here and build.needs_build()
+        with pytest.raises(ImportError):
+            B.calls()
+    with monkeypatch.context() as m:
+        m.setattr(sys, "implementation", types.SimpleNamespace(**{**vars(sys.implementation), "cache_tag": "other-99"}))
+        assert build.calls_path() != here and build.needs_build()
+        with pytest.raises(ImportError):
+            B.calls()
+    assert build.calls_path() == here and B.calls()
