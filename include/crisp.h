@@ -390,8 +390,8 @@ int crisp_cache_compact(const crisp_cache* c, int32_t* n_used, void* ws, size_t 
 
 /*
  * The way into and out of the attention of a layer (not part of the paper): the norm of the hidden states, their products
- * with the weights in 8 bits, and the rotary positions.  For these calls a size may be 0 (nothing is launched); rows and
- * columns are at most 2^28.
+ * with the weights in 8 bits, and the rotary positions.  For these calls a number of rows, tokens or output features may be 0
+ * (nothing is launched); rows and columns are at most 2^28.
  *
  * Operand of a product: a matrix [n_rows][n_cols], n_cols a multiple of 16, as
  *   codes  [n_rows][n_cols] e4m3 bytes, and

@@ -76,9 +76,9 @@ struct ProfScope {
 #ifdef __CUDACC__
 // Launch with programmatic dependent launch allowed: the kernel's CTAs may become resident while the kernel
 // before it on the stream is still running.  Every kernel launched this way calls pdl_enter() before it reads or
-// writes what another kernel may write or read (the products set up barriers and prefetch weights first), which lets the kernel after it do the same and then waits until the kernel before it has
-// completed and its writes are visible, so the stream's order is kept; what is saved is the launch latency
-// between two short kernels.  (A kernel that follows a memset or an event record simply starts after it.)
+// writes what another kernel may write or read (the products set up barriers and prefetch weights first), which
+// lets the kernel after it do the same and then waits until the kernel before it has completed and its writes are
+// visible, so the stream's order is kept; what is saved is the launch latency between two short kernels.  (A kernel that follows a memset or an event record simply starts after it.)
 template <typename... KArgs, typename... Args>
 inline void launch_pdl_cluster(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, int cluster, cudaStream_t stream,
                                Args&&... args) {

@@ -229,7 +229,8 @@ int launch_norm(const NormArgs& a, int n_sm, cudaStream_t stream) {
   static std::atomic<int> known[2][2][64];
   int per_sm = 0;
   constexpr int kRows = norm_rows(kThreads);
-  const int rc = resident_ctas(reinterpret_cast<const void*>(kernel), kThreads * kRows, known[a.residual != nullptr][a.codes != nullptr], &per_sm);
+  const int rc = resident_ctas(reinterpret_cast<const void*>(kernel), kThreads * kRows,
+                               known[a.residual != nullptr][a.codes != nullptr], &per_sm);
   if (rc != CRISP_OK) return rc;
   const int most = n_sm * per_sm * kRounds, rows = (a.n_rows + kRows - 1) / kRows;
   CRISP_KERNEL("rms_norm", stream, launch_pdl(kernel, dim3(rows < most ? rows : most), dim3(kThreads * kRows), 0, stream, a));
