@@ -323,3 +323,30 @@ def test_block_refusals():
         block.project(hidden(3, 1).to(DEV)[:, :256].contiguous())
     with pytest.raises(ValueError):
         block.project(hidden(3, 1).to(DEV), positions=torch.zeros(2, dtype=torch.int32, device=DEV))
+
+
+def test_refused_calls_leave_the_cache():
+    """A prompt or an answer that does not fit its layer or its cache raises, and no sequence has grown."""
+    block, *_ = make_block(95)
+    cache = crisp.CrispCache.allocate(8, HKV, 2, 4)
+    other = crisp.CrispCache.allocate(8, 2 * HKV, 2, 4)
+    ids = torch.zeros(1, dtype=torch.int32, device=DEV)
+    first, _ = block.prompt(hidden(130, 96).to(DEV), make_layer(130), cache=cache, seq_ids=ids, dense_below_tokens=1 << 20)
+    x, at = hidden(1, 97).to(DEV), torch.tensor([130], dtype=torch.int32, device=DEV)
+    wide = crisp.CrispLayer(crisp.make_params(130, 2 * HQ, HKV, sink_tokens=4))
+    for bad in (lambda: block.prompt(hidden(10, 98).to(DEV), make_layer(130)), lambda: block.prompt(hidden(131, 98).to(DEV), make_layer(130)),
+                lambda: block.prompt(hidden(130, 98).to(DEV), wide),
+                lambda: block.prompt(hidden(130, 98).to(DEV), make_layer(130), cache=other, seq_ids=ids),
+                lambda: block.answer(x, at, other, ids), lambda: block.answer(x, at, cache, ids, cu_tokens=ids),
+                lambda: block.answer(x, at, cache, ids, max_new=0), lambda: block.answer(x, at, cache, ids, n_new=ids.long()),
+                lambda: block.answer(x, at.long(), cache, ids), lambda: block.answer(x, at, cache, ids, cache_layer=1),
+                lambda: block.answer(torch.cat([x, x]), torch.cat([at, at + 1]), cache, ids)):
+        with pytest.raises((ValueError, crisp.CrispError)):
+            bad()
+    torch.cuda.synchronize()
+    assert cache.seq_lens.tolist() == [130, 0] and other.seq_lens.tolist() == [0, 0]
+    block.answer(x, at, cache, ids, max_new=1)
+    cache.poll()
+    other.poll()
+    block.poll()
+    assert cache.seq_lens.tolist() == [131, 0]
